@@ -419,6 +419,47 @@ int qadc_multi_index_slots(const uint32_t *cell_ids, int64_t n_lists, const int3
 int qadc_rotate(const float *rot, int d, const float *x, int64_t n, float *y, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * Operators of a language model next to the search.  Where the stored vectors are a model's hidden
+ * states and every id stands for the token that followed, the search is a step of the model's
+ * answer: these calls bring a state to the search and its neighbours into the next token's
+ * distribution.  The conventions at the top hold; matrices here may have rows that lie further
+ * apart than they are long (`ld`: elements from one row to the next, at least the row's length).
+ * Elements are of one of three types; sums and statistics are held in float32.
+ */
+#define QADC_TYPE_F32  0
+#define QADC_TYPE_F16  1  /* IEEE binary16 */
+#define QADC_TYPE_BF16 2  /* the upper half of a float32 */
+
+/*
+ * Layer norm.  For every row x of d elements
+ *     mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),
+ *     y[c] = (x[c] - mean) * rstd * weight[c] + bias[c]
+ * in float32, rounded once to `type`.  A row that holds an infinity or a NaN becomes NaN.
+ *   x [rows][ldx] of `type`;  y [rows][d] of `type` (output; may be x when ldx == d)
+ *   weight, bias [d] of `wtype`: QADC_TYPE_F32 or `type`; each may be NULL (1, 0)
+ *   eps >= 0;  mean, rstd [rows] f32 (outputs for the backward pass, each nullable)
+ */
+int qadc_layer_norm(const void *x, int64_t ldx, int type, const void *weight, const void *bias, int wtype,
+                    int64_t rows, int d, float eps, void *y, float *mean, float *rstd, void *stream);
+
+/*
+ * Its backward pass, with h = (x - mean) * rstd and g = dy * weight:
+ *     dx = rstd * (g - sum g / d - h * (sum g h / d)),  dweight = sum over rows of dy h,  dbias = sum over rows of dy
+ * in float32; dx is rounded once to `type`.  The sums over rows are added in a fixed order: equal
+ * calls give equal bits.  With rows = 0 dweight and dbias are zero.
+ *   dy [rows][lddy], x [rows][ldx] of `type`;  weight as above;  mean, rstd [rows] f32 of the forward pass
+ *   dx [rows][d] of `type` (output, nullable; may be dy or x when that is dense)
+ *   dweight, dbias [d] f32 (outputs, each nullable)
+ *   workspace >= qadc_layer_norm_workspace_bytes(rows, d), 16-byte aligned (0 and NULL without dweight and dbias); it need
+ *   not be cleared and is not left cleared.
+ */
+int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int type, const void *weight,
+                             int wtype, const float *mean, const float *rstd, int64_t rows, int d, void *dx,
+                             float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
+
+/*
  * Per-kernel timing for benchmarks (the paper reports Index / Tables / Scan times
  * separately, Section 4.3).  While enabled, the library launches the kernels named
  * below with a start and a stop HIP event attached to each dispatch (the kernel's own
@@ -436,7 +477,8 @@ int qadc_rotate(const float *rot, int d, const float *x, int64_t n, float *y, vo
 #define QADC_PROF_PREPARE    7  /* tables + quantizer + sampling kernel of qadc_search */
 #define QADC_PROF_ROTATE     8  /* qadc_rotate kernel */
 #define QADC_PROF_IVF_SHARED 9  /* shared-list scan kernel of qadc_ivf_search (large batches) */
-#define QADC_PROF_COUNT  10
+#define QADC_PROF_NORM       10 /* kernels of qadc_layer_norm and its backward pass */
+#define QADC_PROF_COUNT  11
 int qadc_profile_enable(int on);
 /* As qadc_profile_enable(1), but only the kernels of slot `which` carry events: their neighbours in
  * the stream are launched as in an untimed run. */

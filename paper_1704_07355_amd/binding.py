@@ -24,10 +24,13 @@ QADC_U8_4BIT, QADC_F32_4BIT, QADC_F32_8BIT, QADC_U8_8BIT, QADC_U8_6BIT = 0, 1, 2
 QADC_WS_SCAN_TOPK, QADC_WS_SCAN_F32_4BIT, QADC_WS_SCAN_F32_8BIT, QADC_WS_SEARCH, QADC_WS_SCAN_U8_8BIT = 0, 1, 2, 3, 4
 QADC_WS_SCAN_U8_6BIT = 5
 (QADC_PROF_SCAN, QADC_PROF_MERGE, QADC_PROF_SEED, QADC_PROF_IVF_INDEX, QADC_PROF_IVF_TABLES,
- QADC_PROF_TABLES, QADC_PROF_QUANTIZE, QADC_PROF_PREPARE, QADC_PROF_ROTATE, QADC_PROF_IVF_SHARED) = range(10)
+ QADC_PROF_TABLES, QADC_PROF_QUANTIZE, QADC_PROF_PREPARE, QADC_PROF_ROTATE, QADC_PROF_IVF_SHARED,
+ QADC_PROF_NORM) = range(11)
 QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
+QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16 = 0, 1, 2
 
 EXPORTS = (
+    "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
     "qadc_profile_enable", "qadc_profile_only", "qadc_profile_read", "qadc_workspace_bytes", "qadc_workspace_init",
@@ -131,6 +134,13 @@ def lib() -> ctypes.CDLL:
         L.qadc_multi_index_encode.restype = i32
         L.qadc_multi_index_slots.argtypes = [vp, i64, vp, i64, vp, vp]
         L.qadc_multi_index_slots.restype = i32
+        f32 = ctypes.c_float
+        L.qadc_layer_norm.argtypes = [vp, i64, i32, vp, vp, i32, i64, i32, f32, vp, vp, vp, vp]
+        L.qadc_layer_norm.restype = i32
+        L.qadc_layer_norm_backward.argtypes = [vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, i32, vp, vp, vp, vp, sz, vp]
+        L.qadc_layer_norm_backward.restype = i32
+        L.qadc_layer_norm_workspace_bytes.argtypes = [i64, i32]
+        L.qadc_layer_norm_workspace_bytes.restype = sz
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -559,3 +569,100 @@ def qadc_search_static(codebooks, queries, codes, R, init, out_idx, out_dist, nb
                                     _ptr(codes, torch.uint8), n, R, init, nbins, qmin_mode, _ptr(out_idx),
                                     _ptr(out_dist), _ptr(qluts_out, torch.uint8), _stream()))
     return out_idx, out_dist
+
+
+# ---------------------------------------------------------------------------------------------
+# operators of a language model next to the search
+
+_TYPES = {torch.float32: QADC_TYPE_F32, torch.float16: QADC_TYPE_F16, torch.bfloat16: QADC_TYPE_BF16}
+
+
+def _type(t) -> int:
+    if t.dtype not in _TYPES:
+        raise ValueError(f"expected float32, float16 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _matrix(t, dtype=None):
+    """Pointer and row distance of a matrix whose rows are dense but may lie apart."""
+    if t.dim() != 2:
+        raise ValueError("expected a matrix")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"expected {dtype}, got {t.dtype}")
+    rows, cols = t.shape
+    ld = t.stride(0) if rows > 1 else cols
+    if not t.is_cuda or (cols > 1 and rows > 0 and t.stride(1) != 1) or ld < cols:
+        raise ValueError("tensor must be a GPU matrix with dense rows that do not overlap")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _vector(t, n, dtype=None):
+    """Pointer of a dense vector of n elements, or None."""
+    if t is None:
+        return None
+    if t.numel() != n:
+        raise ValueError(f"expected {n} elements, got {t.numel()}")
+    return _ptr(t, dtype)
+
+
+def _weight_type(weight, bias, x) -> int:
+    types = {t.dtype for t in (weight, bias) if t is not None}
+    if len(types) > 1 or not types <= {torch.float32, x.dtype}:
+        raise ValueError("weight and bias must both be float32, or both of x's type")
+    return _TYPES[types.pop()] if types else QADC_TYPE_F32
+
+
+def _buffer(t, shape, dtype, device):
+    """The caller's output tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise ValueError(f"output must be {dtype} {tuple(shape)}")
+    return t
+
+
+def _scratch(workspace, need, device):
+    """The caller's workspace, or a new one of `need` bytes (not cleared); its size in bytes."""
+    if workspace is None:
+        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=device)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def qadc_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
+    """x [rows][d] (f32, f16 or bf16; rows may lie apart), weight, bias [d] (f32 or x's type) | None
+    -> (y [rows][d] of x's type, mean f32 [rows], rstd f32 [rows])."""
+    rows, d = x.shape
+    xp, ldx = _matrix(x)
+    y = _buffer(out, (rows, d), x.dtype, x.device)
+    mean = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _check(lib().qadc_layer_norm(xp, ldx, _type(x), _vector(weight, d), _vector(bias, d), _weight_type(weight, bias, x),
+                                 rows, d, eps, _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+    return y, mean, rstd
+
+
+def qadc_layer_norm_workspace_bytes(rows: int, d: int) -> int:
+    return int(lib().qadc_layer_norm_workspace_bytes(rows, d))
+
+
+def qadc_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None, out=None, need_dx=True, need_weights=True):
+    """dy, x [rows][d], weight [d] | None, mean, rstd f32 [rows] of qadc_layer_norm
+    -> (dx [rows][d] of x's type | None, dweight f32 [d] | None, dbias f32 [d] | None)."""
+    rows, d = x.shape
+    if tuple(dy.shape) != (rows, d):
+        raise ValueError("dy must have x's shape")
+    dyp, lddy = _matrix(dy, x.dtype)
+    xp, ldx = _matrix(x)
+    dx = _buffer(out, (rows, d), x.dtype, x.device) if need_dx else None
+    dw = db = None
+    size = 0
+    if need_weights:
+        dw = torch.empty((d,), dtype=torch.float32, device=x.device)
+        db = torch.empty((d,), dtype=torch.float32, device=x.device)
+        workspace, size = _scratch(workspace, qadc_layer_norm_workspace_bytes(rows, d), x.device)
+    else:
+        workspace = None
+    _check(lib().qadc_layer_norm_backward(dyp, lddy, xp, ldx, _type(x), _vector(weight, d), _weight_type(weight, None, x),
+                                          _vector(mean, rows, torch.float32), _vector(rstd, rows, torch.float32), rows, d,
+                                          _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, _stream()))
+    return dx, dw, db

@@ -94,6 +94,11 @@ int multi_index_group(const int32_t *, int64_t, int, int64_t, uint32_t *, int64_
 int multi_index_encode(const float *, int, const float *, int, int, const float *, int64_t, const int32_t *,
                        const uint32_t *, int64_t, uint8_t *, hipStream_t);
 int multi_index_slots(const uint32_t *, int64_t, const int32_t *, int64_t, int32_t *, hipStream_t);
+int layer_norm(const void *, int64_t, int, const void *, const void *, int, int64_t, int, float, void *, float *, float *,
+               hipStream_t);
+int layer_norm_backward(const void *, int64_t, const void *, int64_t, int, const void *, int, const float *, const float *,
+                        int64_t, int, void *, float *, float *, void *, size_t, hipStream_t);
+size_t layer_norm_workspace(int64_t, int);
 int workspace_init(void *, size_t, hipStream_t);
 int pq_train(const float *, int64_t, int, int, int, const int64_t *, int, float *, void *, size_t,
              hipStream_t);
@@ -278,6 +283,22 @@ int qadc_multi_index_slots(const uint32_t *cell_ids, int64_t n_lists, const int3
 {
     return qadc::multi_index_slots(cell_ids, n_lists, cells, count, slots, (hipStream_t)stream);
 }
+
+int qadc_layer_norm(const void *x, int64_t ldx, int type, const void *weight, const void *bias, int wtype, int64_t rows,
+                    int d, float eps, void *y, float *mean, float *rstd, void *stream)
+{
+    return qadc::layer_norm(x, ldx, type, weight, bias, wtype, rows, d, eps, y, mean, rstd, (hipStream_t)stream);
+}
+
+int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int type, const void *weight,
+                             int wtype, const float *mean, const float *rstd, int64_t rows, int d, void *dx,
+                             float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return qadc::layer_norm_backward(dy, lddy, x, ldx, type, weight, wtype, mean, rstd, rows, d, dx, dweight, dbias,
+                                     workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d) { return qadc::layer_norm_workspace(rows, d); }
 
 int qadc_profile_enable(int on) { return qadc::profile_enable(on); }
 

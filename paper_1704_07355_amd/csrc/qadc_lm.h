@@ -1,0 +1,66 @@
+// Element types and row access shared by the language-model operators (layer norm, 4-bit products, log probabilities).
+#pragma once
+
+#include "qadc_common.h"
+
+namespace qadc {
+
+inline size_t type_bytes(int type) { return type == QADC_TYPE_F32 ? 4 : 2; }
+inline bool type_ok(int type) { return type == QADC_TYPE_F32 || type == QADC_TYPE_F16 || type == QADC_TYPE_BF16; }
+
+// Sixteen bytes of a row.  Rows start at multiples of their element's size only; the memory unit takes wide loads and
+// stores at any such address, so no variant is kept for aligned rows.
+template <typename T>
+struct Pack {
+    static constexpr int N = 16 / (int)sizeof(T);
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+// Elements c .. c + N - 1 of a row of d, `fill` beyond its end.
+template <typename T>
+__device__ __forceinline__ void load_pack(const T *row, int64_t c, int64_t d, float fill, float (&v)[Pack<T>::N])
+{
+    constexpr int N = Pack<T>::N;
+    if (c + N <= d) {
+        const typename Pack<T>::V p = *reinterpret_cast<const typename Pack<T>::V *>(row + c);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (float)p[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = c + e < d ? (float)row[c + e] : fill;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_pack(T *row, int64_t c, int64_t d, const float (&v)[Pack<T>::N])
+{
+    constexpr int N = Pack<T>::N;
+    if (c + N <= d) {
+        typename Pack<T>::V p;
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = (T)v[e];
+        *reinterpret_cast<typename Pack<T>::V *>(row + c) = p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (c + e < d) row[c + e] = (T)v[e];
+    }
+}
+
+// Sum over the wavefront, in every lane.
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) v += __shfl_xor(v, s);
+    return v;
+}
+
+// Runs F<T>::run(args...) for the element type `type`, T = float, _Float16 or __bf16.
+#define QADC_BY_TYPE(type, call)                             \
+    switch (type) {                                          \
+    case QADC_TYPE_F32: { using T = float; call; } break;    \
+    case QADC_TYPE_F16: { using T = _Float16; call; } break; \
+    default: { using T = __bf16; call; } break;              \
+    }
+
+}  // namespace qadc
