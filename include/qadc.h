@@ -460,6 +460,43 @@ int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
 size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
 
 /*
+ * Products with 4-bit weights that share a scale by groups of `group` consecutive inputs:
+ *     w[n][k] = (q[n][k] - z[n][k / group]) * s[n][k / group],   y[i][n] = sum_k x[i][k] w[n][k] + bias[n]
+ * with sums in float32, rounded once to `type`.  Weights are brought into the kernels' order once, by
+ * qadc_pack_weights4: 16 outputs x 128 inputs at a time, the 16 bytes of every lane of a wavefront side by
+ * side, the scales and zero points of 16 outputs together.
+ *   codes  [N][ceil(K/2)] u8: byte j of a row holds weight 2j in its low nibble and 2j + 1 in its high nibble
+ *          (the standard code layout; the last high nibble of an odd K is not read)
+ *   scales [N][ceil(K/group)] of `stype`: QADC_TYPE_F16 or QADC_TYPE_BF16
+ *   zeros  [N][ceil(K/group)] u8, any value, or NULL: 8 everywhere
+ *   group  32, 64 or a multiple of 128;  the last group of a row may be shorter
+ *   packed >= qadc_weights4_bytes(N, K, group, zeros != NULL) bytes, 16-byte aligned (output)
+ * The struct lives in host memory; `packed` is a device pointer.
+ */
+typedef struct qadc_weights4 {
+    const void *packed;
+    int64_t N;   /* outputs */
+    int K;       /* inputs, at most 2^24 */
+    int group;
+    int stype;
+    int has_zeros;
+} qadc_weights4;
+
+size_t qadc_weights4_bytes(int64_t N, int K, int group, int has_zeros);
+int qadc_pack_weights4(const uint8_t *codes, const void *scales, int stype, const uint8_t *zeros, int64_t N, int K,
+                       int group, void *packed, void *stream);
+
+/*
+ * The product itself, meant for a few rows (one token of each of a batch of sequences).
+ *   x [M][ldx] of `type`, M >= 0;  bias [N] f32 or NULL;  y [M][ldy] of `type` (output; must not overlap x)
+ * For every type of x the weights enter exactly; x enters exactly too (a float32 x as the sum of three
+ * bfloat16 numbers).  The zero points are taken off after the products, so a row of x that holds an
+ * infinity or a NaN gives NaN for every output (or an infinity).
+ */
+int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_t M, const float *bias, void *y,
+                 int64_t ldy, void *stream);
+
+/*
  * Per-kernel timing for benchmarks (the paper reports Index / Tables / Scan times
  * separately, Section 4.3).  While enabled, the library launches the kernels named
  * below with a start and a stop HIP event attached to each dispatch (the kernel's own
@@ -478,7 +515,8 @@ size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
 #define QADC_PROF_ROTATE     8  /* qadc_rotate kernel */
 #define QADC_PROF_IVF_SHARED 9  /* shared-list scan kernel of qadc_ivf_search (large batches) */
 #define QADC_PROF_NORM       10 /* kernels of qadc_layer_norm and its backward pass */
-#define QADC_PROF_COUNT  11
+#define QADC_PROF_LINEAR4    11 /* kernels of qadc_linear4 */
+#define QADC_PROF_COUNT  12
 int qadc_profile_enable(int on);
 /* As qadc_profile_enable(1), but only the kernels of slot `which` carry events: their neighbours in
  * the stream are launched as in an untimed run. */

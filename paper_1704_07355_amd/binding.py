@@ -25,12 +25,13 @@ QADC_WS_SCAN_TOPK, QADC_WS_SCAN_F32_4BIT, QADC_WS_SCAN_F32_8BIT, QADC_WS_SEARCH,
 QADC_WS_SCAN_U8_6BIT = 5
 (QADC_PROF_SCAN, QADC_PROF_MERGE, QADC_PROF_SEED, QADC_PROF_IVF_INDEX, QADC_PROF_IVF_TABLES,
  QADC_PROF_TABLES, QADC_PROF_QUANTIZE, QADC_PROF_PREPARE, QADC_PROF_ROTATE, QADC_PROF_IVF_SHARED,
- QADC_PROF_NORM) = range(11)
+ QADC_PROF_NORM, QADC_PROF_LINEAR4) = range(12)
 QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
 QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16 = 0, 1, 2
 
 EXPORTS = (
     "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
+    "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
     "qadc_profile_enable", "qadc_profile_only", "qadc_profile_read", "qadc_workspace_bytes", "qadc_workspace_init",
@@ -50,6 +51,12 @@ class qadc_ivf_index(ctypes.Structure):
                 ("ids", ctypes.c_void_p), ("codebooks", ctypes.c_void_p), ("d", ctypes.c_int),
                 ("m", ctypes.c_int), ("K", ctypes.c_int), ("n", ctypes.c_int64),
                 ("halves", ctypes.c_void_p), ("cell_ids", ctypes.c_void_p), ("Kh", ctypes.c_int)]
+
+
+class qadc_weights4(ctypes.Structure):
+    """Mirror of the C struct (include/qadc.h); `tensor` keeps the packed weights alive."""
+    _fields_ = [("packed", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int), ("group", ctypes.c_int),
+                ("stype", ctypes.c_int), ("has_zeros", ctypes.c_int)]
 
 
 class QadcError(RuntimeError):
@@ -141,6 +148,12 @@ def lib() -> ctypes.CDLL:
         L.qadc_layer_norm_backward.restype = i32
         L.qadc_layer_norm_workspace_bytes.argtypes = [i64, i32]
         L.qadc_layer_norm_workspace_bytes.restype = sz
+        L.qadc_weights4_bytes.argtypes = [i64, i32, i32, i32]
+        L.qadc_weights4_bytes.restype = sz
+        L.qadc_pack_weights4.argtypes = [vp, vp, i32, vp, i64, i32, i32, vp, vp]
+        L.qadc_pack_weights4.restype = i32
+        L.qadc_linear4.argtypes = [ctypes.POINTER(qadc_weights4), vp, i64, i32, i64, vp, vp, i64, vp]
+        L.qadc_linear4.restype = i32
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -666,3 +679,40 @@ def qadc_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None, out=None
                                           _vector(mean, rows, torch.float32), _vector(rstd, rows, torch.float32), rows, d,
                                           _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, _stream()))
     return dx, dw, db
+
+
+def qadc_weights4_bytes(N: int, K: int, group: int, has_zeros) -> int:
+    return int(lib().qadc_weights4_bytes(N, K, group, int(bool(has_zeros))))
+
+
+def qadc_pack_weights4(codes, scales, zeros, K, group):
+    """codes u8 [N][ceil(K/2)], scales f16 or bf16 [N][ceil(K/group)], zeros u8 like scales | None -> qadc_weights4."""
+    N = codes.shape[0]
+    groups = -(-K // group) if group > 0 else 0
+    if tuple(codes.shape) != (N, -(-K // 2)) or tuple(scales.shape) != (N, groups):
+        raise ValueError(f"expected codes [N][{-(-K // 2)}] and scales [N][{groups}]")
+    if zeros is not None and tuple(zeros.shape) != (N, groups):
+        raise ValueError(f"expected zeros [N][{groups}]")
+    stype = _type(scales)
+    packed = torch.empty((max(16, qadc_weights4_bytes(N, K, group, zeros is not None)),), dtype=torch.uint8, device=codes.device)
+    _check(lib().qadc_pack_weights4(_ptr(codes, torch.uint8), _ptr(scales), stype, _ptr(zeros, torch.uint8), N, K, group,
+                                    _ptr(packed), _stream()))
+    w = qadc_weights4(packed.data_ptr(), N, K, group, stype, int(zeros is not None))
+    w.tensor = packed
+    return w
+
+
+def qadc_linear4(weights, x, bias=None, out=None):
+    """weights of qadc_pack_weights4, x [M][K] (f32, f16 or bf16; rows may lie apart), bias f32 [N] | None -> y [M][N] of x's type."""
+    M, K = x.shape
+    if K != weights.K:
+        raise ValueError(f"weights of {weights.K} inputs, x of {K}")
+    xp, ldx = _matrix(x)
+    if out is None:
+        out = torch.empty((M, weights.N), dtype=x.dtype, device=x.device)
+    elif tuple(out.shape) != (M, weights.N):
+        raise ValueError(f"output must be {(M, weights.N)}")
+    yp, ldy = _matrix(out, x.dtype)
+    _check(lib().qadc_linear4(ctypes.byref(weights), xp, ldx, _type(x), M, _vector(bias, weights.N, torch.float32), yp, ldy,
+                              _stream()))
+    return out

@@ -99,6 +99,9 @@ int layer_norm(const void *, int64_t, int, const void *, const void *, int, int6
 int layer_norm_backward(const void *, int64_t, const void *, int64_t, int, const void *, int, const float *, const float *,
                         int64_t, int, void *, float *, float *, void *, size_t, hipStream_t);
 size_t layer_norm_workspace(int64_t, int);
+size_t weights4_bytes(int64_t, int, int, int);
+int pack_weights4(const uint8_t *, const void *, int, const uint8_t *, int64_t, int, int, void *, hipStream_t);
+int linear4(const qadc_weights4 *, const void *, int64_t, int, int64_t, const float *, void *, int64_t, hipStream_t);
 int workspace_init(void *, size_t, hipStream_t);
 int pq_train(const float *, int64_t, int, int, int, const int64_t *, int, float *, void *, size_t,
              hipStream_t);
@@ -299,6 +302,23 @@ int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
 }
 
 size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d) { return qadc::layer_norm_workspace(rows, d); }
+
+size_t qadc_weights4_bytes(int64_t N, int K, int group, int has_zeros)
+{
+    return qadc::weights4_bytes(N, K, group, has_zeros);
+}
+
+int qadc_pack_weights4(const uint8_t *codes, const void *scales, int stype, const uint8_t *zeros, int64_t N, int K,
+                       int group, void *packed, void *stream)
+{
+    return qadc::pack_weights4(codes, scales, stype, zeros, N, K, group, packed, (hipStream_t)stream);
+}
+
+int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_t M, const float *bias, void *y,
+                 int64_t ldy, void *stream)
+{
+    return qadc::linear4(w, x, ldx, type, M, bias, y, ldy, (hipStream_t)stream);
+}
 
 int qadc_profile_enable(int on) { return qadc::profile_enable(on); }
 

@@ -1,0 +1,170 @@
+"""Products with 4-bit weights and group scales against the formula in 64 bits.
+
+Tolerances: weights and x enter the products exactly, so what is off is float32 addition.  With e = 2^-24, a product and the
+sums up to it have magnitudes of at most (16 + q) |x| before the zero point is taken off, (16 + z) |x| for what is taken off;
+over a group of G inputs that is S = sum |x| (32 + z) at most, and chains of additions are no longer than 64 in a group and
+K / group + 64 over the groups.  So y is off by at most e ((64 + 8) sum_g |s| S_g + (K / group + 64) sum |x w|) and its rounding.
+"""
+
+import pytest
+
+import torch
+
+from lm_common import DEV, EPS, LEAST, TYPES, UNIT, apart, gen, within
+
+pytestmark = pytest.mark.gpu
+
+
+def make(N, K, group, type, zeros, seed):
+    g = gen(seed)
+    groups = -(-K // group)
+    codes = torch.randint(0, 256, (N, -(-K // 2)), generator=g, device=DEV, dtype=torch.uint8)
+    stype = torch.bfloat16 if type == "bf16" else torch.float16
+    scales = (0.01 * torch.randn((N, groups), generator=g, device=DEV)).to(stype)
+    z = torch.randint(0, 16, (N, groups), generator=g, device=DEV, dtype=torch.uint8) if zeros else None
+    return codes, scales, z
+
+
+def check(y, x, codes, scales, z, K, group, type, bias=None):
+    q = torch.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[0], -1)[:, :K].double()
+    of = torch.arange(K, device=DEV) // group
+    zk = torch.full_like(q, 8.0) if z is None else z.double()[:, of]
+    sk = scales.double()[:, of]
+    x64 = x.double()
+    w = ((q - zk) * sk).t().contiguous()
+    want = x64 @ w
+    tol = EPS * (72.0 * (x64.abs() @ ((32.0 + zk) * sk.abs()).t().contiguous()) + (K / group + 64.0) * (x64.abs() @ w.abs()))
+    if bias is not None:
+        want = want + bias.double()
+        tol = tol + EPS * (want.abs() + bias.double().abs())
+    within(y, want, tol * (1 + UNIT[type]) + UNIT[type] * want.abs() + LEAST[type], "y")
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("group,zeros", [(32, True), (32, False), (64, True), (64, False), (128, True), (128, False), (384, True)])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 16, 128), (1, 17, 129), (2, 100, 33), (3, 257, 1000), (4, 64, 2048), (5, 33, 515),
+                                   (8, 48, 640), (9, 1000, 300), (16, 31, 4096), (17, 40, 777), (32, 80, 256), (33, 15, 1025),
+                                   (64, 129, 500), (65, 20, 130), (130, 18, 260)])
+def test_product(M, N, K, group, zeros, type):
+    import paper_1704_07355_amd as Q
+    codes, scales, z = make(N, K, group, type, zeros, M * 7 + N + K)
+    x = torch.randn((M, K), generator=gen(K), device=DEV).to(TYPES[type])
+    w = Q.qadc_pack_weights4(codes, scales, z, K, group)
+    check(Q.qadc_linear4(w, x), x, codes, scales, z, K, group, type)
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("M,N,K,group", [(1, 5000, 4096, 128), (1, 20000, 1000, 32), (7, 40000, 512, 64), (24, 10007, 5000, 32),
+                                         (1, 300, 20000, 64), (40, 4100, 3000, 128), (2, 70000, 600, 32), (16, 256, 17000, 128)])
+def test_large_products(M, N, K, group, type):
+    import paper_1704_07355_amd as Q
+    codes, scales, z = make(N, K, group, type, True, N)
+    x = (torch.randn((M, K), generator=gen(M), device=DEV) + 0.5).to(TYPES[type])
+    w = Q.qadc_pack_weights4(codes, scales, z, K, group)
+    check(Q.qadc_linear4(w, x), x, codes, scales, z, K, group, type)
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("M,N,K,ldx,ldy", [(1, 70, 300, 300, 70), (6, 70, 301, 305, 83), (20, 100, 1000, 1003, 101)])
+def test_rows_apart_bias_and_output(M, N, K, ldx, ldy, type):
+    import paper_1704_07355_amd as Q
+    codes, scales, z = make(N, K, 64, type, True, 3)
+    x = torch.randn((M, K), generator=gen(4), device=DEV).to(TYPES[type])
+    bias = torch.randn((N,), generator=gen(5), device=DEV)
+    w = Q.qadc_pack_weights4(codes, scales, z, K, 64)
+    out = apart(torch.zeros((M, N), dtype=TYPES[type], device=DEV), ldy, 1)
+    got = Q.qadc_linear4(w, apart(x, ldx, 1), bias, out=out)
+    check(got, x, codes, scales, z, K, 64, type, bias)
+    assert torch.equal(got, Q.qadc_linear4(w, x, bias))
+    between = torch.as_strided(out, (M, ldy), (ldy, 1))[:-1, N:]
+    assert torch.isnan(between).all()  # nothing is written between the rows
+
+
+def test_all_zero_points_and_extreme_codes():
+    """Zero points are any byte; all codes 0 and all 15; scales 0 and negative."""
+    import paper_1704_07355_amd as Q
+    N, K, G = 48, 256, 64
+    x = torch.randn((3, K), generator=gen(1), device=DEV)
+    scales = torch.tensor([0.0, -0.5, 2.0, 0.01], device=DEV).half().expand(N, 4).contiguous()
+    for byte in (0x00, 0xFF):
+        codes = torch.full((N, K // 2), byte, dtype=torch.uint8, device=DEV)
+        for value in (0, 15, 255):
+            z = torch.full((N, 4), value, dtype=torch.uint8, device=DEV)
+            check(Q.qadc_linear4(Q.qadc_pack_weights4(codes, scales, z, K, G), x), x, codes, scales, z, K, G, "f32")
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+def test_rows_of_x_that_are_not_finite_stay_alone(type):
+    import paper_1704_07355_amd as Q
+    N, K = 100, 700
+    codes, scales, z = make(N, K, 32, type, True, 6)
+    w = Q.qadc_pack_weights4(codes, scales, z, K, 32)
+    for M in (6, 20):
+        x = torch.randn((M, K), generator=gen(7), device=DEV).to(TYPES[type])
+        clean = Q.qadc_linear4(w, x)
+        x[1, 5], x[3, 699], x[4, 64] = float("inf"), float("nan"), -float("inf")
+        y = Q.qadc_linear4(w, x)
+        bad = torch.zeros((M,), dtype=torch.bool, device=DEV)
+        bad[[1, 3, 4]] = True
+        assert not torch.isfinite(y[bad]).any() and torch.equal(y[~bad], clean[~bad])
+
+
+def test_small_and_large_magnitudes():
+    """x of 1e-30 and 1e30 in float32 (its three parts stay apart), of the range's ends in binary16 and bfloat16."""
+    import paper_1704_07355_amd as Q
+    N, K, G = 33, 384, 128
+    for type, sizes in (("f32", (1e-30, 1e30)), ("bf16", (1e-30, 1e30)), ("f16", (1e-6, 3e4))):
+        codes, scales, z = make(N, K, G, type, True, 8)
+        w = Q.qadc_pack_weights4(codes, scales, z, K, G)
+        for size in sizes:
+            x = (size * (torch.rand((5, K), generator=gen(9), device=DEV) - 0.5)).to(TYPES[type])
+            check(Q.qadc_linear4(w, x), x, codes, scales, z, K, G, type)
+
+
+def test_no_rows_streams_and_equal_bits():
+    import paper_1704_07355_amd as Q
+    codes, scales, z = make(3000, 2000, 128, "bf16", False, 10)
+    w = Q.qadc_pack_weights4(codes, scales, z, 2000, 128)
+    x = torch.randn((12, 2000), generator=gen(11), device=DEV).bfloat16()
+    assert Q.qadc_linear4(w, x[:0]).shape == (0, 3000)
+    y = Q.qadc_linear4(w, x)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        other = Q.qadc_linear4(w, x)
+    s.synchronize()
+    assert torch.equal(y, other)
+
+
+def test_packed_weights_beyond_2_gib():
+    """Offsets into the packed weights pass 32 bits: the last outputs of 5 G weights."""
+    import paper_1704_07355_amd as Q
+    N, K, G = 1_250_003, 4096, 128
+    codes = torch.zeros((N, K // 2), dtype=torch.uint8, device=DEV)
+    scales = torch.ones((N, K // G), dtype=torch.float16, device=DEV)
+    tail = torch.randint(0, 256, (40, K // 2), generator=gen(12), device=DEV, dtype=torch.uint8)
+    codes[-40:] = tail
+    w = Q.qadc_pack_weights4(codes, scales, None, K, G)
+    del codes
+    x = torch.randn((1, K), generator=gen(13), device=DEV)
+    y = Q.qadc_linear4(w, x)
+    check(y[:, -40:], x, tail, scales[-40:], None, K, G, "f32")
+    check(y[:, :40], x, torch.zeros_like(tail), scales[:40], None, K, G, "f32")
+
+
+def test_refusals_of_the_binding():
+    import paper_1704_07355_amd as Q
+    codes, scales, z = make(20, 100, 32, "f16", True, 1)
+    w = Q.qadc_pack_weights4(codes, scales, z, 100, 32)
+    x = torch.randn((2, 100), device=DEV)
+    for bad in (lambda: Q.qadc_pack_weights4(codes[:, :49], scales, z, 100, 32), lambda: Q.qadc_pack_weights4(codes, scales, z, 100, 64),
+                lambda: Q.qadc_pack_weights4(codes, scales, z[:, :3], 100, 32), lambda: Q.qadc_pack_weights4(codes.int(), scales, z, 100, 32),
+                lambda: Q.qadc_linear4(w, x[:, :99]), lambda: Q.qadc_linear4(w, x.double()),
+                lambda: Q.qadc_linear4(w, x, torch.zeros((19,), device=DEV)),
+                lambda: Q.qadc_linear4(w, x, out=torch.empty((2, 20), dtype=torch.float16, device=DEV))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(Q.QadcError):  # scales of float32
+        Q.qadc_pack_weights4(codes, scales.float(), z, 100, 32)
+    with pytest.raises(Q.QadcError):  # a group of 48
+        Q.qadc_pack_weights4(codes, scales[:, :3].contiguous(), None, 100, 48)

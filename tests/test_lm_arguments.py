@@ -31,3 +31,32 @@ def test_layer_norm_backward():
     assert f(PTR, 8, PTR, 7, 0, None, 0, PTR, PTR, 100, 8, PTR, PTR, PTR, PTR, need, None) == Q.QADC_EINVAL
     assert f(PTR, 9, PTR + 8, 8, 0, None, 0, PTR, PTR, 100, 8, PTR, PTR, PTR, PTR, need, None) == Q.QADC_EINVAL  # dx = dy, apart
     assert f(PTR, 8, PTR, 8, 7, None, 0, PTR, PTR, 100, 8, PTR, PTR, PTR, PTR, need, None) == Q.QADC_EINVAL
+
+
+def test_weights4_and_linear4():
+    import ctypes
+    L = Q.lib()
+    size = Q.qadc_weights4_bytes
+    assert size(16, 128, 128, 0) == 1024 + 32 and size(16, 128, 128, 1) == 1024 + 48
+    assert size(17, 129, 32, 1) == 4 * 1024 + 2 * 5 * 48
+    for bad in ((0, 128, 128, 0), (16, 0, 128, 0), (16, (1 << 24) + 1, 128, 0), (16, 128, 48, 0), (16, 128, 0, 0), (16, 128, 192, 0),
+                (1 << 31, 128, 128, 0)):
+        assert size(*bad) == 0
+    f = L.qadc_pack_weights4
+    assert f(PTR, PTR, 0, None, 16, 128, 128, PTR, None) == Q.QADC_EINVAL      # float32 scales
+    assert f(None, PTR, 1, None, 16, 128, 128, PTR, None) == Q.QADC_EINVAL
+    assert f(PTR, PTR, 1, None, 16, 128, 128, PTR + 8, None) == Q.QADC_EINVAL  # not aligned
+    w = Q.qadc_weights4(PTR, 16, 128, 128, 1, 0)
+    g = lambda w, *a: L.qadc_linear4(None if w is None else ctypes.byref(w), *a)
+    assert g(w, None, 128, 0, 0, None, None, 16, None) == Q.QADC_OK            # nothing to do
+    assert g(None, PTR, 128, 0, 1, None, PTR, 16, None) == Q.QADC_EINVAL
+    assert g(w, None, 128, 0, 1, None, PTR, 16, None) == Q.QADC_EINVAL
+    assert g(w, PTR, 127, 0, 1, None, PTR, 16, None) == Q.QADC_EINVAL
+    assert g(w, PTR, 128, 0, 1, None, PTR, 15, None) == Q.QADC_EINVAL
+    assert g(w, PTR, 128, 5, 1, None, PTR, 16, None) == Q.QADC_EINVAL
+    assert g(w, PTR, 128, 0, -1, None, PTR, 16, None) == Q.QADC_EINVAL
+    for field, value in (("packed", None), ("group", 100), ("stype", 0), ("N", 0), ("K", 0)):
+        bad = Q.qadc_weights4(PTR, 16, 128, 128, 1, 0)
+        setattr(bad, field, value)
+        assert g(bad, PTR, 128, 0, 1, None, PTR, 16, None) == Q.QADC_EINVAL
+    assert b"qadc_linear4" in L.qadc_last_error()
