@@ -497,6 +497,60 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
                  int64_t ldy, void *stream);
 
 /*
+ * Log probabilities of given tokens, with the entropy and the likeliest alternatives.  For every row, with
+ * x[v] = scale * logits[v]:
+ *     lse = log sum_v exp x[v],  logp[t] = x[tokens[t]] - lse,  entropy = lse - sum_v p[v] x[v],  p = exp(x - lse),
+ * and the k tokens with the largest logits, in the order (logit descending, token ascending), with their x - lse.
+ * Sums in float32.  A logit of -inf is a token that is masked out: p = 0, and it adds nothing to the entropy.
+ * A row with nothing left has lse = -inf, entropy 0 and every log probability -inf.  A row that holds a NaN or +inf has
+ * lse, entropy and log probabilities NaN; its alternatives are still ordered, a NaN before +inf.
+ *   logits [rows][ld] of `type`, V <= ld of them per row;  scale > 0 (the inverse of a temperature)
+ *   tokens [rows][T] i32, 0 <= T <= QADC_MAX_R, NULL when T = 0: an entry outside [0, V) is an unused slot, its logp is 0
+ *   k      0..QADC_MAX_ALTERNATIVES
+ *   logp [rows][T], lse [rows], entropy [rows] f32;  top_idx [rows][k] u32, top_logp [rows][k] f32 (outputs; lse, entropy
+ *   nullable; when V < k the tail is padded with 0xFFFFFFFF and -inf)
+ *   workspace >= qadc_token_logprobs_workspace_bytes(rows, V, k), 256-byte aligned, cleared once as above
+ */
+#define QADC_MAX_ALTERNATIVES 128
+int qadc_token_logprobs(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const int32_t *tokens,
+                        int T, int k, float *logp, float *lse, float *entropy, uint32_t *top_idx, float *top_logp,
+                        void *workspace, size_t workspace_bytes, void *stream);
+size_t qadc_token_logprobs_workspace_bytes(int64_t rows, int V, int k);
+
+/*
+ * The gradient of sum dlogp logp + sum dentropy entropy with respect to the logits:
+ *     dlogits[v] = scale * (sum_t dlogp[t] (1 if tokens[t] = v, else 0, - p[v]) - dentropy p[v] (x[v] - lse + entropy))
+ * in float32, rounded once to `type`; unused slots give nothing, a token given twice gives both its shares.  A masked
+ * token (logit -inf) has p = 0; a row with nothing left (lse = -inf) gets zeros.
+ *   lse, entropy [rows] f32 as qadc_token_logprobs wrote them (entropy is read only with dentropy)
+ *   dlogp [rows][T] f32 (NULL when T = 0);  dentropy [rows] f32 or NULL
+ *   dlogits [rows][ldd] of `type` (output; may be logits when ldd == ld)
+ */
+int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale,
+                                 const int32_t *tokens, int T, const float *lse, const float *entropy, const float *dlogp,
+                                 const float *dentropy, void *dlogits, int64_t ldd, void *stream);
+
+/*
+ * The tokens of the nearest stored states, mixed into a model's log probabilities.  Every neighbour i of a row votes for
+ * values[ids[i]] with a weight that falls with its distance:
+ *     P(t) = sum_i w_i (values[ids[i]] = t),  w = softmax over the row of -beta * distance
+ *     knn[t] = log P(tokens[t]),   mix[t] = log((1 - lambda) exp lm_logp[t] + lambda P(tokens[t]))
+ * all in float32 and in the logarithm, so that small weights are not lost.  ids and dist are what a search wrote: a
+ * neighbour with an id >= n (0xFFFFFFFF padding) or a distance that is not finite is left out.  A row without neighbours
+ * has knn = -inf and mix = lm_logp (no weight is taken from the model).  A negative token is an unused slot: knn and mix
+ * are 0.
+ *   ids  [rows][R] u32;  1 <= R <= QADC_MAX_R
+ *   dist [rows][R] f32 (dist_bytes = 4), or u8 quantized sums (dist_bytes = 1)
+ *   step [rows] f32 or NULL: the distance is step[row] * dist (`delta` of qadc_quantize_luts), 1 without
+ *   values [n] i32: the token that followed each stored state;  beta >= 0
+ *   tokens [rows][T] i32, lm_logp [rows][T] f32, T >= 0;  0 <= lambda <= 1
+ *   mix, knn [rows][T] f32 (outputs; knn nullable)
+ */
+int qadc_neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const float *step, int64_t rows, int R,
+                       const int32_t *values, int64_t n, float beta, const int32_t *tokens, int T, const float *lm_logp,
+                       float lambda, float *mix, float *knn, void *stream);
+
+/*
  * Per-kernel timing for benchmarks (the paper reports Index / Tables / Scan times
  * separately, Section 4.3).  While enabled, the library launches the kernels named
  * below with a start and a stop HIP event attached to each dispatch (the kernel's own
@@ -516,7 +570,9 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
 #define QADC_PROF_IVF_SHARED 9  /* shared-list scan kernel of qadc_ivf_search (large batches) */
 #define QADC_PROF_NORM       10 /* kernels of qadc_layer_norm and its backward pass */
 #define QADC_PROF_LINEAR4    11 /* kernels of qadc_linear4 */
-#define QADC_PROF_COUNT  12
+#define QADC_PROF_LOGPROBS   12 /* kernels of qadc_token_logprobs and its backward pass */
+#define QADC_PROF_MIX        13 /* kernel of qadc_neighbour_mix */
+#define QADC_PROF_COUNT  14
 int qadc_profile_enable(int on);
 /* As qadc_profile_enable(1), but only the kernels of slot `which` carry events: their neighbours in
  * the stream are launched as in an untimed run. */

@@ -25,13 +25,15 @@ QADC_WS_SCAN_TOPK, QADC_WS_SCAN_F32_4BIT, QADC_WS_SCAN_F32_8BIT, QADC_WS_SEARCH,
 QADC_WS_SCAN_U8_6BIT = 5
 (QADC_PROF_SCAN, QADC_PROF_MERGE, QADC_PROF_SEED, QADC_PROF_IVF_INDEX, QADC_PROF_IVF_TABLES,
  QADC_PROF_TABLES, QADC_PROF_QUANTIZE, QADC_PROF_PREPARE, QADC_PROF_ROTATE, QADC_PROF_IVF_SHARED,
- QADC_PROF_NORM, QADC_PROF_LINEAR4) = range(12)
+ QADC_PROF_NORM, QADC_PROF_LINEAR4, QADC_PROF_LOGPROBS, QADC_PROF_MIX) = range(14)
 QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
 QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16 = 0, 1, 2
+QADC_MAX_ALTERNATIVES = 128
 
 EXPORTS = (
     "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
     "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
+    "qadc_token_logprobs", "qadc_token_logprobs_workspace_bytes", "qadc_token_logprobs_backward", "qadc_neighbour_mix",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
     "qadc_profile_enable", "qadc_profile_only", "qadc_profile_read", "qadc_workspace_bytes", "qadc_workspace_init",
@@ -154,6 +156,14 @@ def lib() -> ctypes.CDLL:
         L.qadc_pack_weights4.restype = i32
         L.qadc_linear4.argtypes = [ctypes.POINTER(qadc_weights4), vp, i64, i32, i64, vp, vp, i64, vp]
         L.qadc_linear4.restype = i32
+        L.qadc_token_logprobs.argtypes = [vp, i64, i32, i64, i32, f32, vp, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.qadc_token_logprobs.restype = i32
+        L.qadc_token_logprobs_workspace_bytes.argtypes = [i64, i32, i32]
+        L.qadc_token_logprobs_workspace_bytes.restype = sz
+        L.qadc_token_logprobs_backward.argtypes = [vp, i64, i32, i64, i32, f32, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.qadc_token_logprobs_backward.restype = i32
+        L.qadc_neighbour_mix.argtypes = [vp, vp, i32, vp, i64, i32, vp, i64, f32, vp, i32, vp, f32, vp, vp, vp]
+        L.qadc_neighbour_mix.restype = i32
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -716,3 +726,73 @@ def qadc_linear4(weights, x, bias=None, out=None):
     _check(lib().qadc_linear4(ctypes.byref(weights), xp, ldx, _type(x), M, _vector(bias, weights.N, torch.float32), yp, ldy,
                               _stream()))
     return out
+
+
+def qadc_token_logprobs_workspace_bytes(rows: int, V: int, k: int) -> int:
+    return int(lib().qadc_token_logprobs_workspace_bytes(rows, V, k))
+
+
+def _tokens(tokens, rows):
+    """Pointer and number per row of the given tokens, i32 [rows][T] or None."""
+    if tokens is None:
+        return None, 0
+    if tokens.dim() != 2 or tokens.shape[0] != rows:
+        raise ValueError(f"expected tokens [{rows}][T]")
+    return _ptr(tokens, torch.int32), tokens.shape[1]
+
+
+def qadc_token_logprobs(logits, tokens=None, k=0, scale=1.0, workspace=None):
+    """logits [rows][V] (f32, f16 or bf16; rows may lie apart), tokens i32 [rows][T] | None
+    -> (logp f32 [rows][T], lse f32 [rows], entropy f32 [rows], top_idx i32-bits-of-u32 [rows][k], top_logp f32 [rows][k])."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    tp, T = _tokens(tokens, rows)
+    dev = logits.device
+    f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
+    logp, lse, entropy, top_logp = f32(rows, T), f32(rows), f32(rows), f32(rows, k)
+    top_idx = torch.empty((rows, k), dtype=torch.int32, device=dev)
+    if workspace is None:
+        need = qadc_token_logprobs_workspace_bytes(rows, V, k)
+        workspace = qadc_workspace_init(torch.empty((max(need, 256),), dtype=torch.uint8, device=dev))
+    _check(lib().qadc_token_logprobs(xp, ld, _type(logits), rows, V, scale, tp, T, k, _ptr(logp), _ptr(lse), _ptr(entropy),
+                                     _ptr(top_idx), _ptr(top_logp), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size(), _stream()))
+    return logp, lse, entropy, top_idx, top_logp
+
+
+def qadc_token_logprobs_backward(logits, tokens, lse, entropy, dlogp, dentropy=None, scale=1.0, out=None):
+    """The gradient with respect to the logits, [rows][V] of their type; entropy may be None without dentropy."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    tp, T = _tokens(tokens, rows)
+    if dentropy is not None and entropy is None:
+        raise ValueError("dentropy needs the entropy")
+    if out is None:
+        out = torch.empty((rows, V), dtype=logits.dtype, device=logits.device)
+    elif tuple(out.shape) != (rows, V):
+        raise ValueError(f"output must be {(rows, V)}")
+    op, ldd = _matrix(out, logits.dtype)
+    _check(lib().qadc_token_logprobs_backward(xp, ld, _type(logits), rows, V, scale, tp, T, _vector(lse, rows, torch.float32),
+                                              _vector(entropy, rows, torch.float32),
+                                              _vector(dlogp, rows * T, torch.float32) if T else None,
+                                              _vector(dentropy, rows, torch.float32), op, ldd, _stream()))
+    return out
+
+
+def qadc_neighbour_mix(ids, dist, values, tokens, lm_logp, lam, beta, step=None):
+    """ids i32-bits-of-u32 [rows][R], dist f32 or u8 [rows][R], values i32 [n], tokens i32 [rows][T], lm_logp f32 [rows][T],
+    step f32 [rows] | None -> (mix f32 [rows][T], knn f32 [rows][T])."""
+    rows, R = ids.shape
+    if tuple(dist.shape) != (rows, R) or dist.dtype not in (torch.float32, torch.uint8):
+        raise ValueError("dist must be float32 or uint8 and have the shape of ids")
+    if ids.dtype not in (torch.int32, torch.uint32):
+        raise ValueError(f"expected 32-bit ids, got {ids.dtype}")
+    if tokens is None or tuple(lm_logp.shape) != tuple(tokens.shape):
+        raise ValueError("lm_logp must have the shape of tokens")
+    tp, T = _tokens(tokens, rows)
+    mix = torch.empty((rows, T), dtype=torch.float32, device=ids.device)
+    knn = torch.empty((rows, T), dtype=torch.float32, device=ids.device)
+    _check(lib().qadc_neighbour_mix(_ptr(ids), _ptr(dist), dist.element_size(), _vector(step, rows, torch.float32), rows, R,
+                                    _ptr(values, torch.int32), values.numel(), beta, tp, T, _ptr(lm_logp, torch.float32), lam,
+                                    _ptr(mix), _ptr(knn), _stream()))
+    return mix, knn

@@ -102,6 +102,13 @@ size_t layer_norm_workspace(int64_t, int);
 size_t weights4_bytes(int64_t, int, int, int);
 int pack_weights4(const uint8_t *, const void *, int, const uint8_t *, int64_t, int, int, void *, hipStream_t);
 int linear4(const qadc_weights4 *, const void *, int64_t, int, int64_t, const float *, void *, int64_t, hipStream_t);
+int token_logprobs(const void *, int64_t, int, int64_t, int, float, const int32_t *, int, int, float *, float *, float *,
+                   uint32_t *, float *, void *, size_t, hipStream_t);
+size_t token_logprobs_workspace(int64_t, int, int);
+int token_logprobs_backward(const void *, int64_t, int, int64_t, int, float, const int32_t *, int, const float *, const float *,
+                            const float *, const float *, void *, int64_t, hipStream_t);
+int neighbour_mix(const uint32_t *, const void *, int, const float *, int64_t, int, const int32_t *, int64_t, float,
+                  const int32_t *, int, const float *, float, float *, float *, hipStream_t);
 int workspace_init(void *, size_t, hipStream_t);
 int pq_train(const float *, int64_t, int, int, int, const int64_t *, int, float *, void *, size_t,
              hipStream_t);
@@ -318,6 +325,32 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
                  int64_t ldy, void *stream)
 {
     return qadc::linear4(w, x, ldx, type, M, bias, y, ldy, (hipStream_t)stream);
+}
+
+int qadc_token_logprobs(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const int32_t *tokens,
+                        int T, int k, float *logp, float *lse, float *entropy, uint32_t *top_idx, float *top_logp,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    return qadc::token_logprobs(logits, ld, type, rows, V, scale, tokens, T, k, logp, lse, entropy, top_idx, top_logp,
+                                workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+size_t qadc_token_logprobs_workspace_bytes(int64_t rows, int V, int k) { return qadc::token_logprobs_workspace(rows, V, k); }
+
+int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale,
+                                 const int32_t *tokens, int T, const float *lse, const float *entropy, const float *dlogp,
+                                 const float *dentropy, void *dlogits, int64_t ldd, void *stream)
+{
+    return qadc::token_logprobs_backward(logits, ld, type, rows, V, scale, tokens, T, lse, entropy, dlogp, dentropy, dlogits,
+                                         ldd, (hipStream_t)stream);
+}
+
+int qadc_neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const float *step, int64_t rows, int R,
+                       const int32_t *values, int64_t n, float beta, const int32_t *tokens, int T, const float *lm_logp,
+                       float lambda, float *mix, float *knn, void *stream)
+{
+    return qadc::neighbour_mix(ids, dist, dist_bytes, step, rows, R, values, n, beta, tokens, T, lm_logp, lambda, mix, knn,
+                               (hipStream_t)stream);
 }
 
 int qadc_profile_enable(int on) { return qadc::profile_enable(on); }

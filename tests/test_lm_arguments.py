@@ -60,3 +60,46 @@ def test_weights4_and_linear4():
         setattr(bad, field, value)
         assert g(bad, PTR, 128, 0, 1, None, PTR, 16, None) == Q.QADC_EINVAL
     assert b"qadc_linear4" in L.qadc_last_error()
+
+
+def test_token_logprobs():
+    L = Q.lib()
+    need = Q.qadc_token_logprobs_workspace_bytes(4, 1000, 10)
+    assert need > 0
+    for bad in ((0, 1000, 10), (4, 0, 10), (4, 1000, -1), (4, 1000, 129)):
+        assert Q.qadc_token_logprobs_workspace_bytes(*bad) == 0
+    P = PTR
+    f = L.qadc_token_logprobs
+    assert f(None, 1000, 0, 0, 1000, 1.0, None, 0, 0, None, None, None, None, None, None, 0, None) == Q.QADC_OK
+    ok = [P, 1000, 0, 4, 1000, 1.0, P, 2, 10, P, P, P, P, P, P, need, None]
+    for at, value, code in ((0, None, Q.QADC_EINVAL), (1, 999, Q.QADC_EINVAL), (2, 3, Q.QADC_EINVAL), (3, -1, Q.QADC_EINVAL),
+                            (4, 0, Q.QADC_EINVAL), (5, 0.0, Q.QADC_EINVAL), (5, float("nan"), Q.QADC_EINVAL), (6, None, Q.QADC_EINVAL),
+                            (7, -1, Q.QADC_EINVAL), (7, 1025, Q.QADC_EINVAL), (8, 129, Q.QADC_EINVAL), (9, None, Q.QADC_EINVAL),
+                            (12, None, Q.QADC_EINVAL), (13, None, Q.QADC_EINVAL), (14, None, Q.QADC_ENOMEM), (15, need - 1, Q.QADC_ENOMEM)):
+        args = list(ok)
+        args[at] = value
+        assert f(*args) == code, (at, value)
+    assert b"qadc_token_logprobs" in L.qadc_last_error()
+    g = L.qadc_token_logprobs_backward
+    assert g(None, 1000, 0, 0, 1000, 1.0, None, 0, None, None, None, None, None, 1000, None) == Q.QADC_OK
+    ok = [P, 1000, 0, 4, 1000, 1.0, P, 2, P, P, P, P, P + 256, 1000, None]
+    for at, value in ((0, None), (1, 999), (2, -1), (5, -1.0), (6, None), (7, 1025), (8, None), (9, None), (10, None), (12, None), (13, 999)):
+        args = list(ok)
+        args[at] = value
+        assert g(*args) == Q.QADC_EINVAL, (at, value)
+    assert g(P, 1000, 0, 4, 1000, 1.0, P, 2, P, P, P, P, P, 1001, None) == Q.QADC_EINVAL  # in place, other row distances
+
+
+def test_neighbour_mix():
+    L = Q.lib()
+    P = PTR
+    f = L.qadc_neighbour_mix
+    assert f(None, None, 4, None, 0, 10, None, 5, 1.0, None, 3, None, 0.5, None, None, None) == Q.QADC_OK
+    assert f(None, None, 4, None, 2, 10, None, 5, 1.0, None, 0, None, 0.5, None, None, None) == Q.QADC_OK
+    ok = [P, P, 4, None, 2, 10, P, 5, 1.0, P, 3, P, 0.5, P, P, None]
+    for at, value in ((0, None), (1, None), (2, 2), (4, -1), (5, 0), (5, 1025), (6, None), (7, -1), (8, -0.5), (8, float("nan")), (9, None),
+                      (10, -1), (11, None), (12, 1.1), (12, float("nan")), (13, None)):
+        args = list(ok)
+        args[at] = value
+        assert f(*args) == Q.QADC_EINVAL, (at, value)
+    assert b"qadc_neighbour_mix" in L.qadc_last_error()
