@@ -47,15 +47,35 @@ __device__ __forceinline__ void store_pack(T *row, int64_t c, int64_t d, const f
     }
 }
 
-// Sum over the wavefront, in every lane.
+// Float joined over the wavefront without a trip through LDS, in every lane: lanes of 16, then rows, then the last lane's value.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or(float old, float v)
+{
+    return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)__float_as_uint(old), (int)__float_as_uint(v), CTRL, ROWS,
+                                                                 0xf, false));
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) v += __shfl_xor(v, s);
-    return v;
+    v += dpp_or<0x111, 0xf>(0.0f, v);
+    v += dpp_or<0x112, 0xf>(0.0f, v);
+    v += dpp_or<0x114, 0xf>(0.0f, v);
+    v += dpp_or<0x118, 0xf>(0.0f, v);
+    v += dpp_or<0x142, 0xa>(0.0f, v);
+    v += dpp_or<0x143, 0xc>(0.0f, v);
+    return __uint_as_float(lane_value(__float_as_uint(v), 63));
+}
+__device__ __forceinline__ float wave_max(float v)
+{
+    v = fmaxf(v, dpp_or<0x111, 0xf>(v, v));
+    v = fmaxf(v, dpp_or<0x112, 0xf>(v, v));
+    v = fmaxf(v, dpp_or<0x114, 0xf>(v, v));
+    v = fmaxf(v, dpp_or<0x118, 0xf>(v, v));
+    v = fmaxf(v, dpp_or<0x142, 0xa>(v, v));
+    v = fmaxf(v, dpp_or<0x143, 0xc>(v, v));
+    return __uint_as_float(lane_value(__float_as_uint(v), 63));
 }
 
-// Runs F<T>::run(args...) for the element type `type`, T = float, _Float16 or __bf16.
+// Runs `call` with T = float, _Float16 or __bf16 by the element type.
 #define QADC_BY_TYPE(type, call)                             \
     switch (type) {                                          \
     case QADC_TYPE_F32: { using T = float; call; } break;    \

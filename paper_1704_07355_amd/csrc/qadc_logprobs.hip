@@ -1,9 +1,16 @@
 // Log probabilities of given tokens with the entropy and the likeliest alternatives, and their gradient, on gfx950.
 //
-// With x = scale logits, m = max x and e = exp(x - m): lse = m + log sum e, entropy = log sum e - sum e (x - m) / sum e.  The
-// alternatives are the k largest under one 64-bit key: the logit's bits made monotone above, the complement of the token below.
+// With x = scale logits, m = max x and e = exp(x - m): lse = m + log sum e, entropy = log sum e - sum e (x - m) / sum e.  A
+// thread keeps (m, s, w) = (largest logit, sum e, sum e (x - m) / log 2) of what it has read and rescales s and w where m grows,
+// so that a row is read once; threads and workgroups are joined the same way.
+//
+// The alternatives are the k largest under one 64-bit key: the logit's bits made monotone above, the complement of the token
+// below.  While the row streams by, only the largest logit of every block (32 logits of one thread) is kept.  The k-th largest of
+// the threads' largest logits bounds the k-th logit from below, since k different logits reach it; the few blocks that reach it
+// are read again, from the cache, and what reaches it is ordered.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "qadc_lm.h"
 #include "qadc_profile.h"
@@ -13,102 +20,394 @@ namespace qadc {
 namespace {
 
 constexpr int LP_WG = 256;
+constexpr int LP_BLOCK = 32;                  // logits of a thread whose largest is kept
+constexpr int LP_CHUNK = LP_WG * LP_BLOCK;    // logits of a workgroup at a time
+constexpr int LP_LDS_BLOCKS = 24 * LP_WG;     // blocks of a row whose largest logits fit in LDS beside the list: 196608 logits
+constexpr int LP_LIST = 4096;                 // candidates for the alternatives
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// (logit descending, token ascending) as one number, larger first; 0 is below every key.
-__device__ __forceinline__ uint64_t alt_key(float logit, uint32_t token)
+// A logit's bits in the order of the alternatives: -0 and +0 are equal, a NaN comes first.  0 is below every logit.
+__device__ __forceinline__ uint32_t logit_bits(float logit)
 {
-    uint32_t u = __float_as_uint(logit + 0.0f);  // (-0 and +0 are equal)
-    if (logit != logit) u = 0x7fffffffu;
-    u = (int32_t)u < 0 ? ~u : u | 0x80000000u;
-    return (uint64_t)u << 32 | (uint32_t)~token;
+    uint32_t u = __float_as_uint(logit + 0.0f);
+    if (logit != logit) u = 0x7ffffffeu;  // (something is always above)
+    return (int32_t)u < 0 ? ~u : u | 0x80000000u;
 }
+// (logit descending, token ascending) as one number, larger first.
+__device__ __forceinline__ uint64_t alt_key(uint32_t bits, uint32_t token) { return (uint64_t)bits << 32 | (uint32_t)~token; }
 __device__ __forceinline__ float alt_logit(uint64_t key)
 {
     const uint32_t u = (uint32_t)(key >> 32);
     return __uint_as_float((int32_t)u < 0 ? u & 0x7fffffffu : ~u);
 }
 
-template <typename V, typename F>
-__device__ __forceinline__ V group_join(V v, V *lds, F f)
+// Statistics of a part of a row: e = 2^(c (logit - m)), c = scale / log 2, t = c (logit - m).
+struct Stats {
+    float m, s, w;  // largest logit, sum of e, sum of e t
+};
+
+// What a part whose largest logit is m has to be shifted by to be relative to `to` (>= m).
+__device__ __forceinline__ float shift_of(float m, float to, float c)
 {
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) v = f(v, (V)__shfl_xor(v, s));
-    __syncthreads();
-    if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < LP_WG / WAVE; ++w) v = f(v, lds[w]);
-    return v;
+    return m == to ? 0.0f : m == -INFINITY ? -INFINITY : c * (m - to);
+}
+__device__ __forceinline__ void rescale(Stats &a, float to, float c)
+{
+    const float t = shift_of(a.m, to, c), f = exp2_fast(t);
+    a.w = f * fmaf(fmaxf(t, -2000.0f), a.s, a.w);  // (an empty part has s = w = 0: no infinity times zero)
+    a.s *= f;
+    a.m = to;
+}
+__device__ __forceinline__ Stats join(Stats a, Stats b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    rescale(a, m, c);
+    rescale(b, m, c);
+    return {m, a.s + b.s, a.w + b.w};
 }
 
-// A workgroup per row.
-template <typename T>
-__global__ __launch_bounds__(LP_WG) void logprobs_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V, float scale,
-                                                         const int32_t *__restrict__ tokens, int nt, int k,
-                                                         float *__restrict__ logp, float *__restrict__ lse_out,
-                                                         float *__restrict__ entropy_out, uint32_t *__restrict__ top_idx,
-                                                         float *__restrict__ top_logp)
+// Adds the LP_BLOCK logits of a thread; *top becomes the largest.  True: there was a NaN, which fmaxf passes over, or +inf.
+__device__ __forceinline__ bool add_block(Stats &st, const float (&x)[LP_BLOCK], float c, float *top)
 {
-    __shared__ float lds[LP_WG / WAVE];
-    __shared__ uint64_t keys[LP_WG / WAVE];
-    const auto add = [](float a, float b) { return a + b; };
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T *row = logits + r * ld;
-        float m = -INFINITY;
-        for (int v = threadIdx.x; v < V; v += LP_WG) m = fmaxf(m, scale * (float)row[v]);
-        m = group_join(m, lds, [](float a, float b) { return fmaxf(a, b); });
-        const float m0 = m == -INFINITY ? 0.0f : m;
-        float s = 0.0f, w = 0.0f;
-        for (int v = threadIdx.x; v < V; v += LP_WG) {
-            const float t = scale * (float)row[v] - m0;
-            const float e = expf(t);
-            s += e;
-            if (e > 0.0f) w = fmaf(e, t, w);
+    float v = x[0];
+#pragma unroll
+    for (int e = 1; e < LP_BLOCK; ++e) v = fmaxf(v, x[e]);
+    const float m = fmaxf(st.m, v), m0 = m == -INFINITY ? 0.0f : m;
+    float s[2] = {0.0f, 0.0f}, w[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < LP_BLOCK; ++i) {
+        const float t = c * (x[i] - m0), e = exp2_fast(t);
+        s[i & 1] += e;
+        w[i & 1] = fmaf(e, fmaxf(t, -2000.0f), w[i & 1]);  // (a masked logit: zero times something finite)
+    }
+    const float sum = s[0] + s[1];
+    rescale(st, m, c);
+    st.s += sum;
+    st.w += w[0] + w[1];
+    *top = v;
+    return sum != sum;
+}
+
+// The logits of block (chunk, thread): LP_BLOCK / N packs, those of a wavefront side by side.
+template <typename T>
+__device__ __forceinline__ int64_t pack_at(int64_t chunk, int u)
+{
+    return chunk * LP_CHUNK + ((int64_t)u * LP_WG + threadIdx.x) * Pack<T>::N;
+}
+template <typename T>
+__device__ __forceinline__ void load_block(const T *row, int64_t chunk, int V, float (&x)[LP_BLOCK])
+{
+    constexpr int N = Pack<T>::N;
+    if ((chunk + 1) * LP_CHUNK <= V) {  // (the same in all threads: the loads follow each other without a wait)
+#pragma unroll
+        for (int u = 0; u < LP_BLOCK / N; ++u) {
+            const typename Pack<T>::V p = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(chunk, u));
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[u * N + e] = (float)p[e];
         }
-        s = group_join(s, lds, add);
-        w = group_join(w, lds, add);
-        const float lse = m0 + logf(s);
-        if (threadIdx.x == 0) {
-            if (lse_out) lse_out[r] = lse;
-            if (entropy_out) entropy_out[r] = s == 0.0f ? 0.0f : logf(s) - w / s;
-        }
-        const auto log_prob = [&](float logit) { return s == 0.0f ? -INFINITY : scale * logit - lse; };
-        for (int t = threadIdx.x; t < nt; t += LP_WG) {
-            const int tok = tokens[r * nt + t];
-            logp[r * nt + t] = tok >= 0 && tok < V ? log_prob((float)row[tok]) : 0.0f;
-        }
-        uint64_t last = ~0ull;
-        for (int i = 0; i < k; ++i) {
-            uint64_t best = 0;
-            for (int v = threadIdx.x; v < V; v += LP_WG) {
-                const uint64_t key = alt_key((float)row[v], (uint32_t)v);
-                if (key < last && key > best) best = key;
-            }
-            best = group_join(best, keys, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-            if (threadIdx.x == 0) {
-                top_idx[r * k + i] = best ? ~(uint32_t)best : 0xFFFFFFFFu;
-                top_logp[r * k + i] = best ? log_prob(alt_logit(best)) : -INFINITY;
-            }
-            last = best;
-        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < LP_BLOCK / N; ++u) {
+        float v[N];
+        load_pack(row, pack_at<T>(chunk, u), V, -INFINITY, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[u * N + e] = v[e];
     }
 }
 
-// A workgroup per row: first every logit's own share, then the given tokens', each once.
+// A block's largest logit in the order of the alternatives (0: it has none), where `v` is the largest that is no NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t block_top(const T *row, int64_t chunk, int V, float v, bool odd)
+{
+    uint32_t bits = pack_at<T>(chunk, 0) < V ? logit_bits(v) : 0u;
+    if (odd)
+#pragma unroll 1
+        for (int u = 0; u < LP_BLOCK / Pack<T>::N; ++u)
+#pragma unroll 1
+            for (int64_t at = pack_at<T>(chunk, u), e = 0; e < Pack<T>::N && at + e < V; ++e)
+                bits = max(bits, logit_bits((float)row[at + e]));
+    return bits;
+}
+
+struct StatsLds {
+    float m[LP_WG / WAVE], s[LP_WG / WAVE], w[LP_WG / WAVE];
+};
+struct AltLds {
+    uint64_t list[LP_LIST];
+    uint64_t kept[QADC_MAX_ALTERNATIVES];
+    uint32_t tops[LP_WG];
+    uint32_t counts[2][LP_WG / WAVE];
+    uint32_t count, bound;
+};
+struct NoLds {};
+
+// The threads' statistics joined, in every thread.
+__device__ __forceinline__ Stats group_stats(Stats a, float c, StatsLds &lds)
+{
+    const float m = wave_max(a.m);
+    rescale(a, m, c);
+    a.s = wave_sum(a.s);
+    a.w = wave_sum(a.w);
+    __syncthreads();
+    if (lane_id() == 0) {
+        lds.m[threadIdx.x >> 6] = a.m;
+        lds.s[threadIdx.x >> 6] = a.s;
+        lds.w[threadIdx.x >> 6] = a.w;
+    }
+    __syncthreads();
+    a = {lds.m[0], lds.s[0], lds.w[0]};
+#pragma unroll
+    for (int v = 1; v < LP_WG / WAVE; ++v) a = join(a, Stats{lds.m[v], lds.s[v], lds.w[v]}, c);
+    return a;
+}
+
+struct Out {
+    const int32_t *tokens;
+    int nt, k;
+    float *logp, *lse, *entropy;
+    uint32_t *top_idx;
+    float *top_logp;
+};
+
+// The sum of a count that is equal within a wavefront, in every thread; `turn` alternates between calls.
+__device__ __forceinline__ uint32_t group_count(uint32_t c, AltLds &lds, int turn)
+{
+    if (lane_id() == 0) lds.counts[turn & 1][threadIdx.x >> 6] = c;
+    __syncthreads();
+    uint32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < LP_WG / WAVE; ++w) total += lds.counts[turn & 1][w];
+    return total;
+}
+
+// The k alternatives of a row; top_of(chunk) is the largest logit of this thread's block.
+template <typename T, typename F>
+__device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, float scale, float lse, bool none,
+                                   uint32_t *top_idx, float *top_logp, AltLds &lds, F top_of)
+{
+    constexpr int N = Pack<T>::N;
+    uint32_t top = 0;
+    for (int64_t j = 0; j < chunks; ++j) top = max(top, top_of(j));
+    if (threadIdx.x == 0) {
+        lds.count = 0;
+        lds.bound = 0;
+    }
+    lds.tops[threadIdx.x] = top;
+    __syncthreads();
+    int above = 0, equal = 0;  // a thread whose largest logit is the k-th of the threads' knows it
+    for (int i = 0; i < LP_WG; ++i) {
+        above += lds.tops[i] > top;
+        equal += lds.tops[i] == top;
+    }
+    if (above < k && above + equal >= k) lds.bound = top;
+    __syncthreads();
+    uint32_t bound = lds.bound;  // 0 where fewer than k threads have a logit: all of the row are candidates
+    // f(bits, token) for this thread's logits that reach `from`
+    const auto each = [&](uint32_t from, auto f) {
+        if (top < from) return;
+        for (int64_t j = 0; j < chunks; ++j) {
+            if (top_of(j) < from) continue;
+            for (int u = 0; u < LP_BLOCK / N; ++u) {
+                const int64_t at = pack_at<T>(j, u);
+                for (int e = 0; e < N && at + e < V; ++e) {
+                    const uint32_t bits = logit_bits((float)row[at + e]);
+                    if (bits >= from) f(bits, (uint32_t)(at + e));
+                }
+            }
+        }
+    };
+    const auto collect = [&](uint32_t bits, uint32_t token) {
+        const uint32_t slot = atomicAdd(&lds.count, 1u);
+        if (slot < LP_LIST) lds.list[slot] = alt_key(bits, token);
+    };
+    each(max(bound, 1u), collect);
+    __syncthreads();
+    uint32_t n = lds.count;
+    int turn = 0;
+    if (n > LP_LIST) {
+        // Too many: the k-th logit itself, bit by bit where it is not the bound.  Those above it are fewer than k; of those
+        // equal to it the first in the row fill the list up.
+        const auto reach = [&](uint32_t from) {
+            uint32_t c = 0;
+            each(from, [&](uint32_t, uint32_t) { ++c; });
+            c = lane_value(wave_running_sum(c), 63);
+            return group_count(c, lds, turn++);
+        };
+        if (reach(bound + 1) >= (uint32_t)k) {
+            uint32_t kth = 0;
+            for (int b = 31; b >= 0; --b) {
+                const uint32_t trial = kth | 1u << b;
+                if (trial <= bound || reach(trial) >= (uint32_t)k) kth = trial;
+            }
+            bound = kth;
+        }
+        if (threadIdx.x == 0) lds.count = 0;
+        __syncthreads();
+        each(bound + 1, collect);
+        __syncthreads();
+        n = lds.count;
+        for (int64_t v0 = 0; v0 < V && n < (uint32_t)k; v0 += LP_WG) {
+            const int64_t v = v0 + threadIdx.x;
+            const bool is = v < V && logit_bits((float)row[v]) == bound;
+            const unsigned long long mask = __ballot(is);
+            const uint32_t total = group_count((uint32_t)__popcll(mask), lds, turn);
+            uint32_t slot = n + rank_in_mask(mask);
+            for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) slot += lds.counts[turn & 1][w];
+            if (is && slot < (uint32_t)k) lds.list[slot] = alt_key(bound, (uint32_t)v);
+            n = min(n + total, (uint32_t)k);
+            ++turn;
+        }
+        __syncthreads();
+    }
+    const uint64_t *list = lds.list;
+    if (n > LP_WG) {
+        // Too many to compare each with each: the k-th key, bit by bit (no two are equal, so k of them reach it).
+        uint64_t from = 0;
+        for (int b = 63; b >= 0; --b) {
+            const uint64_t trial = from | 1ull << b;
+            uint32_t c = 0;
+            for (uint32_t i = 0; i < n; i += LP_WG)
+                c += (uint32_t)__popcll(__ballot(i + threadIdx.x < n && lds.list[min(i + threadIdx.x, n - 1)] >= trial));
+            if (group_count(c, lds, turn++) >= (uint32_t)k) from = trial;
+        }
+        if (threadIdx.x == 0) lds.count = 0;
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < n; i += LP_WG)
+            if (lds.list[i] >= from) lds.kept[atomicAdd(&lds.count, 1u)] = lds.list[i];
+        __syncthreads();
+        n = (uint32_t)k;
+        list = lds.kept;
+    }
+    if (threadIdx.x < n) {
+        const uint64_t key = list[threadIdx.x];
+        int rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += list[j] > key;
+        if (rank < k) {
+            top_idx[rank] = ~(uint32_t)key;
+            top_logp[rank] = none ? -INFINITY : scale * alt_logit(key) - lse;
+        }
+    }
+    for (int i = (int)n + threadIdx.x; i < k; i += LP_WG) {  // V < k
+        top_idx[i] = 0xFFFFFFFFu;
+        top_logp[i] = -INFINITY;
+    }
+    __syncthreads();
+}
+
+// What follows once a row's statistics are known.
+template <typename T, bool ALT, typename L, typename F>
+__device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_t chunks, Stats a, float scale, const Out &o,
+                                          L &lds, F top_of)
+{
+    const bool none = a.m == -INFINITY && a.s == 0.0f;
+    const float log_s = logf(a.s), lse = none ? -INFINITY : fmaf(scale, a.m, log_s);
+    if (threadIdx.x == 0) {
+        if (o.lse) o.lse[r] = lse;
+        if (o.entropy) o.entropy[r] = none ? 0.0f : log_s - LN2 * a.w / a.s;
+    }
+    for (int t = threadIdx.x; t < o.nt; t += LP_WG) {
+        const int tok = o.tokens[r * o.nt + t];
+        float v = 0.0f;
+        if (tok >= 0 && tok < V) v = none ? -INFINITY : scale * (float)row[tok] - lse;
+        o.logp[r * o.nt + t] = v;
+    }
+    if constexpr (ALT) write_alternatives(row, V, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds, top_of);
+}
+
+// A workgroup per row.
+template <typename T, bool ALT>
+__global__ __launch_bounds__(LP_WG) void logprobs_row_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
+                                                             float scale, Out o)
+{
+    __shared__ StatsLds stats;
+    __shared__ std::conditional_t<ALT, AltLds, NoLds> alt;
+    extern __shared__ uint32_t tops[];  // [chunks][LP_WG] where there are alternatives
+    const float c = scale * LOG2E;
+    const int64_t chunks = (V + LP_CHUNK - 1) / LP_CHUNK;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const T *row = logits + r * ld;
+        Stats a = {-INFINITY, 0.0f, 0.0f};
+        for (int64_t j = 0; j < chunks; ++j) {
+            float x[LP_BLOCK], top;
+            load_block(row, j, V, x);
+            const bool odd = add_block(a, x, c, &top);
+            if constexpr (ALT) tops[j * LP_WG + threadIdx.x] = block_top(row, j, V, top, odd);
+        }
+        a = group_stats(a, c, stats);
+        write_row<T, ALT>(row, r, V, chunks, a, scale, o, alt, [&](int64_t j) { return tops[j * LP_WG + threadIdx.x]; });
+    }
+}
+
+// A workgroup per `per` chunks of a row: their statistics and their blocks' largest logits into the workspace.
+template <typename T, bool ALT>
+__global__ __launch_bounds__(LP_WG) void logprobs_part_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
+                                                              float scale, int64_t chunks, int parts, int per,
+                                                              Stats *__restrict__ stats, uint32_t *__restrict__ tops)
+{
+    __shared__ StatsLds lds;
+    const float c = scale * LOG2E;
+    for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
+        const int64_t r = i / parts, j0 = i % parts * per;
+        const T *row = logits + r * ld;
+        Stats a = {-INFINITY, 0.0f, 0.0f};
+        for (int64_t j = j0; j < min(j0 + per, chunks); ++j) {
+            float x[LP_BLOCK], top;
+            load_block(row, j, V, x);
+            const bool odd = add_block(a, x, c, &top);
+            if constexpr (ALT) tops[(r * chunks + j) * LP_WG + threadIdx.x] = block_top(row, j, V, top, odd);
+        }
+        a = group_stats(a, c, lds);
+        if (threadIdx.x == 0) stats[i] = a;
+    }
+}
+
+template <typename T, bool ALT>
+__global__ __launch_bounds__(LP_WG) void logprobs_join_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
+                                                              float scale, int64_t chunks, int parts,
+                                                              const Stats *__restrict__ stats,
+                                                              const uint32_t *__restrict__ tops, Out o)
+{
+    __shared__ StatsLds lds;
+    __shared__ std::conditional_t<ALT, AltLds, NoLds> alt;
+    const float c = scale * LOG2E;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        Stats a = {-INFINITY, 0.0f, 0.0f};
+        for (int p = threadIdx.x; p < parts; p += LP_WG) a = join(a, stats[r * parts + p], c);
+        a = group_stats(a, c, lds);
+        write_row<T, ALT>(logits + r * ld, r, V, chunks, a, scale, o, alt,
+                          [&](int64_t j) { return tops[(r * chunks + j) * LP_WG + threadIdx.x]; });
+    }
+}
+
+// exp(t), t <= 0 or thereabouts.  A float32 gradient shows the rounding of t log2(e), |t| units in its last place of a p that
+// has its own size (16-bit ones do not): there what the product leaves out is put back in.
+template <typename T>
+__device__ __forceinline__ float exp_of(float t)
+{
+    const float y = t * LOG2E;
+    if constexpr (sizeof(T) == 2) return exp2_fast(y);
+    const float rest = fmaf(t, LOG2E, -y) + t * 1.9259629911e-8f;  // log2(e) - LOG2E = 1.92596e-8
+    const float p = exp2_fast(y);
+    return y > -3000.0f ? fmaf(p, rest * LN2, p) : p;  // (an infinite t: no infinity less infinity)
+}
+
+// A workgroup per `per` chunks of a row: first every logit's own share, then the given tokens', each once.
 template <typename T>
 __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, int64_t ld, int64_t rows, int V, float scale,
-                                                              const int32_t *__restrict__ tokens, int nt,
+                                                              int parts, int per, const int32_t *__restrict__ tokens, int nt,
                                                               const float *__restrict__ lse, const float *__restrict__ entropy,
                                                               const float *__restrict__ dlogp,
                                                               const float *__restrict__ dentropy, T *dlogits, int64_t ldd)
 {
-    __shared__ float lds[LP_WG / WAVE];
+    constexpr int N = Pack<T>::N;
+    __shared__ float sums[LP_WG / WAVE];
     __shared__ int tok[QADC_MAX_R];
     __shared__ float at[QADC_MAX_R], dl[QADC_MAX_R];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+    for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
+        const int64_t r = i / parts, v0 = i % parts * per * LP_CHUNK, v1 = min(v0 + (int64_t)per * LP_CHUNK, (int64_t)V);
         const T *row = logits + r * ld;
         T *out = dlogits + r * ldd;
         const float l = lse[r], dh = dentropy ? dentropy[r] : 0.0f, h = dentropy ? entropy[r] : 0.0f;
@@ -116,18 +415,46 @@ __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, i
         float total = 0.0f;
         for (int t = threadIdx.x; t < nt; t += LP_WG) {
             const int v = tokens[r * nt + t];
-            const bool used = v >= 0 && v < V;
-            tok[t] = used ? v : -1;
-            at[t] = used ? (float)row[v] : 0.0f;
-            dl[t] = used ? dlogp[r * nt + t] : 0.0f;
-            total += dl[t];
+            const bool used = v >= 0 && v < V, here = v >= v0 && v < v1;
+            const float g = used ? dlogp[r * nt + t] : 0.0f;
+            tok[t] = here ? v : -1;
+            at[t] = here ? (float)row[v] : 0.0f;
+            dl[t] = g;
+            total += g;
         }
-        total = group_join(total, lds, [](float a, float b) { return a + b; });
+        total = wave_sum(total);
+        if (lane_id() == 0) sums[threadIdx.x >> 6] = total;
+        __syncthreads();
+        total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LP_WG / WAVE; ++w) total += sums[w];
         const auto share = [&](float logit) {
-            const float lp = scale * logit - l, p = expf(lp);
-            return p > 0.0f || p != p ? -p * fmaf(dh, lp + h, total) : 0.0f;
+            const float lp = fmaf(scale, logit, -l), p = exp_of<T>(lp);
+            return p * -fmaf(dh, fmaxf(lp, -2000.0f) + h, total);  // (a masked logit: zero times something finite)
         };
-        for (int v = threadIdx.x; v < V; v += LP_WG) out[v] = (T)(none ? 0.0f : scale * share((float)row[v]));
+        const auto value = [&](float logit) { return none ? 0.0f : scale * share(logit); };
+        for (int64_t c0 = v0; c0 < v1; c0 += LP_CHUNK) {
+            if (c0 + LP_CHUNK <= v1) {
+                typename Pack<T>::V p[LP_BLOCK / N];
+#pragma unroll
+                for (int u = 0; u < LP_BLOCK / N; ++u)
+                    p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + c0 + ((int64_t)u * LP_WG + threadIdx.x) * N);
+#pragma unroll
+                for (int u = 0; u < LP_BLOCK / N; ++u) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) p[u][e] = (T)value((float)p[u][e]);
+                    *reinterpret_cast<typename Pack<T>::V *>(out + c0 + ((int64_t)u * LP_WG + threadIdx.x) * N) = p[u];
+                }
+            } else {
+                for (int64_t c = c0 + threadIdx.x * N; c < v1; c += LP_WG * N) {
+                    float x[N];
+                    load_pack(row, c, v1, 0.0f, x);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) x[e] = value(x[e]);
+                    store_pack(out, c, v1, x);
+                }
+            }
+        }
         __syncthreads();
         for (int t = threadIdx.x; t < nt; t += LP_WG) {
             if (tok[t] < 0 || none) continue;
@@ -156,10 +483,52 @@ int check_logits(const char *who, int type, int64_t ld, int64_t rows, int V, flo
 
 }  // namespace
 
+// How a call is cut: a row per workgroup where the rows alone fill the chip, parts of rows otherwise.
+struct Plan {
+    int64_t chunks;
+    int parts, per;  // workgroups a row, chunks each; parts = 1: one kernel and no workspace
+    size_t tops, bytes;
+};
+
+static Plan plan_logprobs(int64_t rows, int V, int k)
+{
+    Plan p;
+    p.chunks = ceil_div(V, LP_CHUNK);
+    const int64_t want = std::max<int64_t>(1, ceil_div(1024, rows));
+    p.per = (int)ceil_div(p.chunks, std::min(p.chunks, want));
+    p.parts = (int)ceil_div(p.chunks, p.per);
+    if (p.parts == 1 && k > 0 && p.chunks * LP_WG > LP_LDS_BLOCKS) {  // the blocks do not fit in LDS
+        p.per = (int)ceil_div(p.chunks, 2);
+        p.parts = 2;
+    }
+    p.tops = p.parts == 1 ? 0 : align_up((size_t)rows * p.parts * sizeof(Stats), 256);
+    p.bytes = p.parts == 1 ? 256 : p.tops + (k > 0 ? (size_t)rows * p.chunks * LP_WG * sizeof(uint32_t) : 0);
+    return p;
+}
+
 size_t token_logprobs_workspace(int64_t rows, int V, int k)
 {
     if (rows < 1 || V < 1 || k < 0 || k > QADC_MAX_ALTERNATIVES) return 0;
-    return 256;
+    return plan_logprobs(rows, V, k).bytes;
+}
+
+template <typename T, bool ALT>
+static void launch_logprobs(const Plan &p, const void *logits, int64_t ld, int64_t rows, int V, float scale, const Out &o,
+                            void *workspace, hipStream_t st)
+{
+    const T *x = (const T *)logits;
+    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
+    if (p.parts == 1) {
+        launch(QADC_PROF_LOGPROBS, logprobs_row_kernel<T, ALT>, grid, dim3(LP_WG),
+               ALT ? (size_t)p.chunks * LP_WG * sizeof(uint32_t) : 0, st, x, ld, rows, V, scale, o);
+        return;
+    }
+    Stats *stats = (Stats *)workspace;
+    uint32_t *tops = (uint32_t *)((char *)workspace + p.tops);
+    launch(QADC_PROF_LOGPROBS, logprobs_part_kernel<T, ALT>, dim3((unsigned)std::min<int64_t>(rows * p.parts, 1 << 20)),
+           dim3(LP_WG), 0, st, x, ld, rows, V, scale, p.chunks, p.parts, p.per, stats, tops);
+    launch(QADC_PROF_LOGPROBS, logprobs_join_kernel<T, ALT>, grid, dim3(LP_WG), 0, st, x, ld, rows, V, scale, p.chunks, p.parts,
+           (const Stats *)stats, (const uint32_t *)tops, o);
 }
 
 int token_logprobs(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const int32_t *tokens, int T,
@@ -171,13 +540,15 @@ int token_logprobs(const void *logits, int64_t ld, int type, int64_t rows, int V
     if (rows == 0) return QADC_OK;
     if (!logits || (T > 0 && !logp) || (k > 0 && (!top_idx || !top_logp)))
         return fail(QADC_EINVAL, "qadc_token_logprobs: null pointer");
-    const size_t need = token_logprobs_workspace(rows, V, k);
-    if (!workspace || workspace_bytes < need)
-        return fail(QADC_ENOMEM, "qadc_token_logprobs: workspace of %zu bytes, %zu needed", workspace_bytes, need);
-    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
-    const int nt = T;
-    QADC_BY_TYPE(type, (launch(QADC_PROF_LOGPROBS, logprobs_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows, V,
-                               scale, tokens, nt, k, logp, lse, entropy, top_idx, top_logp)));
+    const Plan p = plan_logprobs(rows, V, k);
+    if (!workspace || workspace_bytes < p.bytes)
+        return fail(QADC_ENOMEM, "qadc_token_logprobs: workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+    const Out o = {tokens, T, k, logp, lse, entropy, top_idx, top_logp};
+    if (k > 0) {
+        QADC_BY_TYPE(type, (launch_logprobs<T, true>(p, logits, ld, rows, V, scale, o, workspace, st)));
+    } else {
+        QADC_BY_TYPE(type, (launch_logprobs<T, false>(p, logits, ld, rows, V, scale, o, workspace, st)));
+    }
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }
@@ -193,10 +564,13 @@ int token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t ro
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: null pointer");
     if (logits == dlogits && ld != ldd)
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: in place needs equal row distances");
-    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
+    const int64_t chunks = ceil_div(V, LP_CHUNK);
+    const int per = (int)std::min<int64_t>(chunks, std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048)));
+    const int parts = (int)ceil_div(chunks, per);
+    const dim3 grid((unsigned)std::min<int64_t>(rows * parts, 1 << 20));
     const int nt = T;
     QADC_BY_TYPE(type, (launch(QADC_PROF_LOGPROBS, logprobs_grad_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows,
-                               V, scale, tokens, nt, lse, entropy, dlogp, dentropy, (T *)dlogits, ldd)));
+                               V, scale, parts, per, tokens, nt, lse, entropy, dlogp, dentropy, (T *)dlogits, ldd)));
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }
