@@ -64,6 +64,18 @@ __device__ __forceinline__ float wave_sum(float v)
     v += dpp_or<0x143, 0xc>(0.0f, v);
     return __uint_as_float(lane_value(__float_as_uint(v), 63));
 }
+// Sum over groups of 16, 32 or 64 lanes, in every lane: a row of 16 turned by 8, 4, 2 and 1, then the rows.
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    if constexpr (G == WAVE) return wave_sum(v);
+    v += dpp_or<0x128, 0xf>(0.0f, v);
+    v += dpp_or<0x124, 0xf>(0.0f, v);
+    v += dpp_or<0x122, 0xf>(0.0f, v);
+    v += dpp_or<0x121, 0xf>(0.0f, v);
+    if constexpr (G == 32) v += __shfl_xor(v, 16);
+    return v;
+}
 __device__ __forceinline__ float wave_max(float v)
 {
     v = fmaxf(v, dpp_or<0x111, 0xf>(v, v));

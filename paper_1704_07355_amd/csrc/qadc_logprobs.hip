@@ -23,7 +23,8 @@ constexpr int LP_WG = 256;
 constexpr int LP_BLOCK = 32;                  // logits of a thread whose largest is kept
 constexpr int LP_CHUNK = LP_WG * LP_BLOCK;    // logits of a workgroup at a time
 constexpr int LP_LDS_BLOCKS = 24 * LP_WG;     // blocks of a row whose largest logits fit in LDS beside the list: 196608 logits
-constexpr int LP_LIST = 4096;                 // candidates for the alternatives
+constexpr int LP_LIST = 3072;                 // candidates for the alternatives
+constexpr int LP_READ = 1024;                 // blocks that are read again by all threads together
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -139,8 +140,9 @@ struct AltLds {
     uint64_t list[LP_LIST];
     uint64_t kept[QADC_MAX_ALTERNATIVES];
     uint32_t tops[LP_WG];
+    uint32_t blocks[LP_READ];
     uint32_t counts[2][LP_WG / WAVE];
-    uint32_t count, bound;
+    uint32_t count, block_count, bound;
 };
 struct NoLds {};
 
@@ -183,24 +185,40 @@ __device__ __forceinline__ uint32_t group_count(uint32_t c, AltLds &lds, int tur
     return total;
 }
 
+// f(chunk, its block's largest logit) for every block of this thread, eight in flight.
+template <typename F, typename G>
+__device__ __forceinline__ void each_top(int64_t chunks, F top_of, G f)
+{
+    for (int64_t j = 0; j < chunks; j += 8) {
+        uint32_t t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = j + i < chunks ? top_of(j + i) : 0u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(j + i, t[i]);
+    }
+}
+
 // The k alternatives of a row; top_of(chunk) is the largest logit of this thread's block.
 template <typename T, typename F>
 __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, float scale, float lse, bool none,
                                    uint32_t *top_idx, float *top_logp, AltLds &lds, F top_of)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
     uint32_t top = 0;
-    for (int64_t j = 0; j < chunks; ++j) top = max(top, top_of(j));
+    each_top(chunks, top_of, [&](int64_t, uint32_t t) { top = max(top, t); });
     if (threadIdx.x == 0) {
         lds.count = 0;
+        lds.block_count = 0;
         lds.bound = 0;
     }
     lds.tops[threadIdx.x] = top;
     __syncthreads();
     int above = 0, equal = 0;  // a thread whose largest logit is the k-th of the threads' knows it
-    for (int i = 0; i < LP_WG; ++i) {
-        above += lds.tops[i] > top;
-        equal += lds.tops[i] == top;
+#pragma unroll 4
+    for (int i = 0; i < LP_WG; i += 4) {
+        const uint4 t = *reinterpret_cast<const uint4 *>(&lds.tops[i]);
+        above += (t.x > top) + (t.y > top) + (t.z > top) + (t.w > top);
+        equal += (t.x == top) + (t.y == top) + (t.z == top) + (t.w == top);
     }
     if (above < k && above + equal >= k) lds.bound = top;
     __syncthreads();
@@ -210,7 +228,7 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
         if (top < from) return;
         for (int64_t j = 0; j < chunks; ++j) {
             if (top_of(j) < from) continue;
-            for (int u = 0; u < LP_BLOCK / N; ++u) {
+            for (int u = 0; u < PACKS; ++u) {
                 const int64_t at = pack_at<T>(j, u);
                 for (int e = 0; e < N && at + e < V; ++e) {
                     const uint32_t bits = logit_bits((float)row[at + e]);
@@ -223,7 +241,31 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
         const uint32_t slot = atomicAdd(&lds.count, 1u);
         if (slot < LP_LIST) lds.list[slot] = alt_key(bits, token);
     };
-    each(max(bound, 1u), collect);
+    // The blocks that reach the bound are listed, then read by all threads, a pack each.
+    const uint32_t least = max(bound, 1u);
+    if (top >= least)
+        each_top(chunks, top_of, [&](int64_t j, uint32_t t) {
+            if (t < least) return;
+            const uint32_t slot = atomicAdd(&lds.block_count, 1u);
+            if (slot < LP_READ) lds.blocks[slot] = (uint32_t)j * LP_WG + threadIdx.x;
+        });
+    __syncthreads();
+    const uint32_t blocks = lds.block_count;
+    if (blocks <= LP_READ) {
+        for (uint32_t i = threadIdx.x; i < blocks * PACKS; i += LP_WG) {
+            const uint32_t block = lds.blocks[i / PACKS];
+            const int64_t at = (int64_t)(block / LP_WG) * LP_CHUNK + ((int64_t)(i % PACKS) * LP_WG + block % LP_WG) * N;
+            float x[N];
+            load_pack(row, at, V, 0.0f, x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint32_t bits = logit_bits(x[e]);
+                if (bits >= least && at + e < V) collect(bits, (uint32_t)(at + e));
+            }
+        }
+    } else {
+        each(least, collect);
+    }
     __syncthreads();
     uint32_t n = lds.count;
     int turn = 0;
@@ -302,7 +344,7 @@ template <typename T, bool ALT, typename L, typename F>
 __device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_t chunks, Stats a, float scale, const Out &o,
                                           L &lds, F top_of)
 {
-    const bool none = a.m == -INFINITY && a.s == 0.0f;
+    const bool none = a.m == -INFINITY && a.s == 0.0f;  // a mask has left nothing
     const float log_s = logf(a.s), lse = none ? -INFINITY : fmaf(scale, a.m, log_s);
     if (threadIdx.x == 0) {
         if (o.lse) o.lse[r] = lse;

@@ -3,6 +3,10 @@
 // Forward: mean = sum x / d, then the squared differences to that mean (two passes over the row: no difference of large sums),
 // y = (x - mean) rstd w + b.  Backward: with h = (x - mean) rstd and g = dy w, dx = rstd (g - sum g / d - h sum(g h) / d); the
 // weight's gradients are sums over the rows, added in a fixed order: each workgroup its stretch of rows, then the stretches.
+//
+// A row of up to 16384 elements stays in the registers of its group of threads, 8 or 16 a thread; the group goes on to further
+// rows with the weights (and the sums of the weight's gradients) in registers, the next row's elements already on their way.
+// Longer rows are read again for every pass.
 
 #include <algorithm>
 
@@ -14,6 +18,267 @@ namespace qadc {
 namespace {
 
 constexpr int NORM_WG = 256;
+
+// Sums over a group of G threads, in every one of them; `turn` alternates between calls (a buffer is written again only
+// behind the barrier of the call in between).
+template <int G, int NS>
+__device__ __forceinline__ void group_sums(float (&v)[NS], float *lds, int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < NS; ++i) v[i] = lanes_sum<G < WAVE ? G : WAVE>(v[i]);
+    if constexpr (G > WAVE) {
+        constexpr int W = G / WAVE;
+        float *buf = lds + (turn & 1) * (1024 / WAVE) * NS;
+        ++turn;
+        const int wave = threadIdx.x >> 6, first = wave / W * W;
+        if (lane_id() == 0)
+#pragma unroll
+            for (int i = 0; i < NS; ++i) buf[wave * NS + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            v[i] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) v[i] += buf[(first + w) * NS + i];
+        }
+    }
+}
+
+// The elements of a row that thread t of a group of G holds: E / N packs, those of the group side by side.
+template <typename T, int G, int E>
+struct Part {
+    static constexpr int N = Pack<T>::N, P = E / N;
+    typedef typename Pack<T>::V V;
+    V raw[P];
+
+    __device__ __forceinline__ void load(const T *row, int t, int d)  // 0 beyond the row
+    {
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int c = (u * G + t) * N;
+            if ((u + 1) * G * N <= d) {  // (the same in all threads)
+                raw[u] = *reinterpret_cast<const V *>(row + c);
+            } else if (c + N <= d) {
+                raw[u] = *reinterpret_cast<const V *>(row + c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) raw[u][e] = c + e < d ? row[c + e] : (T)0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return (float)raw[i / N][i % N]; }
+    __device__ static __forceinline__ int column(int i, int t) { return (i / N * G + t) * N + i % N; }
+    __device__ __forceinline__ void set(int i, float v) { raw[i / N][i % N] = (T)v; }
+    __device__ __forceinline__ void store(T *row, int t, int d) const
+    {
+#pragma unroll
+        for (int u = 0; u < P; ++u) {
+            const int c = (u * G + t) * N;
+            if (c + N <= d) {
+                *reinterpret_cast<V *>(row + c) = raw[u];
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (c + e < d) row[c + e] = raw[u][e];
+            }
+        }
+    }
+};
+
+template <typename T, int G, int E, typename W>
+__device__ __forceinline__ void load_weights(const W *w, float none, int t, int d, float (&v)[E])
+{
+    constexpr int N = Pack<T>::N;
+    typedef W Wide __attribute__((ext_vector_type(N), aligned(sizeof(W))));
+#pragma unroll
+    for (int u = 0; u < E / N; ++u) {
+        const int c = (u * G + t) * N;
+        if (w && c + N <= d) {
+            const Wide p = *reinterpret_cast<const Wide *>(w + c);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[u * N + e] = (float)p[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[u * N + e] = w && c + e < d ? (float)w[c + e] : none;
+        }
+    }
+}
+
+// A group of G threads per row, THREADS / G rows of a workgroup at a time.
+template <typename T, typename W, int G, int E, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_rows_kernel(const T *x, int64_t ldx, const W *__restrict__ weight,
+                                                            const W *__restrict__ bias, int64_t rows, int d, float eps, T *y,
+                                                            float *__restrict__ mean_out, float *__restrict__ rstd_out)
+{
+    __shared__ float lds[2 * (1024 / WAVE)];
+    constexpr int R = THREADS / G;
+    const int t = threadIdx.x % G;
+    int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / G;
+    const int64_t ahead = (int64_t)gridDim.x * R;
+    Part<T, G, E> now, next;
+    now.load(x + min(r, rows - 1) * ldx, t, d);
+    float w[E], b[E];
+    load_weights<T, G, E>(weight, 1.0f, t, d, w);
+    load_weights<T, G, E>(bias, 0.0f, t, d, b);
+    int turn = 0;
+    for (; r - threadIdx.x / G < rows; r += ahead) {  // (all groups of a workgroup go round together)
+        const bool more = r - threadIdx.x / G + ahead < rows;
+        if (more) next.load(x + min(r + ahead, rows - 1) * ldx, t, d);
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < E; ++i) s[0] += now[i];
+        group_sums<G, 1>(s, lds, turn);
+        const float mean = s[0] / (float)d;
+        s[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float h = Part<T, G, E>::column(i, t) < d ? now[i] - mean : 0.0f;
+            s[0] = fmaf(h, h, s[0]);
+        }
+        group_sums<G, 1>(s, lds, turn);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)d + eps);
+        if (r < rows) {
+            Part<T, G, E> out;
+#pragma unroll
+            for (int i = 0; i < E; ++i) out.set(i, fmaf((now[i] - mean) * rstd, w[i], b[i]));
+            out.store(y + r * d, t, d);
+            if (t == 0) {
+                if (mean_out) mean_out[r] = mean;
+                if (rstd_out) rstd_out[r] = rstd;
+            }
+        }
+        if (more) now = next;
+    }
+}
+
+// dx of the workgroup's rows and, where `parts` is set, their share of the weight's gradients: parts [workgroup][2][d].
+template <typename T, typename W, int G, int E, int THREADS, bool AHEAD>
+__global__ __launch_bounds__(THREADS) void norm_back_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx,
+                                                            const W *__restrict__ weight, const float *__restrict__ mean,
+                                                            const float *__restrict__ rstd, int64_t rows, int d, T *dx,
+                                                            float *__restrict__ parts)
+{
+    __shared__ float lds[4 * (1024 / WAVE)];
+    constexpr int R = THREADS / G;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    int64_t r = (int64_t)blockIdx.x * R + group;
+    const int64_t ahead = (int64_t)gridDim.x * R;
+    typedef Part<T, G, E> P;
+    P xs, gs, xn, gn;
+    float mu, rs, mun = 0.0f, rsn = 0.0f;
+    {
+        const int64_t at = min(r, rows - 1);
+        xs.load(x + at * ldx, t, d);
+        gs.load(dy + at * lddy, t, d);
+        mu = mean[at];
+        rs = rstd[at];
+    }
+    float w[E], dw[E], db[E];
+    load_weights<T, G, E>(weight, 1.0f, t, d, w);
+#pragma unroll
+    for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
+    int turn = 0;
+    for (; r - group < rows; r += ahead) {
+        const bool more = r - group + ahead < rows;
+        const int64_t at = min(r + ahead, rows - 1);
+        if (AHEAD && more) {
+            xn.load(x + at * ldx, t, d);
+            gn.load(dy + at * lddy, t, d);
+            mun = mean[at];
+            rsn = rstd[at];
+        }
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float g = gs[i] * w[i];
+            s[0] += g;
+            s[1] = fmaf(g, (xs[i] - mu) * rs, s[1]);
+        }
+        group_sums<G, 2>(s, lds, turn);
+        if (r < rows) {
+            const float a = s[0] / (float)d, b = s[1] / (float)d;
+            P out;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float dyi = gs[i], h = (xs[i] - mu) * rs;
+                dw[i] = fmaf(dyi, h, dw[i]);
+                db[i] += dyi;
+                out.set(i, rs * (fmaf(dyi, w[i], -a) - h * b));
+            }
+            if (dx) out.store(dx + r * d, t, d);
+        }
+        if (AHEAD) {
+            if (more) {
+                xs = xn;
+                gs = gn;
+                mu = mun;
+                rs = rsn;
+            }
+        } else if (more) {
+            xs.load(x + at * ldx, t, d);
+            gs.load(dy + at * lddy, t, d);
+            mu = mean[at];
+            rs = rstd[at];
+        }
+    }
+    if (!parts) return;
+    if constexpr (R > 1) {  // the groups' sums, in their order
+        __shared__ float both[2 * G * E];
+        for (int g = 0; g < R; ++g) {
+            __syncthreads();
+            if (group == g)
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    float *p = both + 2 * (i * G + t);
+                    p[0] = g ? p[0] + dw[i] : dw[i];
+                    p[1] = g ? p[1] + db[i] : db[i];
+                }
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            dw[i] = both[2 * (i * G + t)];
+            db[i] = both[2 * (i * G + t) + 1];
+        }
+    }
+    float *mine = parts + (size_t)blockIdx.x * 2 * d;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int c = P::column(i, t);
+        if (c < d) {
+            mine[c] = dw[i];
+            mine[d + c] = db[i];
+        }
+    }
+}
+
+// The sums of `count` parts [count][2][d], 64 columns a workgroup, a sixteenth of the parts each wavefront.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float *__restrict__ parts, int count, int d,
+                                                         float *__restrict__ dweight, float *__restrict__ dbias)
+{
+    __shared__ float lds[16][WAVE];
+    const int wave = threadIdx.x >> 6, lane = lane_id();
+    const int64_t c = (int64_t)blockIdx.x * WAVE + lane;
+    float s = 0.0f;
+    if (c < 2 * (int64_t)d) {
+#pragma unroll 8
+        for (int p = wave; p < count; p += 16) s += parts[(size_t)p * 2 * d + c];
+    }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= 2 * (int64_t)d) return;
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) s += lds[w][lane];
+    if (c < d) {
+        if (dweight) dweight[c] = s;
+    } else if (dbias) {
+        dbias[c - d] = s;
+    }
+}
+
+// Rows beyond 16384 elements.
 
 // Sum over the workgroup, in every thread.
 __device__ __forceinline__ float group_sum(float v, float *lds)
@@ -77,21 +342,6 @@ __global__ __launch_bounds__(NORM_WG) void norm_weights_kernel(const T *__restri
     parts[((size_t)blockIdx.y * 2 + 1) * d + c] = sb;
 }
 
-// The sums of `count` parts [count][2][d].
-__global__ __launch_bounds__(NORM_WG) void norm_join_kernel(const float *__restrict__ parts, int count, int d,
-                                                            float *__restrict__ dweight, float *__restrict__ dbias)
-{
-    const int c = blockIdx.x * NORM_WG + threadIdx.x;
-    if (c >= d) return;
-    float sw = 0.0f, sb = 0.0f;
-    for (int p = 0; p < count; ++p) {
-        sw += parts[((size_t)p * 2) * d + c];
-        sb += parts[((size_t)p * 2 + 1) * d + c];
-    }
-    if (dweight) dweight[c] = sw;
-    if (dbias) dbias[c] = sb;
-}
-
 // dx, a workgroup per row.
 template <typename T, typename W>
 __global__ __launch_bounds__(NORM_WG) void norm_dx_kernel(const T *dy, int64_t lddy, const T *x, int64_t ldx,
@@ -118,9 +368,18 @@ __global__ __launch_bounds__(NORM_WG) void norm_dx_kernel(const T *dy, int64_t l
     }
 }
 
-constexpr int NORM_PARTS = 256;  // stretches of rows whose weight gradients are summed apart
+constexpr int NORM_LONG = 16384;  // longest rows that stay in registers
+constexpr int NORM_PARTS = 512;   // most stretches of rows whose weight gradients are summed apart
 
-int norm_parts(int64_t rows) { return (int)std::min<int64_t>(NORM_PARTS, std::max<int64_t>(1, ceil_div(rows, 16))); }
+// Threads that share a row: eight elements each up to 8192, sixteen beyond.
+int norm_group(int d) { return d <= 128 ? 16 : d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
+int back_threads(int d) { return std::max(norm_group(d), 512); }
+
+int norm_parts(int64_t rows, int d)
+{
+    const int64_t at_once = d > NORM_LONG ? 16 : back_threads(d) / norm_group(d);
+    return (int)std::min<int64_t>(NORM_PARTS, std::max<int64_t>(1, ceil_div(rows, at_once)));
+}
 
 unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
 
@@ -129,7 +388,7 @@ unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 <<
 size_t layer_norm_workspace(int64_t rows, int d)
 {
     if (rows < 0 || d < 1) return 0;
-    return (size_t)norm_parts(rows) * 2 * (size_t)d * sizeof(float);
+    return (size_t)norm_parts(rows, d) * 2 * (size_t)d * sizeof(float);
 }
 
 static int norm_check(const char *who, int type, int wtype, int64_t rows, int d, int64_t ldx, int64_t ldy)
@@ -143,12 +402,39 @@ static int norm_check(const char *who, int type, int wtype, int64_t rows, int d,
     return QADC_OK;
 }
 
+template <typename T, typename W, int G, int E>
+static void norm_launch_rows(const void *x, int64_t ldx, const void *weight, const void *bias, int64_t rows, int d, float eps,
+                             void *y, float *mean, float *rstd, hipStream_t st)
+{
+    constexpr int THREADS = G > 256 ? G : 256;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(rows, THREADS / G), 2048 * 256 / THREADS);
+    launch(QADC_PROF_NORM, norm_rows_kernel<T, W, G, E, THREADS>, dim3(grid), dim3(THREADS), 0, st, (const T *)x, ldx,
+           (const W *)weight, (const W *)bias, rows, d, eps, (T *)y, mean, rstd);
+}
+
 template <typename T, typename W>
 static void norm_launch(const void *x, int64_t ldx, const void *weight, const void *bias, int64_t rows, int d, float eps,
                         void *y, float *mean, float *rstd, hipStream_t st)
 {
-    launch(QADC_PROF_NORM, norm_kernel<T, W>, dim3(norm_grid(rows)), dim3(NORM_WG), 0, st, (const T *)x, ldx,
-           (const W *)weight, (const W *)bias, rows, d, eps, (T *)y, mean, rstd);
+#define ROWS(G_, E_) norm_launch_rows<T, W, G_, E_>(x, ldx, weight, bias, rows, d, eps, y, mean, rstd, st)
+    if (d > NORM_LONG) {
+        launch(QADC_PROF_NORM, norm_kernel<T, W>, dim3(norm_grid(rows)), dim3(NORM_WG), 0, st, (const T *)x, ldx,
+               (const W *)weight, (const W *)bias, rows, d, eps, (T *)y, mean, rstd);
+        return;
+    }
+    switch (norm_group(d)) {
+    case 16: ROWS(16, 8); break;
+    case 32: ROWS(32, 8); break;
+    case 64: ROWS(64, 8); break;
+    case 128: ROWS(128, 8); break;
+    case 256: ROWS(256, 8); break;
+    case 512: ROWS(512, 8); break;
+    default:
+        if (d <= 8192) ROWS(1024, 8);
+        else ROWS(1024, 16);
+        break;
+    }
+#undef ROWS
 }
 
 int layer_norm(const void *x, int64_t ldx, int type, const void *weight, const void *bias, int wtype, int64_t rows, int d,
@@ -168,20 +454,49 @@ int layer_norm(const void *x, int64_t ldx, int type, const void *weight, const v
     return QADC_OK;
 }
 
+template <typename T, typename W, int G, int E>
+static void norm_launch_back(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight, const float *mean,
+                             const float *rstd, int64_t rows, int d, void *dx, float *parts, hipStream_t st)
+{
+    constexpr int THREADS = G > 512 ? G : 512;
+    constexpr bool AHEAD = E == 8;  // (sixteen elements a thread leave no registers for the next row's)
+    const unsigned grid = (unsigned)norm_parts(rows, d);
+    launch(QADC_PROF_NORM, norm_back_kernel<T, W, G, E, THREADS, AHEAD>, dim3(grid), dim3(THREADS), 0, st, (const T *)dy, lddy,
+           (const T *)x, ldx, (const W *)weight, mean, rstd, rows, d, (T *)dx, parts);
+}
+
 template <typename T, typename W>
 static void norm_backward_launch(const void *dy, int64_t lddy, const void *x, int64_t ldx, const void *weight,
                                  const float *mean, const float *rstd, int64_t rows, int d, void *dx, float *dweight,
                                  float *dbias, float *parts, hipStream_t st)
 {
-    if (dweight || dbias) {
-        const int count = norm_parts(rows);
-        const int64_t stretch = ceil_div(rows, count);
+    const bool sums = dweight || dbias;
+    int count = 0;  // without rows the sums of no parts are written
+    if (rows > 0 && d <= NORM_LONG) {
+        count = norm_parts(rows, d);
+#define BACK(G_, E_) norm_launch_back<T, W, G_, E_>(dy, lddy, x, ldx, weight, mean, rstd, rows, d, dx, sums ? parts : nullptr, st)
+        switch (norm_group(d)) {
+        case 16: BACK(16, 8); break;
+        case 32: BACK(32, 8); break;
+        case 64: BACK(64, 8); break;
+        case 128: BACK(128, 8); break;
+        case 256: BACK(256, 8); break;
+        case 512: BACK(512, 8); break;
+        default:
+            if (d <= 8192) BACK(1024, 8);
+            else BACK(1024, 16);
+            break;
+        }
+#undef BACK
+    } else if (rows > 0 && sums) {
+        count = norm_parts(rows, d);
         launch(QADC_PROF_NORM, norm_weights_kernel<T>, dim3((unsigned)ceil_div(d, NORM_WG), (unsigned)count), dim3(NORM_WG), 0,
-               st, (const T *)dy, lddy, (const T *)x, ldx, mean, rstd, rows, d, stretch, parts);
-        launch(QADC_PROF_NORM, norm_join_kernel, dim3((unsigned)ceil_div(d, NORM_WG)), dim3(NORM_WG), 0, st, parts, count, d,
-               dweight, dbias);
+               st, (const T *)dy, lddy, (const T *)x, ldx, mean, rstd, rows, d, ceil_div(rows, count), parts);
     }
-    if (dx && rows > 0)
+    if (sums)
+        launch(QADC_PROF_NORM, norm_join_kernel, dim3((unsigned)ceil_div(2 * (int64_t)d, WAVE)), dim3(1024), 0, st, parts, count,
+               d, dweight, dbias);
+    if (dx && rows > 0 && d > NORM_LONG)
         launch(QADC_PROF_NORM, norm_dx_kernel<T, W>, dim3(norm_grid(rows)), dim3(NORM_WG), 0, st, (const T *)dy, lddy,
                (const T *)x, ldx, (const W *)weight, mean, rstd, rows, d, (T *)dx);
 }
