@@ -88,11 +88,11 @@ __device__ __forceinline__ float wave_max(float v)
 }
 
 // Runs `call` with T = float, _Float16 or __bf16 by the element type.
-#define QADC_BY_TYPE(type, call)                             \
-    switch (type) {                                          \
-    case QADC_TYPE_F32: { using T = float; call; } break;    \
-    case QADC_TYPE_F16: { using T = _Float16; call; } break; \
-    default: { using T = __bf16; call; } break;              \
+#define QADC_BY_TYPE(type, ...)                                     \
+    switch (type) {                                                 \
+    case QADC_TYPE_F32: { using T = float; __VA_ARGS__; } break;    \
+    case QADC_TYPE_F16: { using T = _Float16; __VA_ARGS__; } break; \
+    default: { using T = __bf16; __VA_ARGS__; } break;              \
     }
 
 }  // namespace qadc

@@ -38,7 +38,8 @@ def test_weights4_and_linear4():
     L = Q.lib()
     size = Q.qadc_weights4_bytes
     assert size(16, 128, 128, 0) == 1024 + 32 and size(16, 128, 128, 1) == 1024 + 48
-    assert size(17, 129, 32, 1) == 4 * 1024 + 2 * 5 * 48
+    assert size(17, 129, 32, 1) == 4 * 1024 + 2 * 2 * 4 * 48  # the groups of a tile's inputs lie together
+    assert size(17, 129, 256, 1) == 4 * 1024 + 2 * 48
     for bad in ((0, 128, 128, 0), (16, 0, 128, 0), (16, (1 << 24) + 1, 128, 0), (16, 128, 48, 0), (16, 128, 0, 0), (16, 128, 192, 0),
                 (1 << 31, 128, 128, 0)):
         assert size(*bad) == 0
