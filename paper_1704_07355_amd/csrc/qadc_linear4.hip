@@ -130,16 +130,16 @@ struct Inputs {
     static constexpr bool HALF = std::is_same_v<T, _Float16>;
     bits16x8 part[PARTS];
 
-    __device__ __forceinline__ void load(const T *row, int64_t k, int64_t K)
+    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    __device__ static __forceinline__ V load_last(const T *row, int64_t k, int64_t K)  // 0 beyond the row
     {
-        typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
         V v;
-        if (k + 8 <= K) {
-            v = *reinterpret_cast<const V *>(row + k);
-        } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = k + e < K ? row[k + e] : (T)0.0f;
-        }
+        for (int e = 0; e < 8; ++e) v[e] = k + e < K ? row[k + e] : (T)0.0f;
+        return v;
+    }
+    __device__ __forceinline__ explicit Inputs(V v)
+    {
         if constexpr (PARTS == 1) {
             part[0] = __builtin_bit_cast(bits16x8, v);
         } else {
@@ -159,7 +159,7 @@ struct Inputs {
 };
 
 // Wavefronts that may share a block: their sums, `values` a lane, fit in 64 KB.
-constexpr int most_split(int values) { return values <= 16 ? 16 : 256 / values; }
+constexpr int most_split(int values) { return values <= 8 ? 16 : 8; }
 
 struct Args4 {
     const char *packed;
@@ -176,7 +176,7 @@ template <typename T, int STEPS, int MR, int MT, int NT>
 __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y, int split)
 {
     constexpr int DEPTH = 2, PER = 4 / STEPS, ROWS = 4 * MR * MT;
-    constexpr bool HALF = Inputs<T>::HALF;
+    constexpr bool HALF = Inputs<T>::HALF, AHEAD = MT * sizeof(T) <= 4;
     extern __shared__ float lds[];
     const int lane = lane_id(), wave = threadIdx.x >> 6, n = lane & 15, j = lane >> 4;
     const int at_once = (int)(blockDim.x >> 6) / split;  // blocks of a workgroup
@@ -211,36 +211,68 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
 #pragma unroll
     for (int i = 0; i < 4; ++i) ones[i] = HALF ? 0x3C003C00u : 0x3F803F80u;
 
+    // The next tiles on their way: weights, scales and zero points DEPTH tiles ahead, x one.
+    typedef typename Inputs<T>::V V;
+    typedef std::conditional_t<PER == 4, u32x2, std::conditional_t<PER == 2, uint32_t, uint16_t>> Scales;
+    typedef std::conditional_t<PER == 4, uint32_t, std::conditional_t<PER == 2, uint16_t, uint8_t>> Zeros;
     bits16x8 ring[DEPTH][NT];
+    Scales ring_s[DEPTH][NT];
+    Zeros ring_z[DEPTH][NT];
     const auto fetch = [&](int d, int k) {
+        const int64_t set = k / a.s.span * W4_N;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ring[d][t] = __builtin_nontemporal_load(weights[t] + (int64_t)k * WAVE);
+        for (int t = 0; t < NT; ++t) {
+            ring[d][t] = __builtin_nontemporal_load(weights[t] + (int64_t)k * WAVE);
+            ring_s[d][t] = reinterpret_cast<const Scales *>(scales[t])[set];
+            if (a.has_zeros) ring_z[d][t] = reinterpret_cast<const Zeros *>(zeros[t])[set];
+        }
     };
+    const auto fetch_x = [&](int k, V(&v)[MT][4]) {
+        const int64_t at = (int64_t)k * W4_K + 8 * j;
+        if ((int64_t)(k + 1) * W4_K <= a.K) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) v[t][s] = *reinterpret_cast<const V *>(rows[t] + at + 32 * s);
+        } else {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) v[t][s] = Inputs<T>::load_last(rows[t], at + 32 * s, a.K);
+        }
+    };
+    V xs[MT][4], xn[MT][4];
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d)
         if (part + d * split < tiles) fetch(d, part + d * split);
+    if (part < tiles) fetch_x(part, xn);
 
     for (int k0 = part; k0 < tiles; k0 += DEPTH * split) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int k = k0 + d * split;
             if (k < tiles) {
-                // this tile's scales and zero points
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) xs[t][s] = xn[t][s];
+                if (AHEAD && k + split < tiles) fetch_x(k + split, xn);
+                bits16x8 now[NT];
                 float sc[NT][PER], zp[NT][PER];
-                const int64_t set = k / a.s.span;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
+                    now[t] = ring[d][t];
                     uint16_t bits[PER];
-                    __builtin_memcpy(bits, __builtin_assume_aligned(scales[t] + set * (W4_N * PER * 2), PER * 2), PER * 2);
                     uint8_t z[PER];
-                    if (a.has_zeros)
-                        __builtin_memcpy(z, __builtin_assume_aligned(zeros[t] + set * (W4_N * PER), PER), PER);
+                    __builtin_memcpy(bits, &ring_s[d][t], sizeof(bits));
+                    __builtin_memcpy(z, &ring_z[d][t], sizeof(z));
 #pragma unroll
                     for (int g = 0; g < PER; ++g) {
                         sc[t][g] = scale4(bits[g], a.stype);
                         zp[t][g] = a.has_zeros ? 16.0f + (float)z[g] : 24.0f;
                     }
                 }
+                if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
 #pragma unroll
                 for (int g = 0; g < PER; ++g) {
                     f32x4 p[MT][NT], one[MT];
@@ -249,11 +281,10 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
                         const int step = g * STEPS + s;
                         bits16x8 w[NT];
 #pragma unroll
-                        for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(ring[d][u][step]);
+                        for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(now[u][step]);
 #pragma unroll
                         for (int t = 0; t < MT; ++t) {
-                            Inputs<T> in;
-                            in.load(rows[t], (int64_t)k * W4_K + 32 * step + 8 * j, a.K);
+                            const Inputs<T> in(xs[t][step]);
 #pragma unroll
                             for (int q = 0; q < Inputs<T>::PARTS; ++q) {
                                 const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -271,7 +302,7 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
                             for (int i = 0; i < MR; ++i)
                                 sum[t][u][i] = fmaf(sc[u][g], fmaf(-zp[u][g], one[t][i], p[t][u][i]), sum[t][u][i]);
                 }
-                if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
+                if (!AHEAD && k + split < tiles) fetch_x(k + split, xn);
             }
         }
     }
