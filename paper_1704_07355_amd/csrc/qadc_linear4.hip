@@ -13,6 +13,7 @@
 // outputs, a column of ones with x; with p and t the two sums over a group, the group adds s (p - (16 + z) t) to the output.
 
 #include <algorithm>
+#include <mutex>
 #include <type_traits>
 
 #include "qadc_half.h"
@@ -158,50 +159,70 @@ struct Inputs {
     }
 };
 
-// Wavefronts that may share a block: their sums, `values` a lane, fit in 64 KB.
-constexpr int most_split(int values) { return values <= 8 ? 16 : 8; }
-
 struct Args4 {
     const char *packed;
     Shape4 s;
     int64_t N, M, ldx, ldy;
     int K, stype, has_zeros;
     const float *bias;
+    int split;  // wavefronts that share a block
+    int chunk;  // tiles of x in LDS at a time
 };
 
-// A block of NT x 16 outputs and up to 16 MT rows of x: SPLIT wavefronts, each every SPLIT-th tile of the inputs.  Of a matrix
-// instruction's 16 rows, 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work
-// behind the products); the others repeat them.  STEPS: instructions per group.
-template <typename T, int STEPS, int MR, int MT, int NT>
-__global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y, int split)
-{
-    constexpr int DEPTH = 2, PER = 4 / STEPS, ROWS = 4 * MR * MT;
-    constexpr bool HALF = Inputs<T>::HALF, AHEAD = MT * sizeof(T) <= 4;
-    extern __shared__ float lds[];
-    const int lane = lane_id(), wave = threadIdx.x >> 6, n = lane & 15, j = lane >> 4;
-    const int at_once = (int)(blockDim.x >> 6) / split;  // blocks of a workgroup
-    const int64_t block = ((int64_t)blockIdx.x * at_once + wave / split) * NT;
-    const int part = wave % split;
-    const int64_t m0 = (int64_t)blockIdx.y * ROWS;
-    const int tiles = a.s.tiles;
+constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's rows lie in different banks
 
-    // this lane's row of x in each m-tile, and where its weights and scales are
-    const T *rows[MT];
+// A block of NT x 16 outputs and up to 4 MR MT rows of x: `split` wavefronts, each every split-th tile of the inputs; a workgroup
+// has as many blocks as it has wavefronts for, and brings x into LDS for all of them.  Of a matrix instruction's 16 rows,
+// 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
+// others repeat them.  STEPS: instructions per group.
+template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
+__global__ __launch_bounds__(THREADS, MT == 4 || (MT == 2 && (sizeof(T) == 4 || STEPS == 1)) ? 2 : 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
+{
+    constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
+    constexpr bool HALF = Inputs<T>::HALF;
+    extern __shared__ float lds[];
+    uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [PARTS][rows][chunk * W4_K + X_PAD]
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
+    const int split = a.split, at_once = THREADS / WAVE / split;
+    const int64_t block = ((int64_t)blockIdx.x * at_once + wave / split) * NT;
+    const int part = wave % split, tiles = a.s.tiles;
+    const int64_t m0 = (int64_t)blockIdx.y * ROWS;
+    const int rows = (int)min((int64_t)ROWS, a.M - m0), stride = a.chunk * W4_K + X_PAD;
+
+    // where this lane's row of x in each m-tile lies, and its weights and scales
+    int at_x[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int i = n & 3;
-        const int64_t m = m0 + t * 4 * MR + (n >> 2) * MR + (i < MR ? i : 0);
-        rows[t] = x + min(m, a.M - 1) * a.ldx;
+        const int i = n & 3, m = t * 4 * MR + (n >> 2) * MR + (i < MR ? i : 0);
+        at_x[t] = min(m, rows - 1) * stride + 8 * j;
     }
-    const bits16x8 *weights[NT];
-    const char *scales[NT], *zeros[NT];
+    const char *weights[NT], *scales[NT], *zeros[NT];  // (the same in all lanes)
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int64_t b = min(block + t, a.s.blocks - 1);
-        weights[t] = reinterpret_cast<const bits16x8 *>(a.packed) + b * tiles * WAVE + lane;
-        scales[t] = a.packed + a.s.scales + (b * a.s.sets * W4_N + n) * PER * 2;
-        zeros[t] = a.packed + a.s.zeros + (b * a.s.sets * W4_N + n) * PER;
+        weights[t] = a.packed + b * tiles * W4_BYTES;
+        scales[t] = a.packed + a.s.scales + b * a.s.sets * (W4_N * PER * 2);
+        zeros[t] = a.packed + a.s.zeros + b * a.s.sets * (W4_N * PER);
     }
+    // The next tiles on their way.
+    typedef std::conditional_t<PER == 4, u32x2, std::conditional_t<PER == 2, uint32_t, uint16_t>> Scales;
+    typedef std::conditional_t<PER == 4, uint32_t, std::conditional_t<PER == 2, uint16_t, uint8_t>> Zeros;
+    bits16x8 ring[DEPTH][NT];
+    Scales ring_s[DEPTH][NT];
+    Zeros ring_z[DEPTH][NT];
+    const auto fetch = [&](int d, int k) {
+        const unsigned set = (unsigned)(k / a.s.span) * W4_N + n;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            ring[d][t] = __builtin_nontemporal_load(reinterpret_cast<const bits16x8 *>(weights[t]) + ((unsigned)k * WAVE + lane));
+            ring_s[d][t] = reinterpret_cast<const Scales *>(scales[t])[set];
+            if (a.has_zeros) ring_z[d][t] = reinterpret_cast<const Zeros *>(zeros[t])[set];
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (part + d * split < tiles) fetch(d, part + d * split);
+
     f32x4 sum[MT][NT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -211,57 +232,36 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
 #pragma unroll
     for (int i = 0; i < 4; ++i) ones[i] = HALF ? 0x3C003C00u : 0x3F803F80u;
 
-    // The next tiles on their way: weights, scales and zero points DEPTH tiles ahead, x one.
-    typedef typename Inputs<T>::V V;
-    typedef std::conditional_t<PER == 4, u32x2, std::conditional_t<PER == 2, uint32_t, uint16_t>> Scales;
-    typedef std::conditional_t<PER == 4, uint32_t, std::conditional_t<PER == 2, uint16_t, uint8_t>> Zeros;
-    bits16x8 ring[DEPTH][NT];
-    Scales ring_s[DEPTH][NT];
-    Zeros ring_z[DEPTH][NT];
-    const auto fetch = [&](int d, int k) {
-        const int64_t set = k / a.s.span * W4_N;
+    // x, a chunk of tiles at a time; every wavefront comes by here once for each chunk
+    int first = 0, end = 0;  // the tiles in LDS
+    const auto next_chunk = [&]() {
+        first = end;
+        end = min(first + a.chunk, tiles);
+        const unsigned packs = (unsigned)(end - first) * (W4_K / 8), all = packs * (unsigned)rows;
+        if (first) __syncthreads();  // (the chunk before has been read)
+        for (unsigned i = threadIdx.x; i < all; i += THREADS) {
+            const unsigned r = i / packs, c = i % packs * 8;
+            const int64_t k = (int64_t)first * W4_K + c;
+            const T *row = x + (m0 + r) * a.ldx;
+            const Inputs<T> in(k + 8 <= a.K ? *reinterpret_cast<const typename Inputs<T>::V *>(row + k)
+                                            : Inputs<T>::load_last(row, k, a.K));
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            ring[d][t] = __builtin_nontemporal_load(weights[t] + (int64_t)k * WAVE);
-            ring_s[d][t] = reinterpret_cast<const Scales *>(scales[t])[set];
-            if (a.has_zeros) ring_z[d][t] = reinterpret_cast<const Zeros *>(zeros[t])[set];
+            for (int p = 0; p < PARTS; ++p)
+                *reinterpret_cast<bits16x8 *>(xs + ((unsigned)(p * rows) + r) * stride + c) = in.part[p];
         }
+        __syncthreads();
     };
-    const auto fetch_x = [&](int k, V(&v)[MT][4]) {
-        const int64_t at = (int64_t)k * W4_K + 8 * j;
-        if ((int64_t)(k + 1) * W4_K <= a.K) {
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int s = 0; s < 4; ++s) v[t][s] = *reinterpret_cast<const V *>(rows[t] + at + 32 * s);
-        } else {
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int s = 0; s < 4; ++s) v[t][s] = Inputs<T>::load_last(rows[t], at + 32 * s, a.K);
-        }
-    };
-    V xs[MT][4], xn[MT][4];
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d)
-        if (part + d * split < tiles) fetch(d, part + d * split);
-    if (part < tiles) fetch_x(part, xn);
+    next_chunk();
 
     for (int k0 = part; k0 < tiles; k0 += DEPTH * split) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const int k = k0 + d * split;
             if (k < tiles) {
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) xs[t][s] = xn[t][s];
-                if (AHEAD && k + split < tiles) fetch_x(k + split, xn);
-                bits16x8 now[NT];
+                while (k >= end) next_chunk();
                 float sc[NT][PER], zp[NT][PER];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    now[t] = ring[d][t];
                     uint16_t bits[PER];
                     uint8_t z[PER];
                     __builtin_memcpy(bits, &ring_s[d][t], sizeof(bits));
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
                         zp[t][g] = a.has_zeros ? 16.0f + (float)z[g] : 24.0f;
                     }
                 }
-                if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
+                const uint16_t *tile = xs + (k - first) * W4_K;
 #pragma unroll
                 for (int g = 0; g < PER; ++g) {
                     f32x4 p[MT][NT], one[MT];
@@ -281,18 +281,18 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
                         const int step = g * STEPS + s;
                         bits16x8 w[NT];
 #pragma unroll
-                        for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(now[u][step]);
+                        for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(ring[d][u][step]);
 #pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            const Inputs<T> in(xs[t][step]);
+                        for (int t = 0; t < MT; ++t)
 #pragma unroll
-                            for (int q = 0; q < Inputs<T>::PARTS; ++q) {
+                            for (int q = 0; q < PARTS; ++q) {
+                                const bits16x8 in =
+                                    *reinterpret_cast<const bits16x8 *>(tile + q * rows * stride + at_x[t] + 32 * step);
                                 const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-                                one[t] = mfma16<HALF>(in.part[q], ones, s + q ? one[t] : none);
+                                one[t] = mfma16<HALF>(in, ones, s + q ? one[t] : none);
 #pragma unroll
-                                for (int u = 0; u < NT; ++u) p[t][u] = mfma16<HALF>(in.part[q], w[u], s + q ? p[t][u] : none);
+                                for (int u = 0; u < NT; ++u) p[t][u] = mfma16<HALF>(in, w[u], s + q ? p[t][u] : none);
                             }
-                        }
                     }
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
@@ -302,10 +302,11 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
                             for (int i = 0; i < MR; ++i)
                                 sum[t][u][i] = fmaf(sc[u][g], fmaf(-zp[u][g], one[t][i], p[t][u][i]), sum[t][u][i]);
                 }
-                if (!AHEAD && k + split < tiles) fetch_x(k + split, xn);
+                if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
             }
         }
     }
+    while (end < tiles) next_chunk();
 
     const auto write = [&](int64_t b, int t, int i, float v) {  // output n of block b, row (t, j, i)
         const int64_t m = m0 + t * 4 * MR + j * MR + i, out = b * W4_N + n;
@@ -322,6 +323,7 @@ __global__ __launch_bounds__(WAVE *most_split(MT *NT *MR)) void linear4_kernel(A
     }
     // the wavefronts' sums, joined in their order: [wave][value][lane]
     constexpr int VALUES = MT * NT * MR;
+    __syncthreads();  // (x has been read)
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -371,34 +373,52 @@ int pack_weights4(const uint8_t *codes, const void *scales, int stype, const uin
     return QADC_OK;
 }
 
-template <typename T, int STEPS, int MR, int MT, int NT>
-static void linear4_launch(const Args4 &a, const void *x, void *y, hipStream_t st)
+// LDS for x: two workgroups a compute unit, one where a float32 x takes three times the room.
+constexpr size_t x_lds(size_t type_bytes) { return type_bytes == 4 ? 156 << 10 : 78 << 10; }
+
+template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
+static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
 {
+    constexpr int WAVES = THREADS / WAVE, PARTS = Inputs<T>::PARTS;
+    constexpr size_t sums = (size_t)WAVES * MT * NT * MR * WAVE * sizeof(float);
+    static std::once_flag once;
+    static hipError_t attr = hipSuccess;
+    const auto kernel = &linear4_kernel<T, STEPS, MR, MT, NT, THREADS>;
+    std::call_once(once, [&] {  // more than the default limit of dynamic LDS
+        attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)std::max(x_lds(sizeof(T)), sums));
+    });
+    QADC_HIP_TRY(attr);
     // As many wavefronts a block as the chip holds for these outputs, but no more than there are tiles.
-    constexpr int most = most_split(MT * NT * MR);
-    const int64_t blocks = ceil_div(a.s.blocks, NT), rows = ceil_div(a.M, 4 * MR * MT);
-    int split = 1;
-    while (split < most && blocks * rows * split < 4096 && 2 * split <= a.s.tiles) split *= 2;
-    const int waves = std::max(split, 4), at_once = waves / split;
-    const size_t shared = split > 1 ? (size_t)waves * MT * NT * MR * WAVE * sizeof(float) : 0;
-    launch(QADC_PROF_LINEAR4, linear4_kernel<T, STEPS, MR, MT, NT>, dim3((unsigned)ceil_div(blocks, at_once), (unsigned)rows),
-           dim3(waves * WAVE), shared, st, a, (const T *)x, (T *)y, split);
+    const int64_t blocks = ceil_div(a.s.blocks, NT), row_blocks = ceil_div(a.M, 4 * MR * MT);
+    a.split = 1;
+    while (a.split < WAVES && blocks * row_blocks * a.split < 4096 && 2 * a.split <= a.s.tiles) a.split *= 2;
+    const size_t row_bytes = (size_t)std::min<int64_t>(4 * MR * MT, a.M) * PARTS * 2;
+    a.chunk = (int)std::min<size_t>(a.s.tiles, (x_lds(sizeof(T)) / row_bytes - X_PAD) / W4_K);
+    const size_t shared = std::max(row_bytes * (a.chunk * W4_K + X_PAD), a.split > 1 ? sums : 0);
+    launch(QADC_PROF_LINEAR4, *kernel, dim3((unsigned)ceil_div(blocks, WAVES / a.split), (unsigned)row_blocks), dim3(THREADS),
+           shared, st, a, (const T *)x, (T *)y);
+    return QADC_OK;
 }
 
 template <typename T, int STEPS>
-static void linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
+static int linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
 {
     // the y dimension of a grid is 16 bits wide: rows in slabs
-    const int64_t slab = 65535 * 64ll, M = a.M;
+    const int64_t slab = 65535 * 32ll, M = a.M;
     for (int64_t m = 0; m < M; m += slab) {
         a.M = std::min(slab, M - m);
         const T *xs = x + m * a.ldx;
         T *ys = y + m * a.ldy;
-        if (a.M <= 4) linear4_launch<T, STEPS, 1, 1, 2>(a, xs, ys, st);
-        else if (a.M <= 16) linear4_launch<T, STEPS, 4, 1, 2>(a, xs, ys, st);
-        else if (a.M <= 32) linear4_launch<T, STEPS, 4, 2, 2>(a, xs, ys, st);
-        else linear4_launch<T, STEPS, 4, 4, 2>(a, xs, ys, st);
+        int rc;
+        if (a.M <= 4) rc = a.s.blocks < 1024 ? linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st)
+                                             : linear4_launch<T, STEPS, 1, 1, 2, 512>(a, xs, ys, st);
+        else if (a.M <= 16) rc = linear4_launch<T, STEPS, 4, 1, 2, 512>(a, xs, ys, st);
+        else if (a.M <= 32 || sizeof(T) == 4) rc = linear4_launch<T, STEPS, 4, 2, 2, 512>(a, xs, ys, st);
+        else rc = linear4_launch<T, STEPS, 4, 4, 2, 512>(a, xs, ys, st);
+        if (rc != QADC_OK) return rc;
     }
+    return QADC_OK;
 }
 
 int linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_t M, const float *bias, void *y, int64_t ldy,
@@ -413,12 +433,14 @@ int linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_
     if (!w->packed || !x || !y) return fail(QADC_EINVAL, "qadc_linear4: null pointer");
     if ((uintptr_t)w->packed % 16) return fail(QADC_EINVAL, "qadc_linear4: packed is not 16-byte aligned");
     const Args4 a = {(const char *)w->packed, shape4(w->N, w->K, w->group, w->has_zeros != 0), w->N, M, ldx, ldy, w->K, w->stype,
-                     w->has_zeros != 0, bias};
+                     w->has_zeros != 0, bias, 1, 1};
+    int rc = QADC_OK;
     QADC_BY_TYPE(type, {
-        if (w->group == 32) linear4_rows<T, 1>(a, (const T *)x, (T *)y, st);
-        else if (w->group == 64) linear4_rows<T, 2>(a, (const T *)x, (T *)y, st);
-        else linear4_rows<T, 4>(a, (const T *)x, (T *)y, st);
+        if (w->group == 32) rc = linear4_rows<T, 1>(a, (const T *)x, (T *)y, st);
+        else if (w->group == 64) rc = linear4_rows<T, 2>(a, (const T *)x, (T *)y, st);
+        else rc = linear4_rows<T, 4>(a, (const T *)x, (T *)y, st);
     });
+    if (rc != QADC_OK) return rc;
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }
