@@ -95,22 +95,17 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // The eight weights of a dword as 16 + q, in the type that the matrix units take: nibbles into bits 6 .. 9 of a binary16 of
-// exponent 4, into bits 3 .. 6 of a bfloat16.
+// exponent 4, into bits 3 .. 6 of a bfloat16.  `sixteen` is a pair of 16s that the compiler does not know: a three-operand
+// instruction takes one constant from outside the vector registers, not two.
 template <bool HALF>
-__device__ __forceinline__ bits16x8 weights8(unsigned v)
+__device__ __forceinline__ bits16x8 weights8(unsigned v, unsigned sixteen)
 {
+    constexpr unsigned mask = HALF ? 0x03C003C0u : 0x00780078u;
     bits16x8 w;
-    if constexpr (HALF) {
-        w[0] = (v << 6 & 0x03C003C0u) | 0x4C004C00u;
-        w[1] = (v << 2 & 0x03C003C0u) | 0x4C004C00u;
-        w[2] = (v >> 2 & 0x03C003C0u) | 0x4C004C00u;
-        w[3] = (v >> 6 & 0x03C003C0u) | 0x4C004C00u;
-    } else {
-        w[0] = (v << 3 & 0x00780078u) | 0x41804180u;
-        w[1] = (v >> 1 & 0x00780078u) | 0x41804180u;
-        w[2] = (v >> 5 & 0x00780078u) | 0x41804180u;
-        w[3] = (v >> 9 & 0x00780078u) | 0x41804180u;
-    }
+    w[0] = ((HALF ? v << 6 : v << 3) & mask) | sixteen;
+    w[1] = ((HALF ? v << 2 : v >> 1) & mask) | sixteen;
+    w[2] = ((HALF ? v >> 2 : v >> 5) & mask) | sixteen;
+    w[3] = ((HALF ? v >> 6 : v >> 9) & mask) | sixteen;
     return w;
 }
 
@@ -176,10 +171,11 @@ constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's
 // 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
 // others repeat them.  STEPS: instructions per group.
 template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
-__global__ __launch_bounds__(THREADS, MT == 4 || (MT == 2 && (sizeof(T) == 4 || STEPS == 1)) ? 2 : 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
+__global__ __launch_bounds__(THREADS, MT == 4 ? 2 : 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
 {
     constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
     constexpr bool HALF = Inputs<T>::HALF;
+    constexpr int UNROLL = MT == 1 ? PER : 1;  // (groups side by side do not fit the registers of more rows)
     extern __shared__ float lds[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [PARTS][rows][chunk * W4_K + X_PAD]
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
@@ -253,57 +249,80 @@ __global__ __launch_bounds__(THREADS, MT == 4 || (MT == 2 && (sizeof(T) == 4 || 
     };
     next_chunk();
 
-    for (int k0 = part; k0 < tiles; k0 += DEPTH * split) {
+    unsigned sixteen = HALF ? 0x4C004C00u : 0x41804180u;
+    asm volatile("" : "+v"(sixteen));
+
+    // one tile: its groups in turn, the weights, scales and zero points of the next one moved to the front each time
+    const auto tile = [&](auto which, int k) {
+        constexpr int d = decltype(which)::value;
+        while (k >= end) next_chunk();
+        bits16x8 q[NT];
+        Scales sb[NT];
+        Zeros zb[NT];
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int k = k0 + d * split;
-            if (k < tiles) {
-                while (k >= end) next_chunk();
-                float sc[NT][PER], zp[NT][PER];
+        for (int u = 0; u < NT; ++u) {
+            q[u] = ring[d][u];
+            sb[u] = ring_s[d][u];
+            zb[u] = ring_z[d][u];
+        }
+        if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
+        const uint16_t *from = xs + (k - first) * W4_K;
+#pragma unroll UNROLL
+        for (int g = 0; g < PER; ++g, from += 32 * STEPS) {
+            f32x4 p[MT][NT], one[MT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    uint16_t bits[PER];
-                    uint8_t z[PER];
-                    __builtin_memcpy(bits, &ring_s[d][t], sizeof(bits));
-                    __builtin_memcpy(z, &ring_z[d][t], sizeof(z));
+            for (int s = 0; s < STEPS; ++s) {
+                bits16x8 w[NT];
 #pragma unroll
-                    for (int g = 0; g < PER; ++g) {
-                        sc[t][g] = scale4(bits[g], a.stype);
-                        zp[t][g] = a.has_zeros ? 16.0f + (float)z[g] : 24.0f;
+                for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(q[u][s], sixteen);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int part_of = 0; part_of < PARTS; ++part_of) {
+                        const bits16x8 in =
+                            *reinterpret_cast<const bits16x8 *>(from + part_of * rows * stride + at_x[t] + 32 * s);
+                        const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+                        const bool more = s + part_of > 0;
+                        one[t] = mfma16<HALF>(in, ones, more ? one[t] : none);
+#pragma unroll
+                        for (int u = 0; u < NT; ++u) p[t][u] = mfma16<HALF>(in, w[u], more ? p[t][u] : none);
                     }
-                }
-                const uint16_t *tile = xs + (k - first) * W4_K;
-#pragma unroll
-                for (int g = 0; g < PER; ++g) {
-                    f32x4 p[MT][NT], one[MT];
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) {
-                        const int step = g * STEPS + s;
-                        bits16x8 w[NT];
-#pragma unroll
-                        for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(ring[d][u][step]);
-#pragma unroll
-                        for (int t = 0; t < MT; ++t)
-#pragma unroll
-                            for (int q = 0; q < PARTS; ++q) {
-                                const bits16x8 in =
-                                    *reinterpret_cast<const bits16x8 *>(tile + q * rows * stride + at_x[t] + 32 * step);
-                                const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-                                one[t] = mfma16<HALF>(in, ones, s + q ? one[t] : none);
-#pragma unroll
-                                for (int u = 0; u < NT; ++u) p[t][u] = mfma16<HALF>(in, w[u], s + q ? p[t][u] : none);
-                            }
-                    }
-#pragma unroll
-                    for (int t = 0; t < MT; ++t)
-#pragma unroll
-                        for (int u = 0; u < NT; ++u)
-#pragma unroll
-                            for (int i = 0; i < MR; ++i)
-                                sum[t][u][i] = fmaf(sc[u][g], fmaf(-zp[u][g], one[t][i], p[t][u][i]), sum[t][u][i]);
-                }
-                if (k + DEPTH * split < tiles) fetch(d, k + DEPTH * split);
             }
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                uint16_t bits;
+                uint8_t z;
+                __builtin_memcpy(&bits, &sb[u], 2);
+                __builtin_memcpy(&z, &zb[u], 1);
+                const float sc = scale4(bits, a.stype), zp = a.has_zeros ? 16.0f + (float)z : 24.0f;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int i = 0; i < MR; ++i) sum[t][u][i] = fmaf(sc, fmaf(-zp, one[t][i], p[t][u][i]), sum[t][u][i]);
+                if constexpr (PER == 4) {
+                    q[u] = __builtin_shufflevector(q[u], q[u], 1, 2, 3, 0);
+                    sb[u] = u32x2{sb[u][0] >> 16 | sb[u][1] << 16, sb[u][1] >> 16};
+                    zb[u] >>= 8;
+                } else if constexpr (PER == 2) {
+                    q[u] = __builtin_shufflevector(q[u], q[u], 2, 3, 0, 1);
+                    sb[u] >>= 16;
+                    zb[u] >>= 8;
+                }
+            }
+        }
+    };
+    int k = part;
+    while (k < tiles) {
+        tile(std::integral_constant<int, 0>(), k);
+        if ((k += split) >= tiles) break;
+        tile(std::integral_constant<int, 1>(), k);
+        k += split;
+        if constexpr (DEPTH == 4) {
+            if (k >= tiles) break;
+            tile(std::integral_constant<int, 2>(), k);
+            if ((k += split) >= tiles) break;
+            tile(std::integral_constant<int, 3>(), k);
+            k += split;
         }
     }
     while (end < tiles) next_chunk();

@@ -3,6 +3,11 @@
 // A row's neighbours have v_i = -beta (d_i - min d), so the largest is 0 and Z = sum exp v_i is at least 1.  For a token, with
 // a = the largest v_i among its votes: log P = a + log(sum of its exp(v_i - a)) - log Z, and
 // mix = logaddexp(lm + log(1 - lambda), log P + log lambda); nothing leaves the logarithm, so no weight is too small.
+//
+// A workgroup per row.  What costs most is the trip to values[ids[i]]: one for all neighbours of a row at once.  They then lie in
+// LDS as (token, exp v), and a thread adds up what its token has among its share of them, three instructions a neighbour and no
+// branch; P parts of a row's neighbours where there are fewer tokens than threads.  A token whose votes are all too small for
+// that (below e^-69) is added up again relative to its own largest.
 
 #include <algorithm>
 
@@ -13,72 +18,114 @@ namespace qadc {
 
 namespace {
 
-constexpr int MIX_WG = 256;
-
 __device__ __forceinline__ float log_add(float a, float b)
 {
     const float hi = fmaxf(a, b);
     return hi == -INFINITY || a != a || b != b ? a + b : hi + log1pf(expf(fminf(a, b) - hi));
 }
 
-template <typename F>
+template <int THREADS, typename F>
 __device__ __forceinline__ float group_join(float v, float *lds, F f)
 {
-#pragma unroll
-    for (int s = 32; s >= 1; s >>= 1) v = f(v, __shfl_xor(v, s));
-    __syncthreads();
+    if constexpr (THREADS == WAVE) return v;
     if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
-    for (int w = 1; w < MIX_WG / WAVE; ++w) v = f(v, lds[w]);
+#pragma unroll
+    for (int w = 1; w < THREADS / WAVE; ++w) v = f(v, lds[w]);
     return v;
 }
 
-// A workgroup per row, a thread per token.
-template <typename D>
-__global__ __launch_bounds__(MIX_WG) void mix_kernel(const uint32_t *__restrict__ ids, const D *__restrict__ dist,
-                                                     const float *__restrict__ step, int64_t rows, int R,
-                                                     const int32_t *__restrict__ values, int64_t n, float beta,
-                                                     const int32_t *__restrict__ tokens, int T, const float *__restrict__ lm,
-                                                     float log_keep, float log_lambda, float *__restrict__ mix,
-                                                     float *__restrict__ knn)
+template <typename D, int THREADS>
+__global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict__ ids, const D *__restrict__ dist,
+                                                      const float *__restrict__ step, int64_t rows, int R,
+                                                      const int32_t *__restrict__ values, int64_t n, float beta,
+                                                      const int32_t *__restrict__ tokens, int T, int tokens_at_once,
+                                                      const float *__restrict__ lm, float log_keep, float log_lambda,
+                                                      float *__restrict__ mix, float *__restrict__ knn)
 {
-    __shared__ float lds[MIX_WG / WAVE];
-    __shared__ int value[QADC_MAX_R];
-    __shared__ float vs[QADC_MAX_R];
+    constexpr int MINE = QADC_MAX_R / THREADS < 4 ? QADC_MAX_R / THREADS : 4;  // neighbours a thread, THREADS apart
+    __shared__ float lds[2][THREADS / WAVE];
+    __shared__ int2 votes[THREADS * MINE];  // (token, exp v)
+    __shared__ float far[THREADS * MINE];   // v
+    __shared__ float2 sums[THREADS];        // of a part: (sum of exp v, 1 if there is a vote)
+    const int t_mine = threadIdx.x % tokens_at_once, part = threadIdx.x / tokens_at_once, parts = THREADS / tokens_at_once;
+    const int padded = (R + 7) / 8 * 8;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const float b = step ? beta * step[r] : beta;
+        int tok = t_mine < T ? tokens[r * T + t_mine] : -1;  // on their way with the neighbours
+        float l = t_mine < T ? lm[r * T + t_mine] : 0.0f;
+        uint32_t id[MINE];
+        float d[MINE];
+        int val[MINE];
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int at = i * THREADS + threadIdx.x;
+            id[i] = at < R ? ids[r * R + at] : 0xFFFFFFFFu;
+            d[i] = at < R ? (float)dist[r * R + at] : INFINITY;
+        }
         float near = INFINITY;
-        __syncthreads();
-        for (int i = threadIdx.x; i < R; i += MIX_WG) {
-            const uint32_t id = ids[r * R + i];
-            const float d = (float)dist[r * R + i];
-            const bool used = (int64_t)id < n && fabsf(d) < INFINITY;
-            value[i] = used ? values[id] : -1;
-            vs[i] = used ? d : INFINITY;
-            near = fminf(near, vs[i]);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const bool used = (int64_t)id[i] < n && fabsf(d[i]) < INFINITY;
+            val[i] = used ? values[id[i]] : -1;
+            d[i] = used ? d[i] : INFINITY;
+            near = fminf(near, d[i]);
         }
-        near = group_join(near, lds, [](float p, float q) { return fminf(p, q); });
-        float z = 0.0f;
-        for (int i = threadIdx.x; i < R; i += MIX_WG) {
-            vs[i] = vs[i] < INFINITY ? -b * (vs[i] - near) : -INFINITY;
-            z += expf(vs[i]);
-        }
-        const float log_z = logf(group_join(z, lds, [](float p, float q) { return p + q; }));
+        near = group_join<THREADS>(-wave_max(-near), lds[0], [](float p, float q) { return fminf(p, q); });
         const bool any = near < INFINITY;
-        for (int t = threadIdx.x; t < T; t += MIX_WG) {
-            const int tok = tokens[r * T + t];
-            float a = -INFINITY, s = 0.0f;
-            for (int i = 0; i < R; ++i)
-                if (value[i] == tok) a = fmaxf(a, vs[i]);
-            if (a > -INFINITY)
-                for (int i = 0; i < R; ++i)
-                    if (value[i] == tok) s += expf(vs[i] - a);
-            const float log_p = a > -INFINITY ? a + logf(s) - log_z : -INFINITY;
-            const float l = lm[r * T + t];
-            const float out = !any ? l : log_add(l + log_keep, log_p + log_lambda);
-            mix[r * T + t] = tok >= 0 ? out : 0.0f;
-            if (knn) knn[r * T + t] = tok >= 0 ? log_p : 0.0f;
+        float z = 0.0f;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int at = i * THREADS + threadIdx.x;
+            const float v = d[i] < INFINITY ? -b * (d[i] - near) : -INFINITY, e = expf(v);
+            z += e;
+            if (at < padded) {
+                votes[at] = make_int2(val[i], __float_as_int(e));
+                far[at] = v;
+            }
+        }
+        const float log_z = logf(group_join<THREADS>(wave_sum(z), lds[1], [](float p, float q) { return p + q; }));
+        if constexpr (THREADS == WAVE) __syncthreads();
+        for (int t0 = 0; t0 < T; t0 += tokens_at_once) {
+            const int t = t0 + t_mine;
+            if (t0) {
+                tok = t < T ? tokens[r * T + t] : -1;
+                l = t < T ? lm[r * T + t] : 0.0f;
+            }
+            float s[2] = {0.0f, 0.0f};
+            bool vote = false;
+#pragma unroll 4
+            for (int i = 2 * part; i < padded; i += 2 * parts) {
+                const int4 two = *reinterpret_cast<const int4 *>(&votes[i]);
+                s[0] += two.x == tok ? __int_as_float(two.y) : 0.0f;
+                s[1] += two.z == tok ? __int_as_float(two.w) : 0.0f;
+                vote |= two.x == tok || two.z == tok;
+            }
+            sums[threadIdx.x] = make_float2(s[0] + s[1], vote ? 1.0f : 0.0f);
+            __syncthreads();
+            if (part == 0 && t < T) {
+                float sum = 0.0f, votes_of = 0.0f;
+                for (int p = 0; p < parts; ++p) {
+                    const float2 v = sums[p * tokens_at_once + t_mine];
+                    sum += v.x;
+                    votes_of += v.y;
+                }
+                float log_p = -INFINITY;
+                if (votes_of > 0.0f && any && tok >= 0) {
+                    log_p = logf(sum) - log_z;
+                    if (sum < 1e-30f) {
+                        float a = -INFINITY, own = 0.0f;
+                        for (int i = 0; i < R; ++i) a = fmaxf(a, votes[i].x == tok ? far[i] : -INFINITY);
+                        for (int i = 0; i < R; ++i) own += votes[i].x == tok ? expf(far[i] - a) : 0.0f;
+                        log_p = a == -INFINITY ? a : a + logf(own) - log_z;
+                    }
+                }
+                const float out = !any ? l : log_add(l + log_keep, log_p + log_lambda);
+                mix[r * T + t] = tok >= 0 ? out : 0.0f;
+                if (knn) knn[r * T + t] = tok >= 0 ? log_p : 0.0f;
+            }
+            __syncthreads();
         }
     }
 }
@@ -99,12 +146,21 @@ int neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const f
         return fail(QADC_EINVAL, "qadc_neighbour_mix: null pointer");
     const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
     const float log_keep = log1pf(-lambda), log_lambda = logf(lambda);
-    if (dist_bytes == 1)
-        launch(QADC_PROF_MIX, mix_kernel<uint8_t>, grid, dim3(MIX_WG), 0, st, ids, (const uint8_t *)dist, step, rows, R, values, n,
-               beta, tokens, T, lm_logp, log_keep, log_lambda, mix, knn);
-    else
-        launch(QADC_PROF_MIX, mix_kernel<float>, grid, dim3(MIX_WG), 0, st, ids, (const float *)dist, step, rows, R, values, n,
-               beta, tokens, T, lm_logp, log_keep, log_lambda, mix, knn);
+    // Rows of few neighbours and tokens have a wavefront each, where there are enough of them.
+    const int threads = R <= 256 && T <= 64 && rows >= 2048 ? WAVE : 256;
+    int at_once = 1;
+    while (at_once < T && at_once < threads) at_once *= 2;
+#define MIX(D_, THREADS_)                                                                                                       \
+    launch(QADC_PROF_MIX, mix_kernel<D_, THREADS_>, grid, dim3(THREADS_), 0, st, ids, (const D_ *)dist, step, rows, R, values, n, \
+           beta, tokens, T, at_once, lm_logp, log_keep, log_lambda, mix, knn)
+    if (threads == WAVE) {
+        if (dist_bytes == 1) MIX(uint8_t, WAVE);
+        else MIX(float, WAVE);
+    } else {
+        if (dist_bytes == 1) MIX(uint8_t, 256);
+        else MIX(float, 256);
+    }
+#undef MIX
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }
