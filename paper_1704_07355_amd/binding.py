@@ -181,6 +181,9 @@ def _ptr(t, dtype=None):
 
 
 def _stream():
+    # the current device's current stream; the raw handle where torch gives it (the Stream object costs 2.7 us a call)
+    if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -644,10 +647,10 @@ def _buffer(t, shape, dtype, device):
     return t
 
 
-def _scratch(workspace, need, device):
-    """The caller's workspace, or a new one of `need` bytes (not cleared); its size in bytes."""
+def _scratch(workspace, need, sizes, device):
+    """The caller's workspace, or a new one of need(*sizes) bytes (not cleared); its size in bytes."""
     if workspace is None:
-        workspace = torch.empty((max(need, 256),), dtype=torch.uint8, device=device)
+        workspace = torch.empty((max(need(*sizes), 256),), dtype=torch.uint8, device=device)
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -657,8 +660,7 @@ def qadc_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     rows, d = x.shape
     xp, ldx = _matrix(x)
     y = _buffer(out, (rows, d), x.dtype, x.device)
-    mean = torch.empty((rows,), dtype=torch.float32, device=x.device)
-    rstd = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
     _check(lib().qadc_layer_norm(xp, ldx, _type(x), _vector(weight, d), _vector(bias, d), _weight_type(weight, bias, x),
                                  rows, d, eps, _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
     return y, mean, rstd
@@ -680,9 +682,8 @@ def qadc_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None, out=None
     dw = db = None
     size = 0
     if need_weights:
-        dw = torch.empty((d,), dtype=torch.float32, device=x.device)
-        db = torch.empty((d,), dtype=torch.float32, device=x.device)
-        workspace, size = _scratch(workspace, qadc_layer_norm_workspace_bytes(rows, d), x.device)
+        dw, db = torch.empty((2, d), dtype=torch.float32, device=x.device).unbind(0)
+        workspace, size = _scratch(workspace, qadc_layer_norm_workspace_bytes, (rows, d), x.device)
     else:
         workspace = None
     _check(lib().qadc_layer_norm_backward(dyp, lddy, xp, ldx, _type(x), _vector(weight, d), _weight_type(weight, None, x),
@@ -748,15 +749,13 @@ def qadc_token_logprobs(logits, tokens=None, k=0, scale=1.0, workspace=None):
     xp, ld = _matrix(logits)
     tp, T = _tokens(tokens, rows)
     dev = logits.device
-    f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
-    logp, lse, entropy, top_logp = f32(rows, T), f32(rows), f32(rows), f32(rows, k)
+    lse, entropy = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    logp = torch.empty((rows, T), dtype=torch.float32, device=dev)
+    top_logp = torch.empty((rows, k), dtype=torch.float32, device=dev)
     top_idx = torch.empty((rows, k), dtype=torch.int32, device=dev)
-    if workspace is None:
-        need = qadc_token_logprobs_workspace_bytes(rows, V, k)
-        workspace = qadc_workspace_init(torch.empty((max(need, 256),), dtype=torch.uint8, device=dev))
+    workspace, size = _scratch(workspace, qadc_token_logprobs_workspace_bytes, (rows, V, k), dev)
     _check(lib().qadc_token_logprobs(xp, ld, _type(logits), rows, V, scale, tp, T, k, _ptr(logp), _ptr(lse), _ptr(entropy),
-                                     _ptr(top_idx), _ptr(top_logp), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(), _stream()))
+                                     _ptr(top_idx), _ptr(top_logp), _ptr(workspace), size, _stream()))
     return logp, lse, entropy, top_idx, top_logp
 
 
@@ -790,8 +789,7 @@ def qadc_neighbour_mix(ids, dist, values, tokens, lm_logp, lam, beta, step=None)
     if tokens is None or tuple(lm_logp.shape) != tuple(tokens.shape):
         raise ValueError("lm_logp must have the shape of tokens")
     tp, T = _tokens(tokens, rows)
-    mix = torch.empty((rows, T), dtype=torch.float32, device=ids.device)
-    knn = torch.empty((rows, T), dtype=torch.float32, device=ids.device)
+    mix, knn = torch.empty((2, rows, T), dtype=torch.float32, device=ids.device).unbind(0)
     _check(lib().qadc_neighbour_mix(_ptr(ids), _ptr(dist), dist.element_size(), _vector(step, rows, torch.float32), rows, R,
                                     _ptr(values, torch.int32), values.numel(), beta, tp, T, _ptr(lm_logp, torch.float32), lam,
                                     _ptr(mix), _ptr(knn), _stream()))

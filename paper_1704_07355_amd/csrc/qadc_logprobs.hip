@@ -185,11 +185,15 @@ __device__ __forceinline__ uint32_t group_count(uint32_t c, AltLds &lds, int tur
     return total;
 }
 
-// f(chunk, its block's largest logit) for every block of this thread, eight in flight.
+constexpr int LP_FIRST = 16;  // blocks of a thread whose largest logits it has in registers once a row is joined
+
+// f(chunk, its block's largest logit) for every block of this thread; beyond the first, eight in flight.
 template <typename F, typename G>
-__device__ __forceinline__ void each_top(int64_t chunks, F top_of, G f)
+__device__ __forceinline__ void each_top(int64_t chunks, const uint32_t (&first)[LP_FIRST], F top_of, G f)
 {
-    for (int64_t j = 0; j < chunks; j += 8) {
+#pragma unroll
+    for (int j = 0; j < LP_FIRST; ++j) f((int64_t)j, first[j]);  // (0 where there is no block)
+    for (int64_t j = LP_FIRST; j < chunks; j += 8) {
         uint32_t t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = j + i < chunks ? top_of(j + i) : 0u;
@@ -197,30 +201,36 @@ __device__ __forceinline__ void each_top(int64_t chunks, F top_of, G f)
         for (int i = 0; i < 8; ++i) f(j + i, t[i]);
     }
 }
+template <typename F>
+__device__ __forceinline__ void load_first(int64_t chunks, F top_of, uint32_t (&first)[LP_FIRST])
+{
+#pragma unroll
+    for (int j = 0; j < LP_FIRST; ++j) first[j] = j < chunks ? top_of(j) : 0u;
+}
 
 // The k alternatives of a row; top_of(chunk) is the largest logit of this thread's block.
 template <typename T, typename F>
 __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, float scale, float lse, bool none,
-                                   uint32_t *top_idx, float *top_logp, AltLds &lds, F top_of)
+                                   uint32_t *top_idx, float *top_logp, AltLds &lds, const uint32_t (&first)[LP_FIRST], F top_of)
 {
     constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
     uint32_t top = 0;
-    each_top(chunks, top_of, [&](int64_t, uint32_t t) { top = max(top, t); });
+    each_top(chunks, first, top_of, [&](int64_t, uint32_t t) { top = max(top, t); });
     if (threadIdx.x == 0) {
         lds.count = 0;
         lds.block_count = 0;
-        lds.bound = 0;
+        lds.bound = ~0u;
     }
     lds.tops[threadIdx.x] = top;
     __syncthreads();
-    int above = 0, equal = 0;  // a thread whose largest logit is the k-th of the threads' knows it
-#pragma unroll 4
+    // The k-th largest of the threads' largest logits is the least that fewer than k of them exceed.
+    int above = 0;
+#pragma unroll 8
     for (int i = 0; i < LP_WG; i += 4) {
         const uint4 t = *reinterpret_cast<const uint4 *>(&lds.tops[i]);
         above += (t.x > top) + (t.y > top) + (t.z > top) + (t.w > top);
-        equal += (t.x == top) + (t.y == top) + (t.z == top) + (t.w == top);
     }
-    if (above < k && above + equal >= k) lds.bound = top;
+    if (above < k) atomicMin(&lds.bound, top);
     __syncthreads();
     uint32_t bound = lds.bound;  // 0 where fewer than k threads have a logit: all of the row are candidates
     // f(bits, token) for this thread's logits that reach `from`
@@ -244,7 +254,7 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
     // The blocks that reach the bound are listed, then read by all threads, a pack each.
     const uint32_t least = max(bound, 1u);
     if (top >= least)
-        each_top(chunks, top_of, [&](int64_t j, uint32_t t) {
+        each_top(chunks, first, top_of, [&](int64_t j, uint32_t t) {
             if (t < least) return;
             const uint32_t slot = atomicAdd(&lds.block_count, 1u);
             if (slot < LP_READ) lds.blocks[slot] = (uint32_t)j * LP_WG + threadIdx.x;
@@ -339,10 +349,25 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
     __syncthreads();
 }
 
+// A row's first given tokens, one a thread, and their logits.
+struct Given {
+    int token;
+    float logit;
+};
+template <typename T>
+__device__ __forceinline__ Given given(const T *row, int64_t r, int V, const Out &o, int t)
+{
+    Given g = {-1, 0.0f};
+    if (t < o.nt) g.token = o.tokens[r * o.nt + t];
+    if (g.token >= V) g.token = -1;
+    if (g.token >= 0) g.logit = (float)row[g.token];
+    return g;
+}
+
 // What follows once a row's statistics are known.
 template <typename T, bool ALT, typename L, typename F>
 __device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_t chunks, Stats a, float scale, const Out &o,
-                                          L &lds, F top_of)
+                                          Given g, L &lds, const uint32_t (&first)[LP_FIRST], F top_of)
 {
     const bool none = a.m == -INFINITY && a.s == 0.0f;  // a mask has left nothing
     const float log_s = logf(a.s), lse = none ? -INFINITY : fmaf(scale, a.m, log_s);
@@ -351,12 +376,11 @@ __device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_
         if (o.entropy) o.entropy[r] = none ? 0.0f : log_s - LN2 * a.w / a.s;
     }
     for (int t = threadIdx.x; t < o.nt; t += LP_WG) {
-        const int tok = o.tokens[r * o.nt + t];
-        float v = 0.0f;
-        if (tok >= 0 && tok < V) v = none ? -INFINITY : scale * (float)row[tok] - lse;
-        o.logp[r * o.nt + t] = v;
+        if (t >= LP_WG) g = given(row, r, V, o, t);
+        o.logp[r * o.nt + t] = g.token < 0 ? 0.0f : none ? -INFINITY : scale * g.logit - lse;
     }
-    if constexpr (ALT) write_alternatives(row, V, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds, top_of);
+    if constexpr (ALT)
+        write_alternatives(row, V, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds, first, top_of);
 }
 
 // A workgroup per row.
@@ -371,6 +395,7 @@ __global__ __launch_bounds__(LP_WG) void logprobs_row_kernel(const T *__restrict
     const int64_t chunks = (V + LP_CHUNK - 1) / LP_CHUNK;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ld;
+        const Given g = given(row, r, V, o, threadIdx.x);
         Stats a = {-INFINITY, 0.0f, 0.0f};
         for (int64_t j = 0; j < chunks; ++j) {
             float x[LP_BLOCK], top;
@@ -378,12 +403,17 @@ __global__ __launch_bounds__(LP_WG) void logprobs_row_kernel(const T *__restrict
             const bool odd = add_block(a, x, c, &top);
             if constexpr (ALT) tops[j * LP_WG + threadIdx.x] = block_top(row, j, V, top, odd);
         }
+        const auto top_of = [&](int64_t j) { return tops[j * LP_WG + threadIdx.x]; };
+        uint32_t first[LP_FIRST] = {};
+        if constexpr (ALT) load_first(chunks, top_of, first);
         a = group_stats(a, c, stats);
-        write_row<T, ALT>(row, r, V, chunks, a, scale, o, alt, [&](int64_t j) { return tops[j * LP_WG + threadIdx.x]; });
+        write_row<T, ALT>(row, r, V, chunks, a, scale, o, g, alt, first, top_of);
     }
 }
 
-// A workgroup per `per` chunks of a row: their statistics and their blocks' largest logits into the workspace.
+// A workgroup per `per` chunks of a row: their statistics and their blocks' largest logits into the workspace.  The rows are
+// joined by a kernel of its own: joining in the last workgroup of a row to finish takes a fence over the GPU's caches in every
+// one of them, which costs as much as the launch for one row (15.5 us against 15) and three times as much for 64 (60 against 20).
 template <typename T, bool ALT>
 __global__ __launch_bounds__(LP_WG) void logprobs_part_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
                                                               float scale, int64_t chunks, int parts, int per,
@@ -416,11 +446,15 @@ __global__ __launch_bounds__(LP_WG) void logprobs_join_kernel(const T *__restric
     __shared__ std::conditional_t<ALT, AltLds, NoLds> alt;
     const float c = scale * LOG2E;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const T *row = logits + r * ld;
+        const Given g = given(row, r, V, o, threadIdx.x);
+        const auto top_of = [&](int64_t j) { return tops[(r * chunks + j) * LP_WG + threadIdx.x]; };
+        uint32_t first[LP_FIRST] = {};
+        if constexpr (ALT) load_first(chunks, top_of, first);
         Stats a = {-INFINITY, 0.0f, 0.0f};
         for (int p = threadIdx.x; p < parts; p += LP_WG) a = join(a, stats[r * parts + p], c);
         a = group_stats(a, c, lds);
-        write_row<T, ALT>(logits + r * ld, r, V, chunks, a, scale, o, alt,
-                          [&](int64_t j) { return tops[(r * chunks + j) * LP_WG + threadIdx.x]; });
+        write_row<T, ALT>(row, r, V, chunks, a, scale, o, g, alt, first, top_of);
     }
 }
 
@@ -529,7 +563,7 @@ int check_logits(const char *who, int type, int64_t ld, int64_t rows, int V, flo
 struct Plan {
     int64_t chunks;
     int parts, per;  // workgroups a row, chunks each; parts = 1: one kernel and no workspace
-    size_t tops, bytes;
+    size_t tops, bytes;  // in the workspace: [rows][parts] statistics, [rows][chunks][LP_WG] largest logits
 };
 
 static Plan plan_logprobs(int64_t rows, int V, int k)
@@ -543,8 +577,12 @@ static Plan plan_logprobs(int64_t rows, int V, int k)
         p.per = (int)ceil_div(p.chunks, 2);
         p.parts = 2;
     }
-    p.tops = p.parts == 1 ? 0 : align_up((size_t)rows * p.parts * sizeof(Stats), 256);
-    p.bytes = p.parts == 1 ? 256 : p.tops + (k > 0 ? (size_t)rows * p.chunks * LP_WG * sizeof(uint32_t) : 0);
+    p.tops = 0;
+    p.bytes = 256;
+    if (p.parts > 1) {
+        p.tops = align_up((size_t)rows * p.parts * sizeof(Stats), 256);
+        p.bytes = p.tops + (k > 0 ? (size_t)rows * p.chunks * LP_WG * sizeof(uint32_t) : 0);
+    }
     return p;
 }
 
