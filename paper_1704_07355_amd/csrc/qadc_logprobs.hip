@@ -22,9 +22,9 @@ namespace {
 constexpr int LP_WG = 256;
 constexpr int LP_BLOCK = 32;                  // logits of a thread whose largest is kept
 constexpr int LP_CHUNK = LP_WG * LP_BLOCK;    // logits of a workgroup at a time
-constexpr int LP_LDS_BLOCKS = 24 * LP_WG;     // blocks of a row whose largest logits fit in LDS beside the list: 196608 logits
-constexpr int LP_LIST = 3072;                 // candidates for the alternatives
-constexpr int LP_READ = 1024;                 // blocks that are read again by all threads together
+constexpr int LP_LDS_BLOCKS = 48 * LP_WG;     // blocks of a row whose largest logits fit in LDS: 393216 logits
+constexpr int LP_LIST = 1024;                 // candidates for the alternatives
+constexpr int LP_READ = 512;                  // blocks that are read again by all threads together
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
@@ -91,45 +91,64 @@ __device__ __forceinline__ bool add_block(Stats &st, const float (&x)[LP_BLOCK],
     return sum != sum;
 }
 
-// The logits of block (chunk, thread): LP_BLOCK / N packs, those of a wavefront side by side.
+// The logits of block (chunk, thread): LP_BLOCK / N packs, those of a wavefront side by side.  Packs lie at multiples of 16
+// bytes in memory: a row that does not begin at one has its first pack begin `lead` logits before it (packs across those
+// multiples took a quarter longer: 4096 rows of 50021 bfloat16 logits 92 us, their gradient 199).
 template <typename T>
-__device__ __forceinline__ int64_t pack_at(int64_t chunk, int u)
+__device__ __forceinline__ int lead_of(const T *row)
 {
-    return chunk * LP_CHUNK + ((int64_t)u * LP_WG + threadIdx.x) * Pack<T>::N;
+    return (int)((uintptr_t)row % 16 / sizeof(T));
 }
 template <typename T>
-__device__ __forceinline__ void load_block(const T *row, int64_t chunk, int V, float (&x)[LP_BLOCK])
+__device__ __forceinline__ int64_t pack_at(int64_t chunk, int u, int lead)
+{
+    return chunk * LP_CHUNK + ((int64_t)u * LP_WG + threadIdx.x) * Pack<T>::N - lead;
+}
+// A pack that may begin before the row or end behind it; `fill` there.
+template <typename T>
+__device__ __forceinline__ typename Pack<T>::V load_edge(const T *row, int64_t at, int64_t V, float fill)
 {
     constexpr int N = Pack<T>::N;
-    if ((chunk + 1) * LP_CHUNK <= V) {  // (the same in all threads: the loads follow each other without a wait)
+    if (at >= 0 && at + N <= V) return *reinterpret_cast<const typename Pack<T>::V *>(row + at);
+    typename Pack<T>::V p = (T)fill;
+    if (at < V) {
 #pragma unroll
-        for (int u = 0; u < LP_BLOCK / N; ++u) {
-            const typename Pack<T>::V p = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(chunk, u));
+        for (int e = 0; e < N; ++e)
+            if (at + e >= 0 && at + e < V) p[e] = row[at + e];
+    }
+    return p;
+}
+__device__ __forceinline__ int64_t chunks_of(int64_t V, int lead) { return (V + lead + LP_CHUNK - 1) / LP_CHUNK; }
+template <typename T>
+__device__ __forceinline__ void load_block(const T *row, int64_t chunk, int V, int lead, float (&x)[LP_BLOCK])
+{
+    constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
+    typename Pack<T>::V p[PACKS];
+    if ((chunk > 0 || lead == 0) && (chunk + 1) * LP_CHUNK - lead <= V) {  // (the same in all threads: loads without a wait)
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[u * N + e] = (float)p[e];
-        }
-        return;
+        for (int u = 0; u < PACKS; ++u)
+            p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(chunk, u, lead));
+    } else {
+#pragma unroll
+        for (int u = 0; u < PACKS; ++u) p[u] = load_edge(row, pack_at<T>(chunk, u, lead), V, -INFINITY);
     }
 #pragma unroll
-    for (int u = 0; u < LP_BLOCK / N; ++u) {
-        float v[N];
-        load_pack(row, pack_at<T>(chunk, u), V, -INFINITY, v);
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[u * N + e] = v[e];
-    }
+    for (int i = 0; i < LP_BLOCK; ++i) x[i] = (float)p[i / N][i % N];
 }
 
 // A block's largest logit in the order of the alternatives (0: it has none), where `v` is the largest that is no NaN.
 template <typename T>
-__device__ __forceinline__ uint32_t block_top(const T *row, int64_t chunk, int V, float v, bool odd)
+__device__ __forceinline__ uint32_t block_top(const T *row, int64_t chunk, int V, int lead, float v, bool odd)
 {
-    uint32_t bits = pack_at<T>(chunk, 0) < V ? logit_bits(v) : 0u;
+    uint32_t bits = pack_at<T>(chunk, 0, lead) < V ? logit_bits(v) : 0u;  // (a pack before the row ends in it)
     if (odd)
 #pragma unroll 1
         for (int u = 0; u < LP_BLOCK / Pack<T>::N; ++u)
 #pragma unroll 1
-            for (int64_t at = pack_at<T>(chunk, u), e = 0; e < Pack<T>::N && at + e < V; ++e)
-                bits = max(bits, logit_bits((float)row[at + e]));
+            for (int e = 0; e < Pack<T>::N; ++e) {
+                const int64_t at = pack_at<T>(chunk, u, lead) + e;
+                if (at >= 0 && at < V) bits = max(bits, logit_bits((float)row[at]));
+            }
     return bits;
 }
 
@@ -185,15 +204,14 @@ __device__ __forceinline__ uint32_t group_count(uint32_t c, AltLds &lds, int tur
     return total;
 }
 
-constexpr int LP_FIRST = 16;  // blocks of a thread whose largest logits it has in registers once a row is joined
-
-// f(chunk, its block's largest logit) for every block of this thread; beyond the first, eight in flight.
-template <typename F, typename G>
-__device__ __forceinline__ void each_top(int64_t chunks, const uint32_t (&first)[LP_FIRST], F top_of, G f)
+// f(chunk, its block's largest logit) for every block of this thread, the first FIRST of which it has in registers; beyond them
+// eight in flight.
+template <int FIRST, typename F, typename G>
+__device__ __forceinline__ void each_top(int64_t chunks, const uint32_t (&first)[FIRST + 1], F top_of, G f)
 {
 #pragma unroll
-    for (int j = 0; j < LP_FIRST; ++j) f((int64_t)j, first[j]);  // (0 where there is no block)
-    for (int64_t j = LP_FIRST; j < chunks; j += 8) {
+    for (int j = 0; j < FIRST; ++j) f((int64_t)j, first[j]);  // (0 where there is no block)
+    for (int64_t j = FIRST; j < chunks; j += 8) {
         uint32_t t[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) t[i] = j + i < chunks ? top_of(j + i) : 0u;
@@ -201,21 +219,14 @@ __device__ __forceinline__ void each_top(int64_t chunks, const uint32_t (&first)
         for (int i = 0; i < 8; ++i) f(j + i, t[i]);
     }
 }
-template <typename F>
-__device__ __forceinline__ void load_first(int64_t chunks, F top_of, uint32_t (&first)[LP_FIRST])
-{
-#pragma unroll
-    for (int j = 0; j < LP_FIRST; ++j) first[j] = j < chunks ? top_of(j) : 0u;
-}
-
 // The k alternatives of a row; top_of(chunk) is the largest logit of this thread's block.
-template <typename T, typename F>
-__device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, float scale, float lse, bool none,
-                                   uint32_t *top_idx, float *top_logp, AltLds &lds, const uint32_t (&first)[LP_FIRST], F top_of)
+template <int FIRST, typename T, typename F>
+__device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks, int k, float scale, float lse, bool none,
+                                   uint32_t *top_idx, float *top_logp, AltLds &lds, const uint32_t (&first)[FIRST + 1], F top_of)
 {
     constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
     uint32_t top = 0;
-    each_top(chunks, first, top_of, [&](int64_t, uint32_t t) { top = max(top, t); });
+    each_top<FIRST>(chunks, first, top_of, [&](int64_t, uint32_t t) { top = max(top, t); });
     if (threadIdx.x == 0) {
         lds.count = 0;
         lds.block_count = 0;
@@ -239,8 +250,9 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
         for (int64_t j = 0; j < chunks; ++j) {
             if (top_of(j) < from) continue;
             for (int u = 0; u < PACKS; ++u) {
-                const int64_t at = pack_at<T>(j, u);
-                for (int e = 0; e < N && at + e < V; ++e) {
+                const int64_t at = pack_at<T>(j, u, lead);
+                for (int e = 0; e < N; ++e) {
+                    if (at + e < 0 || at + e >= V) continue;
                     const uint32_t bits = logit_bits((float)row[at + e]);
                     if (bits >= from) f(bits, (uint32_t)(at + e));
                 }
@@ -254,7 +266,7 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
     // The blocks that reach the bound are listed, then read by all threads, a pack each.
     const uint32_t least = max(bound, 1u);
     if (top >= least)
-        each_top(chunks, first, top_of, [&](int64_t j, uint32_t t) {
+        each_top<FIRST>(chunks, first, top_of, [&](int64_t j, uint32_t t) {
             if (t < least) return;
             const uint32_t slot = atomicAdd(&lds.block_count, 1u);
             if (slot < LP_READ) lds.blocks[slot] = (uint32_t)j * LP_WG + threadIdx.x;
@@ -264,13 +276,12 @@ __device__ void write_alternatives(const T *row, int V, int64_t chunks, int k, f
     if (blocks <= LP_READ) {
         for (uint32_t i = threadIdx.x; i < blocks * PACKS; i += LP_WG) {
             const uint32_t block = lds.blocks[i / PACKS];
-            const int64_t at = (int64_t)(block / LP_WG) * LP_CHUNK + ((int64_t)(i % PACKS) * LP_WG + block % LP_WG) * N;
-            float x[N];
-            load_pack(row, at, V, 0.0f, x);
+            const int64_t at = (int64_t)(block / LP_WG) * LP_CHUNK + ((int64_t)(i % PACKS) * LP_WG + block % LP_WG) * N - lead;
+            const typename Pack<T>::V x = load_edge(row, at, V, 0.0f);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const uint32_t bits = logit_bits(x[e]);
-                if (bits >= least && at + e < V) collect(bits, (uint32_t)(at + e));
+                const uint32_t bits = logit_bits((float)x[e]);
+                if (bits >= least && at + e >= 0 && at + e < V) collect(bits, (uint32_t)(at + e));
             }
         }
     } else {
@@ -365,9 +376,9 @@ __device__ __forceinline__ Given given(const T *row, int64_t r, int V, const Out
 }
 
 // What follows once a row's statistics are known.
-template <typename T, bool ALT, typename L, typename F>
-__device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_t chunks, Stats a, float scale, const Out &o,
-                                          Given g, L &lds, const uint32_t (&first)[LP_FIRST], F top_of)
+template <typename T, bool ALT, int FIRST, typename L, typename F>
+__device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int lead, int64_t chunks, Stats a, float scale,
+                                          const Out &o, Given g, L &lds, const uint32_t (&first)[FIRST + 1], F top_of)
 {
     const bool none = a.m == -INFINITY && a.s == 0.0f;  // a mask has left nothing
     const float log_s = logf(a.s), lse = none ? -INFINITY : fmaf(scale, a.m, log_s);
@@ -380,7 +391,8 @@ __device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int64_
         o.logp[r * o.nt + t] = g.token < 0 ? 0.0f : none ? -INFINITY : scale * g.logit - lse;
     }
     if constexpr (ALT)
-        write_alternatives(row, V, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds, first, top_of);
+        write_alternatives<FIRST>(row, V, lead, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds,
+                                  first, top_of);
 }
 
 // A workgroup per row.
@@ -392,22 +404,22 @@ __global__ __launch_bounds__(LP_WG) void logprobs_row_kernel(const T *__restrict
     __shared__ std::conditional_t<ALT, AltLds, NoLds> alt;
     extern __shared__ uint32_t tops[];  // [chunks][LP_WG] where there are alternatives
     const float c = scale * LOG2E;
-    const int64_t chunks = (V + LP_CHUNK - 1) / LP_CHUNK;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ld;
+        const int lead = lead_of(row);
+        const int64_t chunks = chunks_of(V, lead);
         const Given g = given(row, r, V, o, threadIdx.x);
         Stats a = {-INFINITY, 0.0f, 0.0f};
         for (int64_t j = 0; j < chunks; ++j) {
             float x[LP_BLOCK], top;
-            load_block(row, j, V, x);
+            load_block(row, j, V, lead, x);
             const bool odd = add_block(a, x, c, &top);
-            if constexpr (ALT) tops[j * LP_WG + threadIdx.x] = block_top(row, j, V, top, odd);
+            if constexpr (ALT) tops[j * LP_WG + threadIdx.x] = block_top(row, j, V, lead, top, odd);
         }
-        const auto top_of = [&](int64_t j) { return tops[j * LP_WG + threadIdx.x]; };
-        uint32_t first[LP_FIRST] = {};
-        if constexpr (ALT) load_first(chunks, top_of, first);
         a = group_stats(a, c, stats);
-        write_row<T, ALT>(row, r, V, chunks, a, scale, o, g, alt, first, top_of);
+        const uint32_t first[1] = {};
+        write_row<T, ALT, 0>(row, r, V, lead, chunks, a, scale, o, g, alt, first,
+                             [&](int64_t j) { return tops[j * LP_WG + threadIdx.x]; });
     }
 }
 
@@ -416,7 +428,7 @@ __global__ __launch_bounds__(LP_WG) void logprobs_row_kernel(const T *__restrict
 // one of them, which costs as much as the launch for one row (15.5 us against 15) and three times as much for 64 (60 against 20).
 template <typename T, bool ALT>
 __global__ __launch_bounds__(LP_WG) void logprobs_part_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
-                                                              float scale, int64_t chunks, int parts, int per,
+                                                              float scale, int64_t stride, int parts, int per,
                                                               Stats *__restrict__ stats, uint32_t *__restrict__ tops)
 {
     __shared__ StatsLds lds;
@@ -424,12 +436,14 @@ __global__ __launch_bounds__(LP_WG) void logprobs_part_kernel(const T *__restric
     for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
         const int64_t r = i / parts, j0 = i % parts * per;
         const T *row = logits + r * ld;
+        const int lead = lead_of(row);
+        const int64_t j1 = min(j0 + per, chunks_of(V, lead));
         Stats a = {-INFINITY, 0.0f, 0.0f};
-        for (int64_t j = j0; j < min(j0 + per, chunks); ++j) {
+        for (int64_t j = j0; j < j1; ++j) {
             float x[LP_BLOCK], top;
-            load_block(row, j, V, x);
+            load_block(row, j, V, lead, x);
             const bool odd = add_block(a, x, c, &top);
-            if constexpr (ALT) tops[(r * chunks + j) * LP_WG + threadIdx.x] = block_top(row, j, V, top, odd);
+            if constexpr (ALT) tops[(r * stride + j) * LP_WG + threadIdx.x] = block_top(row, j, V, lead, top, odd);
         }
         a = group_stats(a, c, lds);
         if (threadIdx.x == 0) stats[i] = a;
@@ -438,7 +452,7 @@ __global__ __launch_bounds__(LP_WG) void logprobs_part_kernel(const T *__restric
 
 template <typename T, bool ALT>
 __global__ __launch_bounds__(LP_WG) void logprobs_join_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V,
-                                                              float scale, int64_t chunks, int parts,
+                                                              float scale, int64_t stride, int parts,
                                                               const Stats *__restrict__ stats,
                                                               const uint32_t *__restrict__ tops, Out o)
 {
@@ -447,14 +461,18 @@ __global__ __launch_bounds__(LP_WG) void logprobs_join_kernel(const T *__restric
     const float c = scale * LOG2E;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ld;
-        const Given g = given(row, r, V, o, threadIdx.x);
-        const auto top_of = [&](int64_t j) { return tops[(r * chunks + j) * LP_WG + threadIdx.x]; };
-        uint32_t first[LP_FIRST] = {};
-        if constexpr (ALT) load_first(chunks, top_of, first);
+        const int lead = lead_of(row);
+        const int64_t chunks = chunks_of(V, lead);
+        const auto top_of = [&](int64_t j) { return tops[(r * stride + j) * LP_WG + threadIdx.x]; };
+        constexpr int FIRST = ALT ? 16 : 0;
+        uint32_t first[FIRST + 1] = {};
+#pragma unroll
+        for (int j = 0; j < FIRST; ++j) first[j] = j < chunks ? top_of(j) : 0u;
         Stats a = {-INFINITY, 0.0f, 0.0f};
         for (int p = threadIdx.x; p < parts; p += LP_WG) a = join(a, stats[r * parts + p], c);
+        const Given g = given(row, r, V, o, threadIdx.x);
         a = group_stats(a, c, lds);
-        write_row<T, ALT>(row, r, V, chunks, a, scale, o, g, alt, first, top_of);
+        write_row<T, ALT, FIRST>(row, r, V, lead, chunks, a, scale, o, g, alt, first, top_of);
     }
 }
 
@@ -478,14 +496,17 @@ __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, i
                                                               const float *__restrict__ dlogp,
                                                               const float *__restrict__ dentropy, T *dlogits, int64_t ldd)
 {
-    constexpr int N = Pack<T>::N;
+    constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
     __shared__ float sums[LP_WG / WAVE];
     __shared__ int tok[QADC_MAX_R];
     __shared__ float at[QADC_MAX_R], dl[QADC_MAX_R];
     for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
-        const int64_t r = i / parts, v0 = i % parts * per * LP_CHUNK, v1 = min(v0 + (int64_t)per * LP_CHUNK, (int64_t)V);
+        const int64_t r = i / parts;
         const T *row = logits + r * ld;
         T *out = dlogits + r * ldd;
+        const int lead = lead_of(out);
+        const int64_t v0 = max((int64_t)0, i % parts * per * LP_CHUNK - lead);
+        const int64_t v1 = min((i % parts + 1) * per * LP_CHUNK - lead, (int64_t)V);
         const float l = lse[r], dh = dentropy ? dentropy[r] : 0.0f, h = dentropy ? entropy[r] : 0.0f;
         const bool none = l == -INFINITY;
         float total = 0.0f;
@@ -509,25 +530,34 @@ __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, i
             return p * -fmaf(dh, fmaxf(lp, -2000.0f) + h, total);  // (a masked logit: zero times something finite)
         };
         const auto value = [&](float logit) { return none ? 0.0f : scale * share(logit); };
-        for (int64_t c0 = v0; c0 < v1; c0 += LP_CHUNK) {
-            if (c0 + LP_CHUNK <= v1) {
-                typename Pack<T>::V p[LP_BLOCK / N];
+        for (int64_t j = i % parts * per; j < (i % parts + 1) * per && j * LP_CHUNK - lead < v1; ++j) {
+            typename Pack<T>::V p[PACKS];
+            if ((j > 0 || lead == 0) && (j + 1) * LP_CHUNK - lead <= v1) {
 #pragma unroll
-                for (int u = 0; u < LP_BLOCK / N; ++u)
-                    p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + c0 + ((int64_t)u * LP_WG + threadIdx.x) * N);
+                for (int u = 0; u < PACKS; ++u)
+                    p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(j, u, lead));
 #pragma unroll
-                for (int u = 0; u < LP_BLOCK / N; ++u) {
+                for (int u = 0; u < PACKS; ++u) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) p[u][e] = (T)value((float)p[u][e]);
-                    *reinterpret_cast<typename Pack<T>::V *>(out + c0 + ((int64_t)u * LP_WG + threadIdx.x) * N) = p[u];
+                    *reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead)) = p[u];
                 }
             } else {
-                for (int64_t c = c0 + threadIdx.x * N; c < v1; c += LP_WG * N) {
-                    float x[N];
-                    load_pack(row, c, v1, 0.0f, x);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) x[e] = value(x[e]);
-                    store_pack(out, c, v1, x);
+                for (int u = 0; u < PACKS; ++u) p[u] = load_edge(row, pack_at<T>(j, u, lead), v1, 0.0f);
+#pragma unroll
+                for (int u = 0; u < PACKS; ++u) {
+                    const int64_t at = pack_at<T>(j, u, lead);
+                    if (at >= v1) continue;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) p[u][e] = (T)value((float)p[u][e]);
+                    if (at >= 0 && at + N <= v1) {
+                        *reinterpret_cast<typename Pack<T>::V *>(out + at) = p[u];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (at + e >= 0 && at + e < v1) out[at + e] = p[u][e];
+                    }
                 }
             }
         }
@@ -569,7 +599,7 @@ struct Plan {
 static Plan plan_logprobs(int64_t rows, int V, int k)
 {
     Plan p;
-    p.chunks = ceil_div(V, LP_CHUNK);
+    p.chunks = ceil_div((int64_t)V + 7, LP_CHUNK);  // (a row begins up to seven logits into its first pack)
     const int64_t want = std::max<int64_t>(1, ceil_div(1024, rows));
     p.per = (int)ceil_div(p.chunks, std::min(p.chunks, want));
     p.parts = (int)ceil_div(p.chunks, p.per);
@@ -644,7 +674,7 @@ int token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t ro
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: null pointer");
     if (logits == dlogits && ld != ldd)
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: in place needs equal row distances");
-    const int64_t chunks = ceil_div(V, LP_CHUNK);
+    const int64_t chunks = ceil_div((int64_t)V + 7, LP_CHUNK);
     const int per = (int)std::min<int64_t>(chunks, std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048)));
     const int parts = (int)ceil_div(chunks, per);
     const dim3 grid((unsigned)std::min<int64_t>(rows * parts, 1 << 20));
