@@ -127,7 +127,7 @@ __device__ __forceinline__ void load_block(const T *row, int64_t chunk, int V, i
     if ((chunk > 0 || lead == 0) && (chunk + 1) * LP_CHUNK - lead <= V) {  // (the same in all threads: loads without a wait)
 #pragma unroll
         for (int u = 0; u < PACKS; ++u)
-            p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(chunk, u, lead));
+            p[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(chunk, u, lead)));
     } else {
 #pragma unroll
         for (int u = 0; u < PACKS; ++u) p[u] = load_edge(row, pack_at<T>(chunk, u, lead), V, -INFINITY);
@@ -488,8 +488,10 @@ __device__ __forceinline__ float exp_of(float t)
     return y > -3000.0f ? fmaf(p, rest * LN2, p) : p;  // (an infinite t: no infinity less infinity)
 }
 
-// A workgroup per `per` chunks of a row: first every logit's own share, then the given tokens', each once.
-template <typename T>
+// A workgroup per `per` chunks of a row: first every logit's own share, then the given tokens', each once.  STREAM: stores past
+// the caches, for gradients that they do not hold (4096 x 65536 bfloat16 208 -> 198 us, 4096 x 50021 190 -> 170; 500 x 131072,
+// which they hold, would go from 47 to 53).
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, int64_t ld, int64_t rows, int V, float scale,
                                                               int parts, int per, const int32_t *__restrict__ tokens, int nt,
                                                               const float *__restrict__ lse, const float *__restrict__ entropy,
@@ -535,12 +537,14 @@ __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, i
             if ((j > 0 || lead == 0) && (j + 1) * LP_CHUNK - lead <= v1) {
 #pragma unroll
                 for (int u = 0; u < PACKS; ++u)
-                    p[u] = *reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(j, u, lead));
+                    p[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(j, u, lead)));
 #pragma unroll
                 for (int u = 0; u < PACKS; ++u) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) p[u][e] = (T)value((float)p[u][e]);
-                    *reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead)) = p[u];
+                    auto *to = reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead));
+                    if constexpr (STREAM) __builtin_nontemporal_store(p[u], to);
+                    else *to = p[u];
                 }
             } else {
 #pragma unroll
@@ -679,8 +683,12 @@ int token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t ro
     const int parts = (int)ceil_div(chunks, per);
     const dim3 grid((unsigned)std::min<int64_t>(rows * parts, 1 << 20));
     const int nt = T;
-    QADC_BY_TYPE(type, (launch(QADC_PROF_LOGPROBS, logprobs_grad_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows,
-                               V, scale, parts, per, tokens, nt, lse, entropy, dlogp, dentropy, (T *)dlogits, ldd)));
+    const bool stream = (size_t)rows * V * type_bytes(type) > ((size_t)384 << 20);
+    QADC_BY_TYPE(type, {
+        const auto kernel = stream ? &logprobs_grad_kernel<T, true> : &logprobs_grad_kernel<T, false>;
+        launch(QADC_PROF_LOGPROBS, *kernel, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows, V, scale, parts, per, tokens, nt,
+               lse, entropy, dlogp, dentropy, (T *)dlogits, ldd);
+    });
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }

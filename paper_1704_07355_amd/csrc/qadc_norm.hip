@@ -56,10 +56,11 @@ struct Part {
 #pragma unroll
         for (int u = 0; u < P; ++u) {
             const int c = (u * G + t) * N;
-            if ((u + 1) * G * N <= d) {  // (the same in all threads)
-                raw[u] = *reinterpret_cast<const V *>(row + c);
-            } else if (c + N <= d) {
-                raw[u] = *reinterpret_cast<const V *>(row + c);
+            if ((u + 1) * G * N <= d || c + N <= d) {  // (the first is the same in all threads)
+                // Every row is read once: past the caches it comes faster (16384 x 4096 float32: forward 97 -> 81 us, backward
+                // 154 -> 131; bfloat16 backward 88 -> 82), but for rows so short that they share lines (200000 x 100: 20 -> 26).
+                const V *from = reinterpret_cast<const V *>(row + c);
+                raw[u] = G > 16 ? __builtin_nontemporal_load(from) : *from;
             } else {
 #pragma unroll
                 for (int e = 0; e < N; ++e) raw[u][e] = c + e < d ? row[c + e] : (T)0.0f;
