@@ -171,7 +171,7 @@ constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's
 // 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
 // others repeat them.  STEPS: instructions per group.
 template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
-__global__ __launch_bounds__(THREADS, MT == 4 ? 2 : 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
+__global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
 {
     constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
     constexpr bool HALF = Inputs<T>::HALF;
@@ -392,32 +392,51 @@ int pack_weights4(const uint8_t *codes, const void *scales, int stype, const uin
     return QADC_OK;
 }
 
-// LDS for x: two workgroups a compute unit, one where a float32 x takes three times the room.
-constexpr size_t x_lds(size_t type_bytes) { return type_bytes == 4 ? 156 << 10 : 78 << 10; }
+// As many wavefronts a block as the chip holds for these outputs, but no more than there are tiles or than a workgroup has.
+int split4(int64_t blocks, int64_t row_blocks, int tiles, int waves)
+{
+    int split = 1;
+    while (split < waves && blocks * row_blocks * split < 4096 && 2 * split <= tiles) split *= 2;
+    return split;
+}
 
+// A workgroup of 16 wavefronts has a compute unit and its LDS to itself, of 8 it shares them with another one.
 template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
 static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
 {
     constexpr int WAVES = THREADS / WAVE, PARTS = Inputs<T>::PARTS;
-    constexpr size_t sums = (size_t)WAVES * MT * NT * MR * WAVE * sizeof(float);
+    constexpr size_t room = THREADS == 1024 ? 156 << 10 : 78 << 10, sums = (size_t)WAVES * MT * NT * MR * WAVE * sizeof(float);
+    static_assert(sums <= room, "the wavefronts' sums fit where x was");
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
     const auto kernel = &linear4_kernel<T, STEPS, MR, MT, NT, THREADS>;
     std::call_once(once, [&] {  // more than the default limit of dynamic LDS
-        attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)std::max(x_lds(sizeof(T)), sums));
+        attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
     });
     QADC_HIP_TRY(attr);
-    // As many wavefronts a block as the chip holds for these outputs, but no more than there are tiles.
     const int64_t blocks = ceil_div(a.s.blocks, NT), row_blocks = ceil_div(a.M, 4 * MR * MT);
-    a.split = 1;
-    while (a.split < WAVES && blocks * row_blocks * a.split < 4096 && 2 * a.split <= a.s.tiles) a.split *= 2;
+    a.split = split4(blocks, row_blocks, a.s.tiles, WAVES);
     const size_t row_bytes = (size_t)std::min<int64_t>(4 * MR * MT, a.M) * PARTS * 2;
-    a.chunk = (int)std::min<size_t>(a.s.tiles, (x_lds(sizeof(T)) / row_bytes - X_PAD) / W4_K);
+    a.chunk = (int)std::min<size_t>(a.s.tiles, (room / row_bytes - X_PAD) / W4_K);
     const size_t shared = std::max(row_bytes * (a.chunk * W4_K + X_PAD), a.split > 1 ? sums : 0);
     launch(QADC_PROF_LINEAR4, *kernel, dim3((unsigned)ceil_div(blocks, WAVES / a.split), (unsigned)row_blocks), dim3(THREADS),
            shared, st, a, (const T *)x, (T *)y);
     return QADC_OK;
+}
+
+// Sixteen wavefronts a workgroup (131072 x 4096, bfloat16: one row 59 -> 54 us, 16 rows 68 -> 59; the large x of 32 rows of
+// 16384 inputs is brought in half as often: 82 -> 62), unless a last round of workgroups would leave much of the chip idle:
+// there eight (one row of 40000 x 8000 37 us against 47, 24 rows of 10007 x 5000 28 against 32).  A float32 x, in three parts,
+// needs the room (12 rows of 20000 x 2000: 22 us against 26).
+template <typename T, int STEPS, int MR, int MT>
+static int linear4_sized(const Args4 &a, const void *x, void *y, hipStream_t st)
+{
+    if constexpr (sizeof(T) == 2) {
+        const int64_t blocks = ceil_div(a.s.blocks, 2), row_blocks = ceil_div(a.M, 4 * MR * MT);
+        const int64_t wgs = ceil_div(blocks, 16 / split4(blocks, row_blocks, a.s.tiles, 16)) * row_blocks;
+        if (wgs > 256 && 5 * wgs < 4 * 256 * ceil_div(wgs, 256)) return linear4_launch<T, STEPS, MR, MT, 2, 512>(a, x, y, st);
+    }
+    return linear4_launch<T, STEPS, MR, MT, 2, 1024>(a, x, y, st);
 }
 
 template <typename T, int STEPS>
@@ -430,11 +449,10 @@ static int linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
         const T *xs = x + m * a.ldx;
         T *ys = y + m * a.ldy;
         int rc;
-        if (a.M <= 4) rc = a.s.blocks < 1024 ? linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st)
-                                             : linear4_launch<T, STEPS, 1, 1, 2, 512>(a, xs, ys, st);
-        else if (a.M <= 16) rc = linear4_launch<T, STEPS, 4, 1, 2, 512>(a, xs, ys, st);
-        else if (a.M <= 32 || sizeof(T) == 4) rc = linear4_launch<T, STEPS, 4, 2, 2, 512>(a, xs, ys, st);
-        else rc = linear4_launch<T, STEPS, 4, 4, 2, 512>(a, xs, ys, st);
+        if (a.M > 16) rc = linear4_sized<T, STEPS, 4, 2>(a, xs, ys, st);
+        else if (a.M > 4) rc = linear4_sized<T, STEPS, 4, 1>(a, xs, ys, st);
+        else if (a.s.blocks >= 1024) rc = linear4_sized<T, STEPS, 1, 1>(a, xs, ys, st);
+        else rc = linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st);  // few outputs: all wavefronts that they are worth
         if (rc != QADC_OK) return rc;
     }
     return QADC_OK;
