@@ -619,7 +619,7 @@ def _matrix(t, dtype=None):
     ld = t.stride(0) if rows > 1 else cols
     if not t.is_cuda or (cols > 1 and rows > 0 and t.stride(1) != 1) or ld < cols:
         raise ValueError("tensor must be a GPU matrix with dense rows that do not overlap")
-    return ctypes.c_void_p(t.data_ptr()), ld
+    return t.data_ptr(), ld
 
 
 def _vector(t, n, dtype=None):
@@ -628,23 +628,35 @@ def _vector(t, n, dtype=None):
         return None
     if t.numel() != n:
         raise ValueError(f"expected {n} elements, got {t.numel()}")
-    return _ptr(t, dtype)
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("tensor must be a contiguous GPU tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"expected {dtype}, got {t.dtype}")
+    return t.data_ptr()
 
 
 def _weight_type(weight, bias, x) -> int:
-    types = {t.dtype for t in (weight, bias) if t is not None}
-    if len(types) > 1 or not types <= {torch.float32, x.dtype}:
+    if weight is None:
+        weight, bias = bias, None
+    if weight is None:
+        return QADC_TYPE_F32
+    if (bias is not None and bias.dtype != weight.dtype) or weight.dtype not in (torch.float32, x.dtype):
         raise ValueError("weight and bias must both be float32, or both of x's type")
-    return _TYPES[types.pop()] if types else QADC_TYPE_F32
+    return _TYPES[weight.dtype]
 
 
-def _buffer(t, shape, dtype, device):
-    """The caller's output tensor, checked, or a new one."""
+def _like(t, x):
+    """The caller's dense output tensor, checked to be one like the matrix x, or a new one."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
-        raise ValueError(f"output must be {dtype} {tuple(shape)}")
+        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if t.shape != x.shape or t.dtype != x.dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"output must be a contiguous {x.dtype} GPU tensor of {tuple(x.shape)}")
     return t
+
+
+def _pair(shape, device):
+    """Two new float32 tensors of one allocation."""
+    return torch.empty((2, *shape), dtype=torch.float32, device=device).unbind(0)
 
 
 def _scratch(workspace, need, sizes, device):
@@ -659,10 +671,10 @@ def qadc_layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     -> (y [rows][d] of x's type, mean f32 [rows], rstd f32 [rows])."""
     rows, d = x.shape
     xp, ldx = _matrix(x)
-    y = _buffer(out, (rows, d), x.dtype, x.device)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    y = _like(out, x)
+    mean, rstd = _pair((rows,), x.device)
     _check(lib().qadc_layer_norm(xp, ldx, _type(x), _vector(weight, d), _vector(bias, d), _weight_type(weight, bias, x),
-                                 rows, d, eps, _ptr(y), _ptr(mean), _ptr(rstd), _stream()))
+                                 rows, d, eps, y.data_ptr(), mean.data_ptr(), rstd.data_ptr(), _stream()))
     return y, mean, rstd
 
 
@@ -678,11 +690,11 @@ def qadc_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None, out=None
         raise ValueError("dy must have x's shape")
     dyp, lddy = _matrix(dy, x.dtype)
     xp, ldx = _matrix(x)
-    dx = _buffer(out, (rows, d), x.dtype, x.device) if need_dx else None
+    dx = _like(out, x) if need_dx else None
     dw = db = None
     size = 0
     if need_weights:
-        dw, db = torch.empty((2, d), dtype=torch.float32, device=x.device).unbind(0)
+        dw, db = _pair((d,), x.device)
         workspace, size = _scratch(workspace, qadc_layer_norm_workspace_bytes, (rows, d), x.device)
     else:
         workspace = None
@@ -749,13 +761,14 @@ def qadc_token_logprobs(logits, tokens=None, k=0, scale=1.0, workspace=None):
     xp, ld = _matrix(logits)
     tp, T = _tokens(tokens, rows)
     dev = logits.device
-    lse, entropy = torch.empty((2, rows), dtype=torch.float32, device=dev).unbind(0)
+    lse, entropy = _pair((rows,), dev)
     logp = torch.empty((rows, T), dtype=torch.float32, device=dev)
     top_logp = torch.empty((rows, k), dtype=torch.float32, device=dev)
     top_idx = torch.empty((rows, k), dtype=torch.int32, device=dev)
     workspace, size = _scratch(workspace, qadc_token_logprobs_workspace_bytes, (rows, V, k), dev)
-    _check(lib().qadc_token_logprobs(xp, ld, _type(logits), rows, V, scale, tp, T, k, _ptr(logp), _ptr(lse), _ptr(entropy),
-                                     _ptr(top_idx), _ptr(top_logp), _ptr(workspace), size, _stream()))
+    _check(lib().qadc_token_logprobs(xp, ld, _type(logits), rows, V, scale, tp, T, k, logp.data_ptr(), lse.data_ptr(),
+                                     entropy.data_ptr(), top_idx.data_ptr(), top_logp.data_ptr(), _ptr(workspace), size,
+                                     _stream()))
     return logp, lse, entropy, top_idx, top_logp
 
 
@@ -789,8 +802,8 @@ def qadc_neighbour_mix(ids, dist, values, tokens, lm_logp, lam, beta, step=None)
     if tokens is None or tuple(lm_logp.shape) != tuple(tokens.shape):
         raise ValueError("lm_logp must have the shape of tokens")
     tp, T = _tokens(tokens, rows)
-    mix, knn = torch.empty((2, rows, T), dtype=torch.float32, device=ids.device).unbind(0)
+    mix, knn = _pair((rows, T), ids.device)
     _check(lib().qadc_neighbour_mix(_ptr(ids), _ptr(dist), dist.element_size(), _vector(step, rows, torch.float32), rows, R,
                                     _ptr(values, torch.int32), values.numel(), beta, tp, T, _ptr(lm_logp, torch.float32), lam,
-                                    _ptr(mix), _ptr(knn), _stream()))
+                                    mix.data_ptr(), knn.data_ptr(), _stream()))
     return mix, knn
