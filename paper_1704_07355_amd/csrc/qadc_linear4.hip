@@ -175,6 +175,7 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
 {
     constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
     constexpr bool HALF = Inputs<T>::HALF;
+    constexpr int FLY = sizeof(T) == 4 ? 2 : 4;
     constexpr int UNROLL = MT == 1 ? PER : 1;  // (groups side by side do not fit the registers of more rows)
     extern __shared__ float lds[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [PARTS][rows][chunk * W4_K + X_PAD]
@@ -234,16 +235,29 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
         first = end;
         end = min(first + a.chunk, tiles);
         const unsigned packs = (unsigned)(end - first) * (W4_K / 8), all = packs * (unsigned)rows;
+        const unsigned inverse = 0xffffffffu / packs + 1u;  // i / packs = i * inverse / 2^32: i * packs is far below 2^32
+        const bool whole = (int64_t)end * W4_K <= a.K;
         if (first) __syncthreads();  // (the chunk before has been read)
-        for (unsigned i = threadIdx.x; i < all; i += THREADS) {
-            const unsigned r = i / packs, c = i % packs * 8;
-            const int64_t k = (int64_t)first * W4_K + c;
-            const T *row = x + (m0 + r) * a.ldx;
-            const Inputs<T> in(k + 8 <= a.K ? *reinterpret_cast<const typename Inputs<T>::V *>(row + k)
-                                            : Inputs<T>::load_last(row, k, a.K));
+        // FLY packs a thread in flight; past the last one it is brought again
+        for (unsigned i = threadIdx.x; i < all; i += FLY * THREADS) {
+            typename Inputs<T>::V v[FLY];
+            unsigned to[FLY];
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-                *reinterpret_cast<bits16x8 *>(xs + ((unsigned)(p * rows) + r) * stride + c) = in.part[p];
+            for (int e = 0; e < FLY; ++e) {
+                const unsigned at = min(i + e * THREADS, all - 1), r = __umulhi(at, inverse), c = (at - r * packs) * 8;
+                const int64_t k = (int64_t)first * W4_K + c;
+                const T *row = x + (m0 + r) * a.ldx;
+                to[e] = r * stride + c;
+                if (whole || k + 8 <= a.K) v[e] = *reinterpret_cast<const typename Inputs<T>::V *>(row + k);
+                else v[e] = Inputs<T>::load_last(row, k, a.K);
+            }
+#pragma unroll
+            for (int e = 0; e < FLY; ++e) {
+                const Inputs<T> in(v[e]);
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+                    *reinterpret_cast<bits16x8 *>(xs + (unsigned)(p * rows) * stride + to[e]) = in.part[p];
+            }
         }
         __syncthreads();
     };
@@ -392,12 +406,22 @@ int pack_weights4(const uint8_t *codes, const void *scales, int stype, const uin
     return QADC_OK;
 }
 
-// As many wavefronts a block as the chip holds for these outputs, but no more than there are tiles or than a workgroup has.
-int split4(int64_t blocks, int64_t row_blocks, int tiles, int waves)
+// How a product is cut: wavefronts that share a block of outputs, and the cost of that in KB of weights that a compute unit could
+// have read meanwhile: those of the fullest one of the 256, and 128 KB for every round of workgroups (6 us from a workgroup's
+// first load to its last store at 21.5 GB/s a compute unit).
+struct Cut4 {
+    int split;
+    int64_t cost;
+};
+Cut4 cut4(int64_t blocks, int64_t row_blocks, int tiles, int nt, int waves)
 {
-    int split = 1;
-    while (split < waves && blocks * row_blocks * split < 4096 && 2 * split <= tiles) split *= 2;
-    return split;
+    Cut4 best = {1, INT64_MAX};
+    for (int split = 1; split <= waves && (split == 1 || split <= tiles); split *= 2) {
+        const int64_t at_once = waves / split, wgs = ceil_div(blocks, at_once) * row_blocks;
+        const int64_t cost = ceil_div(wgs, 256) * at_once * nt * tiles + 128 * ceil_div(wgs, 256 * (16 / waves));
+        if (cost <= best.cost) best = {split, cost};
+    }
+    return best;
 }
 
 // A workgroup of 16 wavefronts has a compute unit and its LDS to itself, of 8 it shares them with another one.
@@ -415,7 +439,7 @@ static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
     });
     QADC_HIP_TRY(attr);
     const int64_t blocks = ceil_div(a.s.blocks, NT), row_blocks = ceil_div(a.M, 4 * MR * MT);
-    a.split = split4(blocks, row_blocks, a.s.tiles, WAVES);
+    a.split = cut4(blocks, row_blocks, a.s.tiles, NT, WAVES).split;
     const size_t row_bytes = (size_t)std::min<int64_t>(4 * MR * MT, a.M) * PARTS * 2;
     a.chunk = (int)std::min<size_t>(a.s.tiles, (room / row_bytes - X_PAD) / W4_K);
     const size_t shared = std::max(row_bytes * (a.chunk * W4_K + X_PAD), a.split > 1 ? sums : 0);
@@ -433,8 +457,8 @@ static int linear4_sized(const Args4 &a, const void *x, void *y, hipStream_t st)
 {
     if constexpr (sizeof(T) == 2) {
         const int64_t blocks = ceil_div(a.s.blocks, 2), row_blocks = ceil_div(a.M, 4 * MR * MT);
-        const int64_t wgs = ceil_div(blocks, 16 / split4(blocks, row_blocks, a.s.tiles, 16)) * row_blocks;
-        if (wgs > 256 && 5 * wgs < 4 * 256 * ceil_div(wgs, 256)) return linear4_launch<T, STEPS, MR, MT, 2, 512>(a, x, y, st);
+        if (cut4(blocks, row_blocks, a.s.tiles, 2, 8).cost < cut4(blocks, row_blocks, a.s.tiles, 2, 16).cost)
+            return linear4_launch<T, STEPS, MR, MT, 2, 512>(a, x, y, st);
     }
     return linear4_launch<T, STEPS, MR, MT, 2, 1024>(a, x, y, st);
 }

@@ -263,7 +263,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float *__restrict
     const int64_t c = (int64_t)blockIdx.x * WAVE + lane;
     float s = 0.0f;
     if (c < 2 * (int64_t)d) {
-#pragma unroll 8
+#pragma unroll 16
         for (int p = wave; p < count; p += 16) s += parts[(size_t)p * 2 * d + c];
     }
     lds[wave][lane] = s;
