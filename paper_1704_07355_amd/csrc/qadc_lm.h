@@ -8,43 +8,19 @@ namespace qadc {
 inline size_t type_bytes(int type) { return type == QADC_TYPE_F32 ? 4 : 2; }
 inline bool type_ok(int type) { return type == QADC_TYPE_F32 || type == QADC_TYPE_F16 || type == QADC_TYPE_BF16; }
 
-// Sixteen bytes of a row.  Rows start at multiples of their element's size only; the memory unit takes wide loads and
-// stores at any such address, so no variant is kept for aligned rows.
+// Sixteen bytes of a row.  Rows begin at multiples of their element's size only; the memory unit takes wide loads and stores at
+// any such address, if more slowly.
 template <typename T>
 struct Pack {
     static constexpr int N = 16 / (int)sizeof(T);
     typedef T V __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
-// Elements c .. c + N - 1 of a row of d, `fill` beyond its end.
+// How many elements before a row the 16 bytes that hold its first one begin.
 template <typename T>
-__device__ __forceinline__ void load_pack(const T *row, int64_t c, int64_t d, float fill, float (&v)[Pack<T>::N])
+__device__ __forceinline__ int lead_of(const T *row)
 {
-    constexpr int N = Pack<T>::N;
-    if (c + N <= d) {
-        const typename Pack<T>::V p = *reinterpret_cast<const typename Pack<T>::V *>(row + c);
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (float)p[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = c + e < d ? (float)row[c + e] : fill;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ void store_pack(T *row, int64_t c, int64_t d, const float (&v)[Pack<T>::N])
-{
-    constexpr int N = Pack<T>::N;
-    if (c + N <= d) {
-        typename Pack<T>::V p;
-#pragma unroll
-        for (int e = 0; e < N; ++e) p[e] = (T)v[e];
-        *reinterpret_cast<typename Pack<T>::V *>(row + c) = p;
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (c + e < d) row[c + e] = (T)v[e];
-    }
+    return (int)((uintptr_t)row % 16 / sizeof(T));
 }
 
 // Float joined over the wavefront without a trip through LDS, in every lane: lanes of 16, then rows, then the last lane's value.

@@ -95,11 +95,6 @@ __device__ __forceinline__ bool add_block(Stats &st, const float (&x)[LP_BLOCK],
 // bytes in memory: a row that does not begin at one has its first pack begin `lead` logits before it (packs across those
 // multiples took a quarter longer: 4096 rows of 50021 bfloat16 logits 92 us, their gradient 199).
 template <typename T>
-__device__ __forceinline__ int lead_of(const T *row)
-{
-    return (int)((uintptr_t)row % 16 / sizeof(T));
-}
-template <typename T>
 __device__ __forceinline__ int64_t pack_at(int64_t chunk, int u, int lead)
 {
     return chunk * LP_CHUNK + ((int64_t)u * LP_WG + threadIdx.x) * Pack<T>::N - lead;

@@ -370,16 +370,24 @@ __global__ __launch_bounds__(NORM_WG) void norm_dx_kernel(const T *dy, int64_t l
 }
 
 constexpr int NORM_LONG = 16384;  // longest rows that stay in registers
-constexpr int NORM_PARTS = 512;   // most stretches of rows whose weight gradients are summed apart
 
 // Threads that share a row: eight elements each up to 8192, sixteen beyond.
 int norm_group(int d) { return d <= 128 ? 16 : d <= 256 ? 32 : d <= 512 ? 64 : d <= 1024 ? 128 : d <= 2048 ? 256 : d <= 4096 ? 512 : 1024; }
-int back_threads(int d) { return std::max(norm_group(d), 512); }
 
-int norm_parts(int64_t rows, int d)
+// Workgroups for `rows`, `at_once` of them at a time in each: at most `most`, and all with the same number of turns.
+int norm_wgs(int64_t rows, int at_once, int most)
 {
-    const int64_t at_once = d > NORM_LONG ? 16 : back_threads(d) / norm_group(d);
-    return (int)std::min<int64_t>(NORM_PARTS, std::max<int64_t>(1, ceil_div(rows, at_once)));
+    const int64_t turns = std::max<int64_t>(1, ceil_div(rows, (int64_t)at_once * most));
+    return (int)std::max<int64_t>(1, ceil_div(rows, at_once * turns));
+}
+
+// Workgroups of the backward pass, each with its own sums of the weight's gradients (8 d bytes written and read again): two of
+// 512 threads a compute unit, one of 1024.  With 512 of the latter 665 x 5702 bfloat16 took 31 us, a third of it for the sums.
+int back_wgs(int64_t rows, int d)
+{
+    if (d > NORM_LONG) return norm_wgs(rows, 16, 512);
+    const int group = norm_group(d);
+    return group > 512 ? norm_wgs(rows, 1, 256) : norm_wgs(rows, 512 / group, 512);
 }
 
 unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
@@ -389,7 +397,7 @@ unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 <<
 size_t layer_norm_workspace(int64_t rows, int d)
 {
     if (rows < 0 || d < 1) return 0;
-    return (size_t)norm_parts(rows, d) * 2 * (size_t)d * sizeof(float);
+    return (size_t)back_wgs(rows, d) * 2 * (size_t)d * sizeof(float);
 }
 
 static int norm_check(const char *who, int type, int wtype, int64_t rows, int d, int64_t ldx, int64_t ldy)
@@ -408,7 +416,7 @@ static void norm_launch_rows(const void *x, int64_t ldx, const void *weight, con
                              void *y, float *mean, float *rstd, hipStream_t st)
 {
     constexpr int THREADS = G > 256 ? G : 256;
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(rows, THREADS / G), 2048 * 256 / THREADS);
+    const unsigned grid = (unsigned)norm_wgs(rows, THREADS / G, 2048 * 256 / THREADS);
     launch(QADC_PROF_NORM, norm_rows_kernel<T, W, G, E, THREADS>, dim3(grid), dim3(THREADS), 0, st, (const T *)x, ldx,
            (const W *)weight, (const W *)bias, rows, d, eps, (T *)y, mean, rstd);
 }
@@ -461,7 +469,7 @@ static void norm_launch_back(const void *dy, int64_t lddy, const void *x, int64_
 {
     constexpr int THREADS = G > 512 ? G : 512;
     constexpr bool AHEAD = E == 8;  // (sixteen elements a thread leave no registers for the next row's)
-    const unsigned grid = (unsigned)norm_parts(rows, d);
+    const unsigned grid = (unsigned)back_wgs(rows, d);
     launch(QADC_PROF_NORM, norm_back_kernel<T, W, G, E, THREADS, AHEAD>, dim3(grid), dim3(THREADS), 0, st, (const T *)dy, lddy,
            (const T *)x, ldx, (const W *)weight, mean, rstd, rows, d, (T *)dx, parts);
 }
@@ -474,7 +482,7 @@ static void norm_backward_launch(const void *dy, int64_t lddy, const void *x, in
     const bool sums = dweight || dbias;
     int count = 0;  // without rows the sums of no parts are written
     if (rows > 0 && d <= NORM_LONG) {
-        count = norm_parts(rows, d);
+        count = back_wgs(rows, d);
 #define BACK(G_, E_) norm_launch_back<T, W, G_, E_>(dy, lddy, x, ldx, weight, mean, rstd, rows, d, dx, sums ? parts : nullptr, st)
         switch (norm_group(d)) {
         case 16: BACK(16, 8); break;
@@ -490,7 +498,7 @@ static void norm_backward_launch(const void *dy, int64_t lddy, const void *x, in
         }
 #undef BACK
     } else if (rows > 0 && sums) {
-        count = norm_parts(rows, d);
+        count = back_wgs(rows, d);
         launch(QADC_PROF_NORM, norm_weights_kernel<T>, dim3((unsigned)ceil_div(d, NORM_WG), (unsigned)count), dim3(NORM_WG), 0,
                st, (const T *)dy, lddy, (const T *)x, ldx, mean, rstd, rows, d, ceil_div(rows, count), parts);
     }
