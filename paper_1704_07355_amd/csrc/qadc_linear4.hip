@@ -162,6 +162,7 @@ struct Args4 {
     const float *bias;
     int split;  // wavefronts that share a block
     int chunk;  // tiles of x in LDS at a time
+    unsigned row_blocks;
 };
 
 constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's rows lie in different banks
@@ -169,21 +170,27 @@ constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's
 // A block of NT x 16 outputs and up to 4 MR MT rows of x: `split` wavefronts, each every split-th tile of the inputs; a workgroup
 // has as many blocks as it has wavefronts for, and brings x into LDS for all of them.  Of a matrix instruction's 16 rows,
 // 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
-// others repeat them.  STEPS: instructions per group.
-template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
+// others repeat them.  STEPS: instructions per group.  AGAIN: there are further rows, whose workgroups read the same weights.
+template <typename T, int STEPS, int MR, int MT, int NT, int THREADS, bool AGAIN>
 __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
 {
     constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
     constexpr bool HALF = Inputs<T>::HALF;
     constexpr int FLY = sizeof(T) == 4 ? 2 : 4;
-    constexpr int UNROLL = MT == 1 ? PER : 1;  // (groups side by side do not fit the registers of more rows)
+    // Four groups one after the other, each done before the next is begun where more rows share the registers (64 rows of
+    // 131072 x 4096, groups of 32: 203 -> 184 us); two groups of 64 are a loop there (32 rows of 16384 x 16384 60 us, 63 unrolled).
+    constexpr int UNROLL = MT == 1 || PER == 4 ? PER : 1;
     extern __shared__ float lds[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(lds);  // [PARTS][rows][chunk * W4_K + X_PAD]
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, j = lane >> 4;
     const int split = a.split, at_once = THREADS / WAVE / split;
-    const int64_t block = ((int64_t)blockIdx.x * at_once + wave / split) * NT;
+    // Workgroups go round the eight XCDs; those of different rows and the same outputs follow each other on one of them, so that
+    // its cache has the weights for all (64 rows of 131072 x 4096 with the rows' workgroups far apart: 150 us).
+    const unsigned turn = blockIdx.x >> 3;
+    const int64_t wg = AGAIN ? turn / a.row_blocks * 8 + (blockIdx.x & 7) : blockIdx.x;
+    const int64_t block = (wg * at_once + wave / split) * NT;
     const int part = wave % split, tiles = a.s.tiles;
-    const int64_t m0 = (int64_t)blockIdx.y * ROWS;
+    const int64_t m0 = AGAIN ? (int64_t)(turn % a.row_blocks) * ROWS : 0;
     const int rows = (int)min((int64_t)ROWS, a.M - m0), stride = a.chunk * W4_K + X_PAD;
 
     // where this lane's row of x in each m-tile lies, and its weights and scales
@@ -211,7 +218,9 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
         const unsigned set = (unsigned)(k / a.s.span) * W4_N + n;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            ring[d][t] = __builtin_nontemporal_load(reinterpret_cast<const bits16x8 *>(weights[t]) + ((unsigned)k * WAVE + lane));
+            const bits16x8 *from = reinterpret_cast<const bits16x8 *>(weights[t]) + ((unsigned)k * WAVE + lane);
+            if constexpr (AGAIN) ring[d][t] = *from;
+            else ring[d][t] = __builtin_nontemporal_load(from);
             ring_s[d][t] = reinterpret_cast<const Scales *>(scales[t])[set];
             if (a.has_zeros) ring_z[d][t] = reinterpret_cast<const Zeros *>(zeros[t])[set];
         }
@@ -323,6 +332,7 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
                     zb[u] >>= 8;
                 }
             }
+            if constexpr (MT > 1 && PER == 4) __builtin_amdgcn_sched_barrier(0);
         }
     };
     int k = part;
@@ -425,7 +435,7 @@ Cut4 cut4(int64_t blocks, int64_t row_blocks, int tiles, int nt, int waves)
 }
 
 // A workgroup of 16 wavefronts has a compute unit and its LDS to itself, of 8 it shares them with another one.
-template <typename T, int STEPS, int MR, int MT, int NT, int THREADS>
+template <typename T, int STEPS, int MR, int MT, int NT, int THREADS, bool AGAIN = false>
 static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
 {
     constexpr int WAVES = THREADS / WAVE, PARTS = Inputs<T>::PARTS;
@@ -433,7 +443,7 @@ static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
     static_assert(sums <= room, "the wavefronts' sums fit where x was");
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
-    const auto kernel = &linear4_kernel<T, STEPS, MR, MT, NT, THREADS>;
+    const auto kernel = &linear4_kernel<T, STEPS, MR, MT, NT, THREADS, AGAIN>;
     std::call_once(once, [&] {  // more than the default limit of dynamic LDS
         attr = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
     });
@@ -443,7 +453,9 @@ static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
     const size_t row_bytes = (size_t)std::min<int64_t>(4 * MR * MT, a.M) * PARTS * 2;
     a.chunk = (int)std::min<size_t>(a.s.tiles, (room / row_bytes - X_PAD) / W4_K);
     const size_t shared = std::max(row_bytes * (a.chunk * W4_K + X_PAD), a.split > 1 ? sums : 0);
-    launch(QADC_PROF_LINEAR4, *kernel, dim3((unsigned)ceil_div(blocks, WAVES / a.split), (unsigned)row_blocks), dim3(THREADS),
+    a.row_blocks = (unsigned)row_blocks;
+    const int64_t wgs = ceil_div(blocks, WAVES / a.split);
+    launch(QADC_PROF_LINEAR4, *kernel, dim3((unsigned)(AGAIN ? ceil_div(wgs, 8) * 8 * row_blocks : wgs)), dim3(THREADS),
            shared, st, a, (const T *)x, (T *)y);
     return QADC_OK;
 }
@@ -452,28 +464,28 @@ static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
 // 16384 inputs is brought in half as often: 82 -> 62), unless a last round of workgroups would leave much of the chip idle:
 // there eight (one row of 40000 x 8000 37 us against 47, 24 rows of 10007 x 5000 28 against 32).  A float32 x, in three parts,
 // needs the room (12 rows of 20000 x 2000: 22 us against 26).
-template <typename T, int STEPS, int MR, int MT>
+template <typename T, int STEPS, int MR, int MT, bool AGAIN = false>
 static int linear4_sized(const Args4 &a, const void *x, void *y, hipStream_t st)
 {
     if constexpr (sizeof(T) == 2) {
         const int64_t blocks = ceil_div(a.s.blocks, 2), row_blocks = ceil_div(a.M, 4 * MR * MT);
         if (cut4(blocks, row_blocks, a.s.tiles, 2, 8).cost < cut4(blocks, row_blocks, a.s.tiles, 2, 16).cost)
-            return linear4_launch<T, STEPS, MR, MT, 2, 512>(a, x, y, st);
+            return linear4_launch<T, STEPS, MR, MT, 2, 512, AGAIN>(a, x, y, st);
     }
-    return linear4_launch<T, STEPS, MR, MT, 2, 1024>(a, x, y, st);
+    return linear4_launch<T, STEPS, MR, MT, 2, 1024, AGAIN>(a, x, y, st);
 }
 
 template <typename T, int STEPS>
 static int linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
 {
-    // the y dimension of a grid is 16 bits wide: rows in slabs
-    const int64_t slab = 65535 * 32ll, M = a.M;
+    const int64_t slab = 4096, M = a.M;  // (a grid's size stays within 32 bits)
     for (int64_t m = 0; m < M; m += slab) {
         a.M = std::min(slab, M - m);
         const T *xs = x + m * a.ldx;
         T *ys = y + m * a.ldy;
         int rc;
-        if (a.M > 16) rc = linear4_sized<T, STEPS, 4, 2>(a, xs, ys, st);
+        if (a.M > 32) rc = linear4_sized<T, STEPS, 4, 2, true>(a, xs, ys, st);
+        else if (a.M > 16) rc = linear4_sized<T, STEPS, 4, 2>(a, xs, ys, st);
         else if (a.M > 4) rc = linear4_sized<T, STEPS, 4, 1>(a, xs, ys, st);
         else if (a.s.blocks >= 1024) rc = linear4_sized<T, STEPS, 1, 1>(a, xs, ys, st);
         else rc = linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st);  // few outputs: all wavefronts that they are worth
@@ -494,7 +506,7 @@ int linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_
     if (!w->packed || !x || !y) return fail(QADC_EINVAL, "qadc_linear4: null pointer");
     if ((uintptr_t)w->packed % 16) return fail(QADC_EINVAL, "qadc_linear4: packed is not 16-byte aligned");
     const Args4 a = {(const char *)w->packed, shape4(w->N, w->K, w->group, w->has_zeros != 0), w->N, M, ldx, ldy, w->K, w->stype,
-                     w->has_zeros != 0, bias, 1, 1};
+                     w->has_zeros != 0, bias, 1, 1, 1};
     int rc = QADC_OK;
     QADC_BY_TYPE(type, {
         if (w->group == 32) rc = linear4_rows<T, 1>(a, (const T *)x, (T *)y, st);
