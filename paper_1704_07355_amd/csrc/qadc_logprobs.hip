@@ -673,9 +673,11 @@ int token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t ro
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: null pointer");
     if (logits == dlogits && ld != ldd)
         return fail(QADC_EINVAL, "qadc_token_logprobs_backward: in place needs equal row distances");
-    const int64_t chunks = ceil_div((int64_t)V + 7, LP_CHUNK);
-    const int per = (int)std::min<int64_t>(chunks, std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048)));
-    const int parts = (int)ceil_div(chunks, per);
+    // (where rows begin off 16 bytes, up to seven logits into their first pack)
+    const bool even = (uintptr_t)dlogits % 16 == 0 && (size_t)ldd * type_bytes(type) % 16 == 0;
+    const int64_t chunks = ceil_div((int64_t)V + (even ? 0 : 7), LP_CHUNK);
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));  // chunks a workgroup
+    const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
     const dim3 grid((unsigned)std::min<int64_t>(rows * parts, 1 << 20));
     const int nt = T;
     const bool stream = (size_t)rows * V * type_bytes(type) > ((size_t)384 << 20);
