@@ -504,7 +504,7 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
  * Sums in float32.  A logit of -inf is a token that is masked out: p = 0, and it adds nothing to the entropy.
  * A row with nothing left has lse = -inf, entropy 0 and every log probability -inf.  A row that holds a NaN or +inf has
  * lse, entropy and log probabilities NaN; its alternatives are still ordered, a NaN before +inf.
- *   logits [rows][ld] of `type`, V <= ld of them per row;  scale > 0 (the inverse of a temperature)
+ *   logits [rows][ld] of `type`, V <= ld of them per row;  0 < scale <= 2e38 (the inverse of a temperature)
  *   tokens [rows][T] i32, 0 <= T <= QADC_MAX_R, NULL when T = 0: an entry outside [0, V) is an unused slot, its logp is 0
  *   k      0..QADC_MAX_ALTERNATIVES
  *   logp [rows][T], lse [rows], entropy [rows] f32;  top_idx [rows][k] u32, top_logp [rows][k] f32 (outputs; lse, entropy

@@ -580,7 +580,7 @@ int check_logits(const char *who, int type, int64_t ld, int64_t rows, int V, flo
 {
     if (!type_ok(type)) return fail(QADC_EINVAL, "%s: unknown type %d", who, type);
     if (rows < 0 || V < 1 || ld < V) return fail(QADC_EINVAL, "%s: rows=%lld V=%d ld=%lld", who, (long long)rows, V, (long long)ld);
-    if (!(scale > 0.0f) || scale == INFINITY) return fail(QADC_EINVAL, "%s: scale=%g", who, (double)scale);
+    if (!(scale > 0.0f) || !(scale * LOG2E < INFINITY)) return fail(QADC_EINVAL, "%s: scale=%g", who, (double)scale);
     if (T < 0 || T > QADC_MAX_R) return fail(QADC_EINVAL, "%s: T=%d", who, T);
     if (T > 0 && rows > 0 && !tokens) return fail(QADC_EINVAL, "%s: null pointer", who);
     return QADC_OK;

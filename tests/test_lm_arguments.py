@@ -91,6 +91,16 @@ def test_token_logprobs():
     assert g(P, 1000, 0, 4, 1000, 1.0, P, 2, P, P, P, P, P, 1001, None) == Q.QADC_EINVAL  # in place, other row distances
 
 
+def test_token_logprobs_scale_beyond_the_exponent():
+    """A scale whose product with log2(e) is no float32 would turn 0 times it into NaN."""
+    L = Q.lib()
+    P = PTR
+    need = Q.qadc_token_logprobs_workspace_bytes(4, 1000, 10)
+    assert L.qadc_token_logprobs(P, 1000, 0, 4, 1000, 3e38, P, 2, 10, P, P, P, P, P, P, need, None) == Q.QADC_EINVAL
+    assert L.qadc_token_logprobs_backward(P, 1000, 0, 4, 1000, 3e38, P, 2, P, P, P, P, P + 256, 1000, None) == Q.QADC_EINVAL
+    assert L.qadc_token_logprobs(None, 1000, 0, 0, 1000, 2e38, None, 0, 0, None, None, None, None, None, None, 0, None) == Q.QADC_OK
+
+
 def test_neighbour_mix():
     L = Q.lib()
     P = PTR
