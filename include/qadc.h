@@ -475,7 +475,7 @@ size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
  */
 typedef struct qadc_weights4 {
     const void *packed;
-    int64_t N;   /* outputs */
+    int64_t N;   /* outputs, at most 2^30 */
     int K;       /* inputs, at most 2^24 */
     int group;
     int stype;

@@ -25,6 +25,7 @@ namespace qadc {
 namespace {
 
 constexpr int W4_N = 16, W4_K = 128, W4_BYTES = W4_N * W4_K / 2;  // a tile
+constexpr int64_t W4_MOST = 1ll << 30;  // outputs
 
 struct Shape4 {
     int64_t blocks;  // of 16 outputs
@@ -383,7 +384,7 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
 
 int check4(const char *who, int64_t N, int K, int group, int stype)
 {
-    if (N < 1 || N > (1ll << 31) - 16 || K < 1 || K > (1 << 24))
+    if (N < 1 || N > W4_MOST || K < 1 || K > (1 << 24))
         return fail(QADC_EINVAL, "%s: N=%lld K=%d", who, (long long)N, K);
     if (group != 32 && group != 64 && (group < 128 || group % 128 != 0))
         return fail(QADC_EINVAL, "%s: group=%d is neither 32, 64 nor a multiple of 128", who, group);
@@ -478,7 +479,9 @@ static int linear4_sized(const Args4 &a, const void *x, void *y, hipStream_t st)
 template <typename T, int STEPS>
 static int linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
 {
-    const int64_t slab = 4096, M = a.M;  // (a grid's size stays within 32 bits)
+    // As many rows at a time as keep the threads of a grid within 32 bits: two an output and 32 rows (a wavefront for 32 outputs),
+    // up to eight workgroups more.
+    const int64_t slab = 32 * std::min<int64_t>(128, ((1ll << 32) - 1) / (2 * a.N + 8 * 1024)), M = a.M;
     for (int64_t m = 0; m < M; m += slab) {
         a.M = std::min(slab, M - m);
         const T *xs = x + m * a.ldx;

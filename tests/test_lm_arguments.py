@@ -63,6 +63,12 @@ def test_weights4_and_linear4():
     assert b"qadc_linear4" in L.qadc_last_error()
 
 
+def test_weights4_of_too_many_outputs():
+    """Beyond 2^30 outputs the threads of a product's grid would pass 32 bits."""
+    assert Q.qadc_weights4_bytes(1 << 30, 128, 128, 0) == (1 << 26) * (1024 + 32)
+    assert Q.qadc_weights4_bytes((1 << 30) + 1, 128, 128, 0) == 0
+
+
 def test_token_logprobs():
     L = Q.lib()
     need = Q.qadc_token_logprobs_workspace_bytes(4, 1000, 10)
