@@ -10,6 +10,7 @@
 // that (below e^-69) is added up again relative to its own largest.
 
 #include <algorithm>
+#include <cfloat>
 
 #include "qadc_lm.h"
 #include "qadc_profile.h"
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             const int at = i * THREADS + threadIdx.x;
-            const float v = d[i] < INFINITY ? -b * (d[i] - near) : -INFINITY, e = expf(v);
+            const float v = d[i] < INFINITY ? -b * fminf(d[i] - near, FLT_MAX) : -INFINITY, e = expf(v);  // (no 0 times inf)
             z += e;
             if (at < padded) {
                 votes[at] = make_int2(val[i], __float_as_int(e));
@@ -144,6 +145,7 @@ int neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const f
     if (rows == 0 || T == 0) return QADC_OK;
     if (!ids || !dist || (n > 0 && !values) || !tokens || !lm_logp || !mix)
         return fail(QADC_EINVAL, "qadc_neighbour_mix: null pointer");
+    n = std::min<int64_t>(n, 0xFFFFFFFF);  // (the padding is no id)
     const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
     const float log_keep = log1pf(-lambda), log_lambda = logf(lambda);
     // Rows of few neighbours and tokens have a wavefront each, where there are enough of them.

@@ -101,6 +101,17 @@ def test_weights_below_the_smallest_float():
     assert torch.isfinite(got[1][0, :3]).all() and got[1][0, 3] == -math.inf
 
 
+def test_distances_further_apart_than_a_float_reaches():
+    """With beta 0 all neighbours weigh the same, also where the difference of two distances overflows."""
+    import paper_1704_07355_amd as Q
+    ids = torch.arange(4, device=DEV, dtype=torch.int32)[None, :].contiguous()
+    dist = torch.tensor([[-3e38, 3e38, 0.0, 1.0]], device=DEV)
+    values = torch.tensor([1, 2, 2, 2], device=DEV, dtype=torch.int32)
+    tokens = torch.tensor([[1, 2, 3]], device=DEV, dtype=torch.int32)
+    lm = torch.tensor([[-1.0, -2.0, -3.0]], device=DEV)
+    check(Q.qadc_neighbour_mix(ids, dist, values, tokens, lm, 0.5, 0.0), ids, dist, values, tokens, lm, 0.5, 0.0, None)
+
+
 def test_results_of_a_search_streams_and_equal_bits():
     import paper_1704_07355_amd as Q
     ids, dist, values, tokens, lm, step = make(50, 100, 30, 1000, "u8", 7)
