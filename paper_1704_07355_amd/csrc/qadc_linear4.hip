@@ -11,6 +11,11 @@
 // The product.  A nibble q put into the mantissa of 16 is the 16-bit number 16 + q, exactly: no conversion, one shift and one
 // and-or for a pair.  The matrix units multiply these with x (float32 x as the sum of three bfloat16 numbers) and, once for all
 // outputs, a column of ones with x; with p and t the two sums over a group, the group adds s (p - (16 + z) t) to the output.
+//
+// Bound by the weights' bytes for a few rows: one row of 131072 x 4096 bfloat16 49 us (277 MB at 5.6 TB/s), of 4096 x 4096
+// binary16 5.2, a launch and a round trip; beyond 16 rows by vector instructions (unpacking, 8 for 8 weights of each lane, and
+// what follows a group) and by x, which every workgroup brings into LDS: 24 rows of 10007 x 5000 in groups of 32 23 us, 64 rows of
+// 131072 x 4096 135 us.
 
 #include <algorithm>
 #include <mutex>

@@ -8,6 +8,10 @@
 // below.  While the row streams by, only the largest logit of every block (32 logits of one thread) is kept.  The k-th largest of
 // the threads' largest logits bounds the k-th logit from below, since k different logits reach it; the few blocks that reach it
 // are read again, from the cache, and what reaches it is ordered.
+//
+// Bound by memory where there are many rows: 4096 x 65536 bfloat16 86 us (537 MB at 6.2 TB/s), its gradient 192 (1.07 GB at
+// 5.6); by launches and round trips where there are few: 131072 logits with 20 alternatives 4 us for the parts and 10 for the
+// join, 64 x 50021 with 50 alternatives 5 and 13.
 
 #include <algorithm>
 #include <type_traits>

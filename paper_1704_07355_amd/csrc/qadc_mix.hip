@@ -8,6 +8,9 @@
 // LDS as (token, exp v), and a thread adds up what its token has among its share of them, three instructions a neighbour and no
 // branch; P parts of a row's neighbours where there are fewer tokens than threads.  A token whose votes are all too small for
 // that (below e^-69) is added up again relative to its own largest.
+//
+// Bound by the gathers: 2048 rows of 1024 neighbours from 10 M values 47 us, 2 M reads of 4 bytes, each a line (246 MB fetched);
+// one row of 100 neighbours 5.4 us, three dependent round trips.
 
 #include <algorithm>
 #include <cfloat>

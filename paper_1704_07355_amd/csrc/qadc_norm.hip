@@ -7,6 +7,9 @@
 // A row of up to 16384 elements stays in the registers of its group of threads, 8 or 16 a thread; the group goes on to further
 // rows with the weights (and the sums of the weight's gradients) in registers, the next row's elements already on their way.
 // Longer rows are read again for every pass.
+//
+// Bound by memory: 16384 x 4096 bfloat16 backward 79 us (402 MB at 5.1 TB/s) and 5 us for the join of the sums, 2049 x 1111
+// float32 14 + 5; five rows of 4096 bfloat16 forward 3.4 us, a launch's latency.
 
 #include <algorithm>
 
