@@ -13,7 +13,6 @@
 // one row of 100 neighbours 5.4 us, three dependent round trips.
 
 #include <algorithm>
-#include <cfloat>
 
 #include "qadc_lm.h"
 #include "qadc_profile.h"
@@ -56,7 +55,7 @@ __global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict
     const int t_mine = threadIdx.x % tokens_at_once, part = threadIdx.x / tokens_at_once, parts = THREADS / tokens_at_once;
     const int padded = (R + 7) / 8 * 8;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const float b = step ? beta * step[r] : beta;
+        const float step_of = step ? step[r] : 1.0f, b = beta * step_of;
         int tok = t_mine < T ? tokens[r * T + t_mine] : -1;  // on their way with the neighbours
         float l = t_mine < T ? lm[r * T + t_mine] : 0.0f;
         uint32_t id[MINE];
@@ -82,7 +81,13 @@ __global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             const int at = i * THREADS + threadIdx.x;
-            const float v = d[i] < INFINITY ? -b * fminf(d[i] - near, FLT_MAX) : -INFINITY, e = expf(v);  // (no 0 times inf)
+            float v = -INFINITY;
+            if (d[i] < INFINITY) {
+                const float away = d[i] - near;
+                if (b < INFINITY && away < INFINITY) v = -b * away;
+                else v = (float)(-(double)beta * step_of * ((double)d[i] - near));  // (a float does not hold a part of it; no 0 times inf)
+            }
+            const float e = expf(v);
             z += e;
             if (at < padded) {
                 votes[at] = make_int2(val[i], __float_as_int(e));

@@ -142,3 +142,27 @@ def test_refusals_of_the_binding():
     wide = torch.zeros((1, 1025), dtype=torch.int32, device=DEV)
     with pytest.raises(Q.QadcError):
         Q.qadc_neighbour_mix(wide, wide.float(), values, tokens[:1], lm[:1], 0.5, 1.0)
+
+
+def test_weights_whose_product_passes_a_float():
+    """beta and step are finite, their product is not: the nearest still have their votes, and a difference that the product brings
+    back to order one still counts.  The same for a difference that passes a float where beta brings it back."""
+    import paper_1704_07355_amd as Q
+    ids = torch.arange(4, device=DEV, dtype=torch.int32)[None, :].expand(3, 4).contiguous()
+    values = torch.tensor([1, 2, 1, 3], device=DEV, dtype=torch.int32)
+    tokens = torch.tensor([[1, 2, 3, 4, -1]], device=DEV, dtype=torch.int32).expand(3, 5).contiguous()
+    lm = -torch.arange(1.0, 16.0, device=DEV).reshape(3, 5)
+    step = torch.tensor([2.0 ** 100, 2.0 ** 90, 1.0], device=DEV)
+    near = torch.full((3, 4), 7, device=DEV, dtype=torch.uint8)
+    check(Q.qadc_neighbour_mix(ids, near, values, tokens, lm, 0.5, 2.0 ** 60, step), ids, near, values, tokens, lm, 0.5, 2.0 ** 60, step)
+    near[:, 3] = 9  # e^(-2^161): no vote is left
+    knn = Q.qadc_neighbour_mix(ids, near, values, tokens, lm, 0.5, 2.0 ** 60, step)[1]
+    want = torch.tensor([2 / 3, 1 / 3], device=DEV, dtype=torch.float64).log().expand(2, 2)
+    within(knn[:2, :2], want, 64 * EPS)
+    assert (knn[:2, 2:4] == -math.inf).all() and not knn[:, 4].any()
+    tiny = torch.tensor([[0.0, 1.0, 2.0, 0.5]]) * 2.0 ** -140
+    tiny = torch.cat((tiny, tiny * 2.0 ** 5, tiny), 0).to(DEV)
+    step = torch.tensor([2.0 ** 80, 2.0 ** 75, 2.0 ** 80], device=DEV)
+    check(Q.qadc_neighbour_mix(ids, tiny, values, tokens, lm, 0.5, 2.0 ** 60, step), ids, tiny, values, tokens, lm, 0.5, 2.0 ** 60, step)
+    far = torch.tensor([[-3e38, 3e38, 0.0, 1e38]], device=DEV).expand(3, 4).contiguous()
+    check(Q.qadc_neighbour_mix(ids, far, values, tokens, lm, 0.5, 2.0 ** -126, None), ids, far, values, tokens, lm, 0.5, 2.0 ** -126, None)
