@@ -49,7 +49,9 @@ __global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict
 {
     constexpr int MINE = QADC_MAX_R / THREADS < 4 ? QADC_MAX_R / THREADS : 4;  // neighbours a thread, THREADS apart
     __shared__ float lds[2][THREADS / WAVE];
-    __shared__ int2 votes[THREADS * MINE];  // (token, exp v)
+    __shared__ int4 pairs[THREADS * MINE / 2];  // (token, exp v), two neighbours in 16 bytes
+    int2 *const votes = reinterpret_cast<int2 *>(pairs);
+    static_assert(alignof(decltype(pairs)) == 16, "two neighbours are read at once");
     __shared__ float far[THREADS * MINE];   // v
     __shared__ float2 sums[THREADS];        // of a part: (sum of exp v, 1 if there is a vote)
     const int t_mine = threadIdx.x % tokens_at_once, part = threadIdx.x / tokens_at_once, parts = THREADS / tokens_at_once;
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(THREADS) void mix_kernel(const uint32_t *__restrict
             bool vote = false;
 #pragma unroll 4
             for (int i = 2 * part; i < padded; i += 2 * parts) {
-                const int4 two = *reinterpret_cast<const int4 *>(&votes[i]);
+                const int4 two = pairs[i / 2];
                 s[0] += two.x == tok ? __int_as_float(two.y) : 0.0f;
                 s[1] += two.z == tok ? __int_as_float(two.w) : 0.0f;
                 vote |= two.x == tok || two.z == tok;
