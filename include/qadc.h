@@ -544,7 +544,7 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
  *   dist [rows][R] f32 (dist_bytes = 4), or u8 quantized sums (dist_bytes = 1)
  *   step [rows] f32 or NULL: the distance is step[row] * dist (`delta` of qadc_quantize_luts; finite, >= 0), 1 without
  *   values [n] i32: the token that followed each stored state;  beta >= 0
- *   tokens [rows][T] i32, lm_logp [rows][T] f32, T >= 0;  0 <= lambda <= 1
+ *   tokens [rows][T] i32, lm_logp [rows][T] f32, 0 <= T < 2^31 - 1024;  0 <= lambda <= 1
  *   mix, knn [rows][T] f32 (outputs; knn nullable)
  */
 int qadc_neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const float *step, int64_t rows, int R,

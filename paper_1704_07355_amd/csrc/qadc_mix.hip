@@ -147,7 +147,8 @@ int neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const f
                   const int32_t *values, int64_t n, float beta, const int32_t *tokens, int T, const float *lm_logp,
                   float lambda, float *mix, float *knn, hipStream_t st)
 {
-    if (rows < 0 || R < 1 || R > QADC_MAX_R || n < 0 || T < 0)
+    // (tokens are counted in an int, up to 256 past the last one)
+    if (rows < 0 || R < 1 || R > QADC_MAX_R || n < 0 || T < 0 || T > INT32_MAX - 1024)
         return fail(QADC_EINVAL, "qadc_neighbour_mix: rows=%lld R=%d n=%lld T=%d", (long long)rows, R, (long long)n, T);
     if (dist_bytes != 1 && dist_bytes != 4) return fail(QADC_EINVAL, "qadc_neighbour_mix: dist_bytes=%d", dist_bytes);
     if (!(beta >= 0.0f) || beta == INFINITY || !(lambda >= 0.0f && lambda <= 1.0f))

@@ -120,3 +120,11 @@ def test_neighbour_mix():
         args[at] = value
         assert f(*args) == Q.QADC_EINVAL, (at, value)
     assert b"qadc_neighbour_mix" in L.qadc_last_error()
+
+
+def test_neighbour_mix_of_more_tokens_than_an_int_counts():
+    """A row's tokens are counted in steps of up to 256: the last step must not pass 2^31."""
+    f = Q.lib().qadc_neighbour_mix
+    for T in (2 ** 31 - 1, 2 ** 31 - 1023):
+        assert f(PTR, PTR, 4, None, 0, 10, PTR, 5, 1.0, PTR, T, PTR, 0.5, PTR, PTR, None) == Q.QADC_EINVAL
+    assert f(PTR, PTR, 4, None, 0, 10, PTR, 5, 1.0, PTR, 2 ** 31 - 1025, PTR, 0.5, PTR, PTR, None) == Q.QADC_OK  # (no rows)
