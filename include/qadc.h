@@ -436,7 +436,7 @@ int qadc_rotate(const float *rot, int d, const float *x, int64_t n, float *y, vo
  *     mean = sum x / d,  rstd = 1 / sqrt(sum (x - mean)^2 / d + eps),
  *     y[c] = (x[c] - mean) * rstd * weight[c] + bias[c]
  * in float32, rounded once to `type`.  A row that holds an infinity or a NaN becomes NaN.
- *   x [rows][ldx] of `type`;  y [rows][d] of `type` (output; may be x when ldx == d)
+ *   x [rows][ldx] of `type`, 1 <= d < 2^31 - 1024;  y [rows][d] of `type` (output; may be x when ldx == d)
  *   weight, bias [d] of `wtype`: QADC_TYPE_F32 or `type`; each may be NULL (1, 0)
  *   eps >= 0;  mean, rstd [rows] f32 (outputs for the backward pass, each nullable)
  */

@@ -421,7 +421,7 @@ unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 <<
 
 size_t layer_norm_workspace(int64_t rows, int d)
 {
-    if (rows < 0 || d < 1) return 0;
+    if (rows < 0 || d < 1 || d > INT32_MAX - 1024) return 0;
     return (size_t)back_wgs(rows, d) * 2 * (size_t)d * sizeof(float);
 }
 
@@ -430,7 +430,8 @@ static int norm_check(const char *who, int type, int wtype, int64_t rows, int d,
     if (!type_ok(type)) return fail(QADC_EINVAL, "%s: unknown type %d", who, type);
     if (wtype != QADC_TYPE_F32 && wtype != type)
         return fail(QADC_EINVAL, "%s: wtype %d is neither QADC_TYPE_F32 nor the rows' type", who, wtype);
-    if (rows < 0 || d < 1) return fail(QADC_EINVAL, "%s: rows=%lld d=%d", who, (long long)rows, d);
+    // (columns are counted in an int, a workgroup's width past the last one)
+    if (rows < 0 || d < 1 || d > INT32_MAX - 1024) return fail(QADC_EINVAL, "%s: rows=%lld d=%d", who, (long long)rows, d);
     if (ldx < d || ldy < d) return fail(QADC_EINVAL, "%s: rows of %d elements, a row distance of %lld", who, d,
                                         (long long)std::min(ldx, ldy));
     return QADC_OK;

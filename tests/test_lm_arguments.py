@@ -128,3 +128,14 @@ def test_neighbour_mix_of_more_tokens_than_an_int_counts():
     for T in (2 ** 31 - 1, 2 ** 31 - 1023):
         assert f(PTR, PTR, 4, None, 0, 10, PTR, 5, 1.0, PTR, T, PTR, 0.5, PTR, PTR, None) == Q.QADC_EINVAL
     assert f(PTR, PTR, 4, None, 0, 10, PTR, 5, 1.0, PTR, 2 ** 31 - 1025, PTR, 0.5, PTR, PTR, None) == Q.QADC_OK  # (no rows)
+
+
+def test_layer_norm_of_longer_rows_than_an_int_counts():
+    """A row's columns are counted in steps of a workgroup: the last step must not pass 2^31."""
+    L = Q.lib()
+    for d in (2 ** 31 - 1, 2 ** 31 - 1023):
+        assert L.qadc_layer_norm(PTR, d, 1, None, None, 1, 0, d, 1e-5, PTR, None, None, None) == Q.QADC_EINVAL
+        assert L.qadc_layer_norm_backward(PTR, d, PTR, d, 1, None, 1, PTR, PTR, 0, d, PTR, None, None, None, 0, None) == Q.QADC_EINVAL
+    assert Q.qadc_layer_norm_workspace_bytes(4, 2 ** 31 - 1) == 0
+    d = 2 ** 31 - 1025
+    assert L.qadc_layer_norm(PTR, d, 1, None, None, 1, 0, d, 1e-5, PTR, None, None, None) == Q.QADC_OK  # (no rows)
