@@ -452,7 +452,7 @@ int qadc_layer_norm(const void *x, int64_t ldx, int type, const void *weight, co
  *   dx [rows][d] of `type` (output, nullable; may be dy or x when that is dense)
  *   dweight, dbias [d] f32 (outputs, each nullable)
  *   workspace >= qadc_layer_norm_workspace_bytes(rows, d), 16-byte aligned (0 and NULL without dweight and dbias); it need
- *   not be cleared and is not left cleared.
+ *   not be cleared and is not left cleared, and serves fewer rows of the same d too.
  */
 int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx, int type, const void *weight,
                              int wtype, const float *mean, const float *rstd, int64_t rows, int d, void *dx,

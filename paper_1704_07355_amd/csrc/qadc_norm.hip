@@ -408,21 +408,23 @@ int norm_wgs(int64_t rows, int at_once, int most)
 
 // Workgroups of the backward pass, each with its own sums of the weight's gradients (8 d bytes written and read again): two of
 // 512 threads a compute unit, one of 1024.  With 512 of the latter 665 x 5702 bfloat16 took 31 us, a third of it for the sums.
-int back_wgs(int64_t rows, int d)
-{
-    if (d > NORM_LONG) return norm_wgs(rows, 16, 512);
-    const int group = norm_group(d);
-    return group > 512 ? norm_wgs(rows, 1, 256) : norm_wgs(rows, 512 / group, 512);
-}
+int back_rows(int d) { return d > NORM_LONG ? 16 : std::max(1, 512 / norm_group(d)); }  // rows of a workgroup at a time
+int back_most(int d) { return d <= NORM_LONG && norm_group(d) > 512 ? 256 : 512; }
+int back_wgs(int64_t rows, int d) { return norm_wgs(rows, back_rows(d), back_most(d)); }
 
 unsigned norm_grid(int64_t rows) { return (unsigned)std::min<int64_t>(rows, 1 << 20); }
 
 }  // namespace
 
+static size_t back_bytes(int wgs, int d) { return (size_t)wgs * 2 * (size_t)d * sizeof(float); }
+
+// Enough for these rows and for any fewer, of which up to twice as many workgroups can be made (4096 columns: 257 for 513 rows, 512
+// for 512).  The call itself asks for its own rows' share only.
 size_t layer_norm_workspace(int64_t rows, int d)
 {
     if (rows < 0 || d < 1 || d > INT32_MAX - 1024) return 0;
-    return (size_t)back_wgs(rows, d) * 2 * (size_t)d * sizeof(float);
+    const int64_t alone = std::min<int64_t>(rows, back_rows(d) * (int64_t)back_most(d));  // the most rows that are done in one turn
+    return back_bytes(back_wgs(alone, d), d);
 }
 
 static int norm_check(const char *who, int type, int wtype, int64_t rows, int d, int64_t ldx, int64_t ldy)
@@ -548,7 +550,7 @@ int layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_t ldx
     if ((dx == dy && dx && lddy != d) || (dx == x && dx && ldx != d))
         return fail(QADC_EINVAL, "qadc_layer_norm_backward: in place needs dense rows");
     if (dweight || dbias) {
-        const size_t need = layer_norm_workspace(rows, d);
+        const size_t need = back_bytes(back_wgs(rows, d), d);
         if (!workspace || workspace_bytes < need)
             return fail(QADC_ENOMEM, "qadc_layer_norm_backward: workspace of %zu bytes, %zu needed", workspace_bytes, need);
     }

@@ -231,3 +231,17 @@ def test_refusals_of_the_binding():
     with pytest.raises(Q.QadcError) as e:
         Q.qadc_layer_norm_backward(dy, x, w, mean, rstd, workspace=torch.empty((16,), dtype=torch.uint8, device=DEV))
     assert e.value.code == Q.QADC_ENOMEM
+
+
+@pytest.mark.parametrize("rows,d", [(513, 4096), (2100, 900), (257, 8000), (8200, 20000)])
+def test_a_workspace_for_a_batch_serves_its_smaller_batches(rows, d):
+    import paper_1704_07355_amd as Q
+    ws = torch.empty((Q.qadc_layer_norm_workspace_bytes(rows, d),), dtype=torch.uint8, device=DEV)
+    x, w, b, dy = _inputs(rows, d, "bf16", 41, "f32")
+    _, mean, rstd = Q.qadc_layer_norm(x, w, b)
+    for n in (rows, rows - 1, rows // 2 + 200, 256, 3):
+        if n > rows:
+            continue
+        part = dy[:n], x[:n], w, mean[:n], rstd[:n]
+        got, want = Q.qadc_layer_norm_backward(*part, workspace=ws), Q.qadc_layer_norm_backward(*part)
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), n

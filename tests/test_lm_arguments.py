@@ -139,3 +139,10 @@ def test_layer_norm_of_longer_rows_than_an_int_counts():
     assert Q.qadc_layer_norm_workspace_bytes(4, 2 ** 31 - 1) == 0
     d = 2 ** 31 - 1025
     assert L.qadc_layer_norm(PTR, d, 1, None, None, 1, 0, d, 1e-5, PTR, None, None, None) == Q.QADC_OK  # (no rows)
+
+
+def test_layer_norm_workspaces_grow_with_the_batch():
+    """What is asked for a batch holds what is asked for any smaller one."""
+    for d in (1, 100, 300, 900, 2000, 4096, 4097, 16384, 16385, 100000):
+        sizes = [Q.qadc_layer_norm_workspace_bytes(rows, d) for rows in [*range(0, 2100), *range(2100, 40000, 37), 1 << 20, 1 << 33]]
+        assert sizes == sorted(sizes) and sizes[1] > 0, d
