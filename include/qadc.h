@@ -510,7 +510,7 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
  *   logp [rows][T], lse [rows], entropy [rows] f32;  top_idx [rows][k] u32, top_logp [rows][k] f32 (outputs; lse, entropy
  *   nullable; when V < k the tail is padded with 0xFFFFFFFF and -inf)
  *   workspace >= qadc_token_logprobs_workspace_bytes(rows, V, k), 16-byte aligned; it need not be cleared and is not left
- *   cleared
+ *   cleared, and serves fewer rows, tokens and alternatives too
  */
 #define QADC_MAX_ALTERNATIVES 128
 int qadc_token_logprobs(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const int32_t *tokens,

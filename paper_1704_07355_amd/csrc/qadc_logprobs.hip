@@ -592,6 +592,8 @@ int check_logits(const char *who, int type, int64_t ld, int64_t rows, int V, flo
 
 }  // namespace
 
+constexpr int64_t LP_WHOLE = 400, LP_PARTS = 1024;
+
 // How a call is cut: a row per workgroup where the rows alone nearly fill the chip, parts of rows otherwise.
 struct Plan {
     int64_t chunks;
@@ -603,9 +605,9 @@ static Plan plan_logprobs(int64_t rows, int V, int k)
 {
     Plan p;
     p.chunks = ceil_div((int64_t)V + 7, LP_CHUNK);  // (a row begins up to seven logits into its first pack)
-    // Rows are cut into parts, joined by a second kernel, up to 400 of them (300 x 131072, 20 alternatives: 34 us against 37 whole;
+    // Rows are cut into parts, joined by a second kernel, where there are fewer than 400 (300 x 131072, 20 alternatives: 34 us against 37 whole;
     // 500: 47 against 42; 1000: 85 against 66); then into as many as make 1024 workgroups.
-    const int64_t want = rows >= 400 ? 1 : ceil_div(1024, rows);
+    const int64_t want = rows >= LP_WHOLE ? 1 : ceil_div(LP_PARTS, rows);
     p.per = (int)ceil_div(p.chunks, std::min(p.chunks, want));
     p.parts = (int)ceil_div(p.chunks, p.per);
     if (p.parts == 1 && k > 0 && p.chunks * LP_WG > LP_LDS_BLOCKS) {  // the blocks do not fit in LDS
@@ -621,10 +623,16 @@ static Plan plan_logprobs(int64_t rows, int V, int k)
     return p;
 }
 
+// Enough for these rows and for any fewer, and for shorter ones and fewer alternatives: of up to 399 rows, those that may be cut into
+// parts (r rows into fewer than 1024 + r of them), and of all where they are too long for LDS.
 size_t token_logprobs_workspace(int64_t rows, int V, int k)
 {
     if (rows < 1 || V < 1 || k < 0 || k > QADC_MAX_ALTERNATIVES) return 0;
-    return plan_logprobs(rows, V, k).bytes;
+    const int64_t chunks = plan_logprobs(rows, V, k).chunks, few = std::min(rows, LP_WHOLE - 1);
+    if (chunks == 1) return 256;
+    const bool all = k > 0 && chunks * LP_WG > LP_LDS_BLOCKS;
+    const int64_t parts = std::max(std::min(few * chunks, LP_PARTS + few), all ? 2 * rows : 0);
+    return align_up((size_t)parts * sizeof(Stats), 256) + (k > 0 ? (size_t)(all ? rows : few) * chunks * LP_WG * sizeof(uint32_t) : 0);
 }
 
 template <typename T, bool ALT>

@@ -320,3 +320,16 @@ def test_no_rows_and_refusals_of_the_binding():
                 lambda: Q.qadc_token_logprobs(x, tokens, 1, float("inf"))):
         with pytest.raises(Q.QadcError):
             bad()
+
+
+@pytest.mark.parametrize("k", [0, 20])
+@pytest.mark.parametrize("rows,V", [(400, 131072), (410, 60000), (1000, 20000), (5, 400000)])
+def test_a_workspace_for_a_batch_serves_its_smaller_batches(rows, V, k):
+    import paper_1704_07355_amd as Q
+    ws = torch.empty((Q.qadc_token_logprobs_workspace_bytes(rows, V, k),), dtype=torch.uint8, device=DEV)
+    x = make(rows, V, "bf16", 31)
+    for n in (rows, 399, 130, 3, 1):
+        if n > rows:
+            continue
+        got, want = Q.qadc_token_logprobs(x[:n], None, k, workspace=ws), Q.qadc_token_logprobs(x[:n], None, k)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), n

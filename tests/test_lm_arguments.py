@@ -146,3 +146,17 @@ def test_layer_norm_workspaces_grow_with_the_batch():
     for d in (1, 100, 300, 900, 2000, 4096, 4097, 16384, 16385, 100000):
         sizes = [Q.qadc_layer_norm_workspace_bytes(rows, d) for rows in [*range(0, 2100), *range(2100, 40000, 37), 1 << 20, 1 << 33]]
         assert sizes == sorted(sizes) and sizes[1] > 0, d
+
+
+def test_token_logprobs_workspaces_grow_with_the_call():
+    """What is asked for a call holds what is asked for one of fewer rows, tokens or alternatives."""
+    size = Q.qadc_token_logprobs_workspace_bytes
+    rows_of, V_of = [*range(1, 600), 1000, 1023, 1024, 1025, 5000], [*range(1, 600000, 4095), 10 ** 6, 8400000, 8400000 + 8192, 10 ** 7]
+    for k in (0, 1, 128):
+        for V in (1, 5000, 8185, 8186, 20000, 60000, 131072, 262144, 390000, 400000, 10 ** 7):
+            sizes = [size(rows, V, k) for rows in rows_of]
+            assert sizes == sorted(sizes), (V, k)
+            assert size(30, V, 0) <= size(30, V, 1) == size(30, V, 128)
+        for rows in (1, 2, 3, 100, 399, 400, 2000):
+            sizes = [size(rows, V, k) for V in V_of]
+            assert sizes == sorted(sizes), (rows, k)
