@@ -504,6 +504,9 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
  * Sums in float32.  A logit of -inf is a token that is masked out: p = 0, and it adds nothing to the entropy.
  * A row with nothing left has lse = -inf, entropy 0 and every log probability -inf.  A row that holds a NaN or +inf has
  * lse, entropy and log probabilities NaN; its alternatives are still ordered, a NaN before +inf.
+ * Log probabilities come from the difference to the row's largest logit, not from lse: they hold for large logits and scales too.
+ * Where scale * logits[v] passes float32's range lse is NaN (and with it the gradient); a logit further below the largest than
+ * 3.4e38 counts as masked out.
  *   logits [rows][ld] of `type`, V <= ld of them per row;  0 < scale <= 2e38 (the inverse of a temperature)
  *   tokens [rows][T] i32, 0 <= T <= QADC_MAX_R, NULL when T = 0: an entry outside [0, V) is an unused slot, its logp is 0
  *   k      0..QADC_MAX_ALTERNATIVES

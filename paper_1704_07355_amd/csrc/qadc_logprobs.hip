@@ -151,6 +151,14 @@ __device__ __forceinline__ uint32_t block_top(const T *row, int64_t chunk, int V
     return bits;
 }
 
+// Log probabilities of a row's logits: scale (logit - m) - log s, which is as near for large logits as for small ones (as
+// scale logit - lse those around 1000 were off by 6e-5), and is finite where scale m is not.
+struct Row {
+    float scale, m, log_s;
+    bool none;  // a mask has left nothing
+    __device__ __forceinline__ float log_p(float logit) const { return none ? -INFINITY : fmaf(scale, logit - m, -log_s); }
+};
+
 struct StatsLds {
     float m[LP_WG / WAVE], s[LP_WG / WAVE], w[LP_WG / WAVE];
 };
@@ -220,7 +228,7 @@ __device__ __forceinline__ void each_top(int64_t chunks, const uint32_t (&first)
 }
 // The k alternatives of a row; top_of(chunk) is the largest logit of this thread's block.
 template <int FIRST, typename T, typename F>
-__device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks, int k, float scale, float lse, bool none,
+__device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks, int k, Row of,
                                    uint32_t *top_idx, float *top_logp, AltLds &lds, const uint32_t (&first)[FIRST + 1], F top_of)
 {
     constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
@@ -349,7 +357,7 @@ __device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks
         for (uint32_t j = 0; j < n; ++j) rank += list[j] > key;
         if (rank < k) {
             top_idx[rank] = ~(uint32_t)key;
-            top_logp[rank] = none ? -INFINITY : scale * alt_logit(key) - lse;
+            top_logp[rank] = of.log_p(alt_logit(key));
         }
     }
     for (int i = (int)n + threadIdx.x; i < k; i += LP_WG) {  // V < k
@@ -379,19 +387,18 @@ template <typename T, bool ALT, int FIRST, typename L, typename F>
 __device__ __forceinline__ void write_row(const T *row, int64_t r, int V, int lead, int64_t chunks, Stats a, float scale,
                                           const Out &o, Given g, L &lds, const uint32_t (&first)[FIRST + 1], F top_of)
 {
-    const bool none = a.m == -INFINITY && a.s == 0.0f;  // a mask has left nothing
-    const float log_s = logf(a.s), lse = none ? -INFINITY : fmaf(scale, a.m, log_s);
+    const Row of = {scale, a.m, logf(a.s), a.m == -INFINITY && a.s == 0.0f};
     if (threadIdx.x == 0) {
-        if (o.lse) o.lse[r] = lse;
-        if (o.entropy) o.entropy[r] = none ? 0.0f : log_s - LN2 * a.w / a.s;
+        const float lse = fmaf(scale, a.m, of.log_s);  // (no float holds it: NaN, since -inf says that nothing is left)
+        if (o.lse) o.lse[r] = of.none ? -INFINITY : fabsf(lse) < INFINITY ? lse : NAN;
+        if (o.entropy) o.entropy[r] = of.none ? 0.0f : of.log_s - LN2 * a.w / a.s;
     }
     for (int t = threadIdx.x; t < o.nt; t += LP_WG) {
         if (t >= LP_WG) g = given(row, r, V, o, t);
-        o.logp[r * o.nt + t] = g.token < 0 ? 0.0f : none ? -INFINITY : scale * g.logit - lse;
+        o.logp[r * o.nt + t] = g.token < 0 ? 0.0f : of.log_p(g.logit);
     }
     if constexpr (ALT)
-        write_alternatives<FIRST>(row, V, lead, chunks, o.k, scale, lse, none, o.top_idx + r * o.k, o.top_logp + r * o.k, lds,
-                                  first, top_of);
+        write_alternatives<FIRST>(row, V, lead, chunks, o.k, of, o.top_idx + r * o.k, o.top_logp + r * o.k, lds, first, top_of);
 }
 
 // A workgroup per row.

@@ -333,3 +333,50 @@ def test_a_workspace_for_a_batch_serves_its_smaller_batches(rows, V, k):
             continue
         got, want = Q.qadc_token_logprobs(x[:n], None, k, workspace=ws), Q.qadc_token_logprobs(x[:n], None, k)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), n
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("rows,V", [(3, 900), (2, 131072), (420, 700)])
+@pytest.mark.parametrize("offset,scale", [(1000.0, 1.0), (-3000.0, 0.75), (100.0, 1e3)])
+def test_log_probabilities_do_not_take_on_the_offset(offset, scale, rows, V, type):
+    """x - lse is scale (logit - m) - log s: the difference of two logits, a product and a difference, however large both are."""
+    import paper_1704_07355_amd as Q
+    logits = (make(rows, V, "f32", 21) + offset).to(TYPES[type])
+    tokens = make_tokens(rows, V, 5, 22)
+    tokens[:, 4] = logits.argmax(1).to(torch.int32)
+    logp, _, _, top, top_logp = Q.qadc_token_logprobs(logits, tokens, 6, scale)
+    x = logits.double() * scale
+    m = x.max(1, keepdim=True).values
+    d = x - m
+    s = torch.exp(d).sum(1, keepdim=True)
+    p = torch.exp(d) / s
+    off = 6 * EPS * d.abs() + (V / 256 + 44) * EPS           # of an exponential and of the sum up to it, relative
+    tol_s = (p * off).sum(1, keepdim=True) + 4 * EPS * torch.log(s)
+    used = (tokens >= 0) & (tokens < V)
+    at = torch.where(used, tokens, 0).long()
+    dt = torch.gather(d, 1, at)
+    within(logp, torch.where(used, dt - torch.log(s), 0.0), tol_s + 4 * EPS * dt.abs(), "logp")
+    order = torch.sort(logits.double(), dim=1, descending=True, stable=True).indices[:, :6]
+    dt = torch.gather(d, 1, order)
+    assert torch.equal(top, order.to(torch.int32))
+    within(top_logp, dt - torch.log(s), tol_s + 4 * EPS * dt.abs(), "top_logp")
+
+
+@pytest.mark.parametrize("V", [300, 70000])
+def test_log_probabilities_where_the_scaled_logit_passes_a_float(V):
+    """A finite row whose scale * logit is no float32: the likeliest token has all, lse is NaN (not the -inf of an empty row),
+    and so is the gradient that would need it."""
+    import paper_1704_07355_amd as Q
+    for sign in (1.0, -1.0):
+        logits = -sign * torch.rand((4, V), generator=gen(V), device=DEV) + (0.0 if sign > 0 else -1000.0)
+        logits[:, 7] = 500.0 if sign > 0 else -500.0
+        logits[3] = -math.inf
+        tokens = torch.tensor([[7, 8]], device=DEV, dtype=torch.int32).expand(4, 2).contiguous()
+        logp, lse, H, top, top_logp = Q.qadc_token_logprobs(logits, tokens, 2, 1e38)
+        assert (logp[:3, 0] == 0).all() and (logp[:3, 1] == -math.inf).all() and not H.any()
+        assert (top[:3, 0] == 7).all() and (top_logp[:3, 0] == 0).all() and (top_logp[:3, 1] == -math.inf).all()
+        assert torch.isnan(lse[:3]).all() and lse[3] == -math.inf and (logp[3] == -math.inf).all()
+        dx = Q.qadc_token_logprobs_backward(logits, tokens, lse, H, torch.ones((4, 2), device=DEV), None, 1e38)
+        assert torch.isnan(dx[:3]).all() and not dx[3].any()
+        logp, lse, H, _, _ = Q.qadc_token_logprobs(logits, tokens, 0, 1e3)
+        assert (logp[:3, 0] == 0).all() and torch.isfinite(lse[:3]).all() and torch.isfinite(logp[:3]).all()
