@@ -7,7 +7,9 @@
 // The alternatives are the k largest under one 64-bit key: the logit's bits made monotone above, the complement of the token
 // below.  While the row streams by, only the largest logit of every block (32 logits of one thread) is kept.  The k-th largest of
 // the threads' largest logits bounds the k-th logit from below, since k different logits reach it; the few blocks that reach it
-// are read again, from the cache, and what reaches it is ordered.
+// are read again, from the cache, and what reaches it is ordered.  Where many logits are equal to the bound, or a mask leaves fewer
+// than k threads any, it is those above it, and the first of those equal to it in the row (131072 bfloat16 logits of which a mask
+// leaves five, 20 alternatives: 17 us; with all that reach the bound collected first 140, and 200 in a row, 50 of them, 374 for 24).
 //
 // Bound by memory where there are many rows: 4096 x 65536 bfloat16 86 us (537 MB at 6.2 TB/s), its gradient 192 (1.07 GB at
 // 5.6); by launches and round trips where there are few: 131072 logits with 20 alternatives 4 us for the parts and 10 for the
@@ -40,6 +42,7 @@ __device__ __forceinline__ uint32_t logit_bits(float logit)
     if (logit != logit) u = 0x7ffffffeu;  // (something is always above)
     return (int32_t)u < 0 ? ~u : u | 0x80000000u;
 }
+constexpr uint32_t MASKED = 0x007fffffu;  // of -inf, below every other logit
 // (logit descending, token ascending) as one number, larger first.
 __device__ __forceinline__ uint64_t alt_key(uint32_t bits, uint32_t token) { return (uint64_t)bits << 32 | (uint32_t)~token; }
 __device__ __forceinline__ float alt_logit(uint64_t key)
@@ -250,18 +253,20 @@ __device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks
     }
     if (above < k) atomicMin(&lds.bound, top);
     __syncthreads();
-    uint32_t bound = lds.bound;  // 0 where fewer than k threads have a logit: all of the row are candidates
-    // f(bits, token) for this thread's logits that reach `from`
-    const auto each = [&](uint32_t from, auto f) {
-        if (top < from) return;
+    // Masked tokens come last: where the bound is no higher than theirs, what is left is ordered and the first masked ones follow.
+    uint32_t bound = max(lds.bound, MASKED), from = max(bound, MASKED + 1);
+    // f(bits, token) for this thread's logits that reach `least`
+    const auto each = [&](uint32_t least, auto f) {
+        if (top < least) return;
         for (int64_t j = 0; j < chunks; ++j) {
-            if (top_of(j) < from) continue;
+            if (top_of(j) < least) continue;
             for (int u = 0; u < PACKS; ++u) {
                 const int64_t at = pack_at<T>(j, u, lead);
+                const typename Pack<T>::V x = load_edge(row, at, V, 0.0f);
+#pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (at + e < 0 || at + e >= V) continue;
-                    const uint32_t bits = logit_bits((float)row[at + e]);
-                    if (bits >= from) f(bits, (uint32_t)(at + e));
+                    const uint32_t bits = logit_bits((float)x[e]);
+                    if (bits >= least && at + e >= 0 && at + e < V) f(bits, (uint32_t)(at + e));
                 }
             }
         }
@@ -270,83 +275,100 @@ __device__ void write_alternatives(const T *row, int V, int lead, int64_t chunks
         const uint32_t slot = atomicAdd(&lds.count, 1u);
         if (slot < LP_LIST) lds.list[slot] = alt_key(bits, token);
     };
-    // The blocks that reach the bound are listed, then read by all threads, a pack each.
-    const uint32_t least = max(bound, 1u);
-    if (top >= least)
-        each_top<FIRST>(chunks, first, top_of, [&](int64_t j, uint32_t t) {
-            if (t < least) return;
-            const uint32_t slot = atomicAdd(&lds.block_count, 1u);
-            if (slot < LP_READ) lds.blocks[slot] = (uint32_t)j * LP_WG + threadIdx.x;
-        });
-    __syncthreads();
-    const uint32_t blocks = lds.block_count;
-    if (blocks <= LP_READ) {
-        for (uint32_t i = threadIdx.x; i < blocks * PACKS; i += LP_WG) {
-            const uint32_t block = lds.blocks[i / PACKS];
-            const int64_t at = (int64_t)(block / LP_WG) * LP_CHUNK + ((int64_t)(i % PACKS) * LP_WG + block % LP_WG) * N - lead;
-            const typename Pack<T>::V x = load_edge(row, at, V, 0.0f);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const uint32_t bits = logit_bits((float)x[e]);
-                if (bits >= least && at + e >= 0 && at + e < V) collect(bits, (uint32_t)(at + e));
-            }
-        }
-    } else {
-        each(least, collect);
-    }
-    __syncthreads();
-    uint32_t n = lds.count;
+    uint32_t n;
     int turn = 0;
-    if (n > LP_LIST) {
-        // Too many: the k-th logit itself, bit by bit where it is not the bound.  Those above it are fewer than k; of those
-        // equal to it the first in the row fill the list up.
-        const auto reach = [&](uint32_t from) {
-            uint32_t c = 0;
-            each(from, [&](uint32_t, uint32_t) { ++c; });
-            c = lane_value(wave_running_sum(c), 63);
-            return group_count(c, lds, turn++);
-        };
-        if (reach(bound + 1) >= (uint32_t)k) {
-            uint32_t kth = 0;
-            for (int b = 31; b >= 0; --b) {
-                const uint32_t trial = kth | 1u << b;
-                if (trial <= bound || reach(trial) >= (uint32_t)k) kth = trial;
+    for (;;) {
+        // The blocks that reach `from` are listed, then read by all threads, a pack each.
+        if (top >= from)
+            each_top<FIRST>(chunks, first, top_of, [&](int64_t j, uint32_t t) {
+                if (t < from) return;
+                const uint32_t slot = atomicAdd(&lds.block_count, 1u);
+                if (slot < LP_READ) lds.blocks[slot] = (uint32_t)j * LP_WG + threadIdx.x;
+            });
+        __syncthreads();
+        const uint32_t blocks = lds.block_count;
+        if (blocks <= LP_READ) {
+            for (uint32_t i = threadIdx.x; i < blocks * PACKS; i += LP_WG) {
+                const uint32_t block = lds.blocks[i / PACKS];
+                const int64_t at = (int64_t)(block / LP_WG) * LP_CHUNK + ((int64_t)(i % PACKS) * LP_WG + block % LP_WG) * N - lead;
+                const typename Pack<T>::V x = load_edge(row, at, V, 0.0f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const uint32_t bits = logit_bits((float)x[e]);
+                    if (bits >= from && at + e >= 0 && at + e < V) collect(bits, (uint32_t)(at + e));
+                }
             }
-            bound = kth;
+        } else if (from > bound) {
+            each(from, collect);
         }
+        __syncthreads();
+        n = lds.count;
+        if (from > bound || (blocks <= LP_READ && n <= LP_LIST)) break;
+        // Too many reach the bound, as where it is the value of many tokens (a mask of the type's lowest value, a clipped row): those
+        // above it alone, and of those equal to it the first in the row.
+        from = bound + 1;
+        __syncthreads();
+        if (threadIdx.x == 0) lds.count = lds.block_count = 0;
+        __syncthreads();
+    }
+    if (n > LP_LIST) {
+        // Too many above the bound, too: the k-th logit itself, bit by bit.  Those above it are fewer than k.
+        uint32_t kth = 0;
+        for (int b = 31; b >= 0; --b) {
+            const uint32_t trial = kth | 1u << b;
+            uint32_t c = 0;
+            if (trial > bound) {
+                each(trial, [&](uint32_t, uint32_t) { ++c; });
+                c = group_count(lane_value(wave_running_sum(c), 63), lds, turn++);
+            }
+            if (trial <= bound || c >= (uint32_t)k) kth = trial;
+        }
+        bound = kth;
+        __syncthreads();
         if (threadIdx.x == 0) lds.count = 0;
         __syncthreads();
         each(bound + 1, collect);
         __syncthreads();
         n = lds.count;
-        for (int64_t v0 = 0; v0 < V && n < (uint32_t)k; v0 += LP_WG) {
-            const int64_t v = v0 + threadIdx.x;
-            const bool is = v < V && logit_bits((float)row[v]) == bound;
-            const unsigned long long mask = __ballot(is);
-            const uint32_t total = group_count((uint32_t)__popcll(mask), lds, turn);
-            uint32_t slot = n + rank_in_mask(mask);
+    }
+    for (int64_t j = 0; j < chunks && n < (uint32_t)k; ++j) {
+        const bool here = top_of(j) >= bound;
+        if (!__syncthreads_or(here)) continue;
+        for (int u = 0; u < PACKS && n < (uint32_t)k; ++u) {
+            const int64_t at = pack_at<T>(j, u, lead);
+            uint32_t equal = 0;
+            if (here && at < V) {
+                const typename Pack<T>::V x = load_edge(row, at, V, 0.0f);
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (logit_bits((float)x[e]) == bound && at + e >= 0 && at + e < V) equal |= 1u << e;
+            }
+            const uint32_t mine = (uint32_t)__popc(equal), running = wave_running_sum(mine);
+            const uint32_t total = group_count(lane_value(running, 63), lds, turn);
+            uint32_t slot = n + running - mine;
             for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) slot += lds.counts[turn & 1][w];
-            if (is && slot < (uint32_t)k) lds.list[slot] = alt_key(bound, (uint32_t)v);
+            for (; equal && slot < (uint32_t)k; equal &= equal - 1)
+                lds.list[slot++] = alt_key(bound, (uint32_t)(at + __ffs((int)equal) - 1));
             n = min(n + total, (uint32_t)k);
             ++turn;
         }
-        __syncthreads();
     }
+    __syncthreads();
     const uint64_t *list = lds.list;
     if (n > LP_WG) {
         // Too many to compare each with each: the k-th key, bit by bit (no two are equal, so k of them reach it).
-        uint64_t from = 0;
+        uint64_t kth = 0;
         for (int b = 63; b >= 0; --b) {
-            const uint64_t trial = from | 1ull << b;
+            const uint64_t trial = kth | 1ull << b;
             uint32_t c = 0;
             for (uint32_t i = 0; i < n; i += LP_WG)
                 c += (uint32_t)__popcll(__ballot(i + threadIdx.x < n && lds.list[min(i + threadIdx.x, n - 1)] >= trial));
-            if (group_count(c, lds, turn++) >= (uint32_t)k) from = trial;
+            if (group_count(c, lds, turn++) >= (uint32_t)k) kth = trial;
         }
         if (threadIdx.x == 0) lds.count = 0;
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < n; i += LP_WG)
-            if (lds.list[i] >= from) lds.kept[atomicAdd(&lds.count, 1u)] = lds.list[i];
+            if (lds.list[i] >= kth) lds.kept[atomicAdd(&lds.count, 1u)] = lds.list[i];
         __syncthreads();
         n = (uint32_t)k;
         list = lds.kept;

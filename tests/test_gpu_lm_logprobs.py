@@ -380,3 +380,46 @@ def test_log_probabilities_where_the_scaled_logit_passes_a_float(V):
         assert torch.isnan(dx[:3]).all() and not dx[3].any()
         logp, lse, H, _, _ = Q.qadc_token_logprobs(logits, tokens, 0, 1e3)
         assert (logp[:3, 0] == 0).all() and torch.isfinite(lse[:3]).all() and torch.isfinite(logp[:3]).all()
+
+
+def usable_rows(rows, V, type, which, lowest):
+    """Logits of which a grammar leaves few, or many of one value: (logits, the place of what is left)."""
+    x = make(rows, V, type, 51)
+    t = torch.arange(V, device=DEV)
+    left = {"five": (t % (V // 5)) == 17, "range of 200": (t >= V // 3) & (t < V // 3 + 200),
+            "range of 2000": (t >= V // 2 + 1) & (t < V // 2 + 2001), "first token": t == 0, "last token": t == V - 1,
+            # of every workgroup's worth of logits the same few threads': more of them than a list holds
+            "a few threads'": (t // 8) % 256 < 20}[which]
+    return torch.where(left, x, torch.finfo(TYPES[type]).min if lowest else -math.inf).to(TYPES[type])
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("lowest", [False, True])
+@pytest.mark.parametrize("which", ["five", "range of 200", "range of 2000", "first token", "last token", "a few threads'"])
+@pytest.mark.parametrize("rows,V", [(1, 131072), (2, 60000), (401, 60000), (3, 500)])
+def test_alternatives_of_masked_rows(rows, V, which, lowest, type):
+    import paper_1704_07355_amd as Q
+    if V < 10000 and which.startswith("range of 2000"):
+        V = 5000
+    x = usable_rows(rows, V, type, which, lowest)
+    for k in (50, 128):
+        check(Q.qadc_token_logprobs(x, None, k), x, None, k, 1.0)
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+def test_alternatives_of_rows_cut_off_below_and_above(type):
+    """Many logits of one value where the k-th lies: the first of them in the row are taken, wherever they begin."""
+    import paper_1704_07355_amd as Q
+    for rows, V in ((1, 131072), (401, 60000)):
+        x = make(rows, V, type, 52)
+        above = torch.clamp(x, max=2.0)
+        below = torch.where(torch.arange(V, device=DEV) < V // 2, x - 100.0, 3.0).to(TYPES[type])
+        below[:, V // 2 + 100::V // 64] = 4.0
+        odd = below.clone()
+        odd[:, 3] = math.nan
+        for k in (20, 128):
+            for y in (above, below):
+                check(Q.qadc_token_logprobs(y, None, k), y, None, k, 1.0)
+            top = Q.qadc_token_logprobs(odd, None, k)[3]
+            want = torch.sort(odd.double(), dim=1, descending=True, stable=True).indices[:, :k]
+            assert torch.equal(top, want.to(torch.int32))
