@@ -168,11 +168,12 @@ struct StatsLds {
 struct AltLds {
     uint64_t list[LP_LIST];
     uint64_t kept[QADC_MAX_ALTERNATIVES];
-    uint32_t tops[LP_WG];
+    __attribute__((aligned(16))) uint32_t tops[LP_WG];  // read four at a time
     uint32_t blocks[LP_READ];
     uint32_t counts[2][LP_WG / WAVE];
     uint32_t count, block_count, bound;
 };
+static_assert(alignof(AltLds) == 16, "the largest logits are read 16 bytes at a time");
 struct NoLds {};
 
 // The threads' statistics joined, in every thread.
