@@ -8,10 +8,14 @@
 // groups of a tile (4, 2 or 1) or, of groups beyond 128 inputs, one group.  Outputs and inputs beyond N and K are zero nibbles
 // with scale 0.
 //
-// The product.  A nibble q put into the mantissa of 16 is the 16-bit number 16 + q, exactly: no conversion, one shift and one
-// and-or for a pair.  The matrix units multiply these with x (float32 x as the sum of three bfloat16 numbers) and, once for all
-// outputs, a column of ones with x; with p and t the two sums over a group, the group adds s (p - (16 + z) t) to the output.
-//
+// The product.  Of a 16-bit x: a nibble q put into the mantissa of 16 is the 16-bit number 16 + q, exactly: no conversion, one shift
+// and one and-or for a pair.  The matrix units multiply these with x and, once for all outputs, a column of ones with x; with p and
+// t the two sums over a group, the group adds s (p - (16 + z) t) to the output.  The sums are about ten times the result's size, which
+// the rounding of a 16-bit y hides and that of a float32 would not.  So a float32 x, the sum of three bfloat16 numbers, is multiplied
+// with q - z itself, a whole number that a bfloat16 holds: 24 vector instructions for 8 weights of each lane instead of 8.  Up to
+// four rows have their three parts in three rows of a matrix instruction, of whose 16 they need no more (one row of 131072 x 4096
+// 68 us, 91 with an instruction for each part; off by the sums' size, it was 75).
+
 // Bound by the weights' bytes for a few rows: one row of 131072 x 4096 bfloat16 49 us (277 MB at 5.6 TB/s), of 4096 x 4096
 // binary16 5.2, a launch and a round trip; beyond 16 rows by vector instructions (unpacking, 8 for 8 weights of each lane, and
 // what follows a group) and by x, which every workgroup brings into LDS: 24 rows of 10007 x 5000 in groups of 32 23 us, 64 rows of
@@ -115,6 +119,23 @@ __device__ __forceinline__ bits16x8 weights8(unsigned v, unsigned sixteen)
     return w;
 }
 
+// The eight weights of a dword as q - z, whole numbers of eight bits and a sign at most, which a bfloat16 holds.
+__device__ __forceinline__ bits16x8 weights8_less(unsigned v, float zero)
+{
+    unsigned even = v & 0x0f0f0f0fu, odd = v >> 4 & 0x0f0f0f0fu;
+    asm("" : "+v"(even), "+v"(odd));  // (bytes, which have a conversion of their own, not bit fields of v to be taken out first)
+    const auto less = [&](unsigned bytes, int at) { return __float_as_uint((float)(bytes >> (8 * at) & 0xffu) - zero); };
+    const auto pair = [&](unsigned bytes, int at) {  // the upper halves of the two float32
+        return __builtin_amdgcn_perm(less(bytes, at + 2), less(bytes, at), 0x07060302u);
+    };
+    bits16x8 w;
+    w[0] = pair(even, 0);
+    w[1] = pair(odd, 0);
+    w[2] = pair(even, 1);
+    w[3] = pair(odd, 1);
+    return w;
+}
+
 template <bool HALF>
 __device__ __forceinline__ f32x4 mfma16(bits16x8 a, bits16x8 b, f32x4 c)
 {
@@ -176,12 +197,12 @@ constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's
 // A block of NT x 16 outputs and up to 4 MR MT rows of x: `split` wavefronts, each every split-th tile of the inputs; a workgroup
 // has as many blocks as it has wavefronts for, and brings x into LDS for all of them.  Of a matrix instruction's 16 rows,
 // 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
-// others repeat them.  STEPS: instructions per group.  AGAIN: there are further rows, whose workgroups read the same weights.
+// others repeat them, or hold the parts of a float32 (SPREAD).  STEPS: instructions per group.  AGAIN: there are further rows, whose workgroups read the same weights.
 template <typename T, int STEPS, int MR, int MT, int NT, int THREADS, bool AGAIN>
 __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
 {
     constexpr int DEPTH = 4 / NT, PER = 4 / STEPS, ROWS = 4 * MR * MT, PARTS = Inputs<T>::PARTS;
-    constexpr bool HALF = Inputs<T>::HALF;
+    constexpr bool HALF = Inputs<T>::HALF, LESS = PARTS == 3, SPREAD = LESS && MR == 1;
     constexpr int FLY = sizeof(T) == 4 ? 2 : 4;
     // Four groups one after the other, each done before the next is begun where more rows share the registers (64 rows of
     // 131072 x 4096, groups of 32: 203 -> 184 us); two groups of 64 are a loop there (32 rows of 16384 x 16384 60 us, 63 unrolled).
@@ -204,7 +225,7 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int i = n & 3, m = t * 4 * MR + (n >> 2) * MR + (i < MR ? i : 0);
-        at_x[t] = min(m, rows - 1) * stride + 8 * j;
+        at_x[t] = (min(m, rows - 1) + (SPREAD ? min(i, PARTS - 1) * rows : 0)) * stride + 8 * j;
     }
     const char *weights[NT], *scales[NT], *zeros[NT];  // (the same in all lanes)
 #pragma unroll
@@ -299,20 +320,28 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
 #pragma unroll UNROLL
         for (int g = 0; g < PER; ++g, from += 32 * STEPS) {
             f32x4 p[MT][NT], one[MT];
+            const auto zero = [&](int u, float more) {  // (what the nibbles are more than they stand for)
+                uint8_t z;
+                __builtin_memcpy(&z, &zb[u], 1);
+                return a.has_zeros ? more + (float)z : more + 8.0f;
+            };
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 bits16x8 w[NT];
 #pragma unroll
-                for (int u = 0; u < NT; ++u) w[u] = weights8<HALF>(q[u][s], sixteen);
+                for (int u = 0; u < NT; ++u) {
+                    if constexpr (LESS) w[u] = weights8_less(q[u][s], zero(u, 0.0f));
+                    else w[u] = weights8<HALF>(q[u][s], sixteen);
+                }
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int part_of = 0; part_of < PARTS; ++part_of) {
+                    for (int part_of = 0; part_of < (SPREAD ? 1 : PARTS); ++part_of) {
                         const bits16x8 in =
                             *reinterpret_cast<const bits16x8 *>(from + part_of * rows * stride + at_x[t] + 32 * s);
                         const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
                         const bool more = s + part_of > 0;
-                        one[t] = mfma16<HALF>(in, ones, more ? one[t] : none);
+                        if constexpr (!LESS) one[t] = mfma16<HALF>(in, ones, more ? one[t] : none);
 #pragma unroll
                         for (int u = 0; u < NT; ++u) p[t][u] = mfma16<HALF>(in, w[u], more ? p[t][u] : none);
                     }
@@ -320,14 +349,17 @@ __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *_
 #pragma unroll
             for (int u = 0; u < NT; ++u) {
                 uint16_t bits;
-                uint8_t z;
                 __builtin_memcpy(&bits, &sb[u], 2);
-                __builtin_memcpy(&z, &zb[u], 1);
-                const float sc = scale4(bits, a.stype), zp = a.has_zeros ? 16.0f + (float)z : 24.0f;
+                const float sc = scale4(bits, a.stype), zp = zero(u, 16.0f);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int i = 0; i < MR; ++i) sum[t][u][i] = fmaf(sc, fmaf(-zp, one[t][i], p[t][u][i]), sum[t][u][i]);
+                    for (int i = 0; i < MR; ++i) {
+                        const float of = SPREAD ? p[t][u][2] + p[t][u][1] + p[t][u][0]
+                                         : LESS ? p[t][u][i]
+                                                : fmaf(-zp, one[t][i], p[t][u][i]);
+                        sum[t][u][i] = fmaf(sc, of, sum[t][u][i]);
+                    }
                 if constexpr (PER == 4) {
                     q[u] = __builtin_shufflevector(q[u], q[u], 1, 2, 3, 0);
                     sb[u] = u32x2{sb[u][0] >> 16 | sb[u][1] << 16, sb[u][1] >> 16};

@@ -168,3 +168,39 @@ def test_refusals_of_the_binding():
         Q.qadc_pack_weights4(codes, scales.float(), z, 100, 32)
     with pytest.raises(Q.QadcError):  # a group of 48
         Q.qadc_pack_weights4(codes, scales[:, :3].contiguous(), None, 100, 48)
+
+
+@pytest.mark.parametrize("offset", [0.0, 3.0])
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True), (128, False), (512, True)])
+@pytest.mark.parametrize("M,N,K", [(1, 1024, 4096), (3, 20000, 512), (12, 1024, 4096), (30, 700, 512), (40, 600, 2048)])
+def test_float32_products_are_as_exact_as_a_sum_in_order(M, N, K, group, zeros, offset):
+    """A float32 sum of K products in their order, of which the n-th partial sum has the size sqrt(n), is off by e sqrt(K / 6) of the
+    sum's size: K roundings, each evenly spread over e = 2^-24 of a partial sum at most, whose squares add up to K^2 / 6 e^2.  What a
+    float32 x is multiplied with is no less exact than that."""
+    import paper_1704_07355_amd as Q
+    g = gen(M + K)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+    scales = (0.004 + 0.008 * torch.rand((N, K // group), generator=g, device=DEV)).half()
+    z = torch.randint(5, 12, (N, K // group), generator=g, device=DEV, dtype=torch.uint8) if zeros else None
+    x = torch.randn((M, K), generator=g, device=DEV) + offset
+    y = Q.qadc_linear4(Q.qadc_pack_weights4(codes, scales, z, K, group), x)
+    q = torch.stack((codes & 15, codes >> 4), -1).reshape(N, K).double()
+    of = torch.arange(K, device=DEV) // group
+    w = ((q - (8.0 if z is None else z.double()[:, of])) * scales.double()[:, of]).t().contiguous()
+    want = x.double() @ w
+    off = ((y.double() - want).square().mean() / want.square().mean()).sqrt().item()
+    assert off <= EPS * (K / 6) ** 0.5, (off, EPS * (K / 6) ** 0.5)
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("M", [4096 + 3, 2 * 4096 + 20])
+def test_rows_beyond_one_slab(M, type):
+    """More rows than one launch takes: the rows on both sides of each border, rows apart, a last slab of another kernel."""
+    import paper_1704_07355_amd as Q
+    N, K = 33, 65
+    codes, scales, z = make(N, K, 32, type, True, 61)
+    x = torch.randn((M, K), generator=gen(62), device=DEV).to(TYPES[type])
+    w = Q.qadc_pack_weights4(codes, scales, z, K, 32)
+    out = apart(torch.zeros((M, N), dtype=TYPES[type], device=DEV), N + 4, 1)
+    check(Q.qadc_linear4(w, apart(x, K + 3, 1), out=out), x, codes, scales, z, K, 32, type)
+    assert torch.isnan(torch.as_strided(out, (M, N + 4), (N + 4, 1))[:-1, N:]).all()
