@@ -492,7 +492,7 @@ int qadc_pack_weights4(const uint8_t *codes, const void *scales, int stype, cons
  * For every type of x the weights enter exactly; x enters exactly too (a float32 x as the sum of three
  * bfloat16 numbers, of which the last may be lost where |x| < 1e-33).  A float32 x is multiplied with q - z; of a 16-bit
  * one the zero points are taken off after the products with 16 + q, whose float32 sums over a group must stay in range
- * (|x| up to 1e34) and leave an error well below y's own rounding.  A row of x that holds an infinity or a NaN gives NaN
+ * (|x| up to 5e33) and leave an error well below y's own rounding.  A row of x that holds an infinity or a NaN gives NaN
  * for every output (or an infinity).
  */
 int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, int64_t M, const float *bias, void *y,

@@ -166,3 +166,15 @@ def test_weights_whose_product_passes_a_float():
     check(Q.qadc_neighbour_mix(ids, tiny, values, tokens, lm, 0.5, 2.0 ** 60, step), ids, tiny, values, tokens, lm, 0.5, 2.0 ** 60, step)
     far = torch.tensor([[-3e38, 3e38, 0.0, 1e38]], device=DEV).expand(3, 4).contiguous()
     check(Q.qadc_neighbour_mix(ids, far, values, tokens, lm, 0.5, 2.0 ** -126, None), ids, far, values, tokens, lm, 0.5, 2.0 ** -126, None)
+
+
+@pytest.mark.parametrize("rows,R,T", [(2047, 100, 20), (2047, 256, 64), (3000, 300, 20), (3000, 100, 65), (2500, 1024, 3)])
+def test_rows_alone_give_the_bits_they_give_among_others(rows, R, T):
+    import paper_1704_07355_amd as Q
+    for kind in ("u8", "f32"):
+        ids, dist, values, tokens, lm, step = make(rows, R, T, 5000, kind, 8)
+        want = Q.qadc_neighbour_mix(ids, dist, values, tokens, lm, 0.2, 0.02, step)
+        for r in (0, 1, rows - 1):
+            one = slice(r, r + 1)
+            got = Q.qadc_neighbour_mix(ids[one], dist[one], values, tokens[one], lm[one], 0.2, 0.02, None if step is None else step[one])
+            assert all(torch.equal(p[0], q[r]) for p, q in zip(got, want))

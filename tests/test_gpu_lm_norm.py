@@ -245,3 +245,16 @@ def test_a_workspace_for_a_batch_serves_its_smaller_batches(rows, d):
         part = dy[:n], x[:n], w, mean[:n], rstd[:n]
         got, want = Q.qadc_layer_norm_backward(*part, workspace=ws), Q.qadc_layer_norm_backward(*part)
         assert all(torch.equal(p, q) for p, q in zip(got, want)), n
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("rows,d", [(3000, 100), (2051, 260), (700, 1111), (1100, 4096), (300, 8000), (270, 12000), (40, 20001)])
+def test_rows_alone_give_the_bits_they_give_among_others(rows, d, type):
+    import paper_1704_07355_amd as Q
+    x, w, b, dy = _inputs(rows, d, type, 42, "f32")
+    y, mean, rstd = Q.qadc_layer_norm(x, w, b)
+    dx, _, _ = Q.qadc_layer_norm_backward(dy, x, w, mean, rstd)
+    for r in (0, 1, rows // 2, rows - 1):
+        one = slice(r, r + 1)
+        assert all(torch.equal(p[0], q[r]) for p, q in zip(Q.qadc_layer_norm(x[one], w, b), (y, mean, rstd)))
+        assert torch.equal(Q.qadc_layer_norm_backward(dy[one], x[one], w, mean[one], rstd[one])[0][0], dx[r])
