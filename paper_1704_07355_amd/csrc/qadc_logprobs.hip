@@ -11,8 +11,8 @@
 // than k threads any, it is those above it, and the first of those equal to it in the row (131072 bfloat16 logits of which a mask
 // leaves five, 20 alternatives: 17 us; with all that reach the bound collected first 140, and 200 in a row, 50 of them, 374 for 24).
 //
-// Bound by memory where there are many rows: 4096 x 65536 bfloat16 86 us (537 MB at 6.2 TB/s), its gradient 192 (1.07 GB at
-// 5.6); by launches and round trips where there are few: 131072 logits with 20 alternatives 4 us for the parts and 10 for the
+// Bound by memory where there are many rows: 4096 x 65536 bfloat16 86 us (537 MB at 6.2 TB/s), its gradient 171 (1.07 GB at
+// 6.3); by launches and round trips where there are few: 131072 logits with 20 alternatives 4 us for the parts and 10 for the
 // join, 64 x 50021 with 50 alternatives 5 and 13.
 
 #include <algorithm>
@@ -519,8 +519,8 @@ __device__ __forceinline__ float exp_of(float t)
 }
 
 // A workgroup per `per` chunks of a row: first every logit's own share, then the given tokens', each once.  STREAM: stores past
-// the caches, for gradients that they do not hold (4096 x 65536 bfloat16 208 -> 198 us, 4096 x 50021 190 -> 170; 500 x 131072,
-// which they hold, would go from 47 to 53).
+// the caches, for gradients that they do not hold (4096 x 65536 bfloat16 176 -> 171 us, 4096 x 50021 157 -> 130; of 262 MB 1000 x
+// 131072 would go from 78 to 85, 4096 x 32000 from 101 to 81).
 template <typename T, bool STREAM>
 __global__ __launch_bounds__(LP_WG) void logprobs_grad_kernel(const T *logits, int64_t ld, int64_t rows, int V, float scale,
                                                               int parts, int per, const int32_t *__restrict__ tokens, int nt,
@@ -721,7 +721,10 @@ int token_logprobs_backward(const void *logits, int64_t ld, int type, int64_t ro
     // (where rows begin off 16 bytes, up to seven logits into their first pack)
     const bool even = (uintptr_t)dlogits % 16 == 0 && (size_t)ldd * type_bytes(type) % 16 == 0;
     const int64_t chunks = ceil_div((int64_t)V + (even ? 0 : 7), LP_CHUNK);
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));  // chunks a workgroup
+    // Chunks a workgroup: one, where a row has more than two and few tokens are given (4096 x 65536 bfloat16 with one token 171 us, 192
+    // with four chunks; with 16 173 for 194); up to four elsewhere: every workgroup goes through the tokens (64 of them 197 us for 212,
+    // 1000 x 50021 with 1000 1060 for 2200), and of two chunks the second is rarely full (4096 x 10000 32 us for 40).
+    const int64_t most = T <= 16 && chunks > 2 ? 1 : std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));
     const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
     const dim3 grid((unsigned)std::min<int64_t>(rows * parts, 1 << 20));
     const int nt = T;
