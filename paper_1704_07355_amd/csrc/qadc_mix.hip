@@ -159,10 +159,10 @@ int neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const f
     n = std::min<int64_t>(n, 0xFFFFFFFF);  // (the padding is no id)
     const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
     const float log_keep = log1pf(-lambda), log_lambda = logf(lambda);
-    // Rows of few neighbours and tokens have a wavefront each, where there are enough of them: 4096 rows of 100 neighbours and 20 tokens
-    // 8.7 us (14.7 with a workgroup of 256 each), of 256 and 64 20.1 (20.6); 2048 rows of 128 and 32 7.7 (9.1), but of 256 and 64 16.4
-    // (12.9), and 1024 of 128 and 32 6.7 (6.0).
-    const int threads = R <= 256 && T <= 64 && rows >= (R * T > 4096 ? 4096 : 2048) ? WAVE : 256;
+    // Rows of few neighbours and tokens have a wavefront each, where there are enough of them: 2048 rows of 128 neighbours and 32 tokens
+    // 7.7 us (9.1 with a workgroup of 256 each), 4096 of 100 and 20 8.7 (14.7), of 256 and 64 20.1 (20.6); but 2048 of 256 and 64
+    // 16.4 (12.9), 3000 of 200 and 40 15.4 (14.6), and 1024 of 128 and 32 6.7 (6.0).
+    const int threads = R <= 256 && T <= 64 && rows >= (R > 128 && T > 16 ? 4096 : 2048) ? WAVE : 256;
     int at_once = 1;
     while (at_once < T && at_once < threads) at_once *= 2;
 #define MIX(D_, THREADS_)                                                                                                       \
