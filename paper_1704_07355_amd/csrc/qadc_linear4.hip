@@ -498,18 +498,15 @@ static int linear4_launch(Args4 a, const void *x, void *y, hipStream_t st)
     return QADC_OK;
 }
 
-// Sixteen wavefronts a workgroup (131072 x 4096, bfloat16: one row 59 -> 54 us, 16 rows 68 -> 59; the large x of 32 rows of
-// 16384 inputs is brought in half as often: 82 -> 62), unless a last round of workgroups would leave much of the chip idle:
-// there eight (one row of 40000 x 8000 37 us against 47, 24 rows of 10007 x 5000 28 against 32).  A float32 x, in three parts,
-// needs the room (12 rows of 20000 x 2000: 22 us against 26).
+// Sixteen wavefronts a workgroup (131072 x 4096, bfloat16: one row 59 us with eight, 55 with sixteen, 16 rows 63 and 59; the large x
+// of 32 rows of 16384 inputs is brought in half as often: 77 and 56; 24 rows of 10007 x 5000 25 and 22), unless the last round of
+// workgroups would leave much of the chip idle: there eight (one row of 40000 x 8000 35 us against 44, of float32 48 against 63).
 template <typename T, int STEPS, int MR, int MT, bool AGAIN = false>
 static int linear4_sized(const Args4 &a, const void *x, void *y, hipStream_t st)
 {
-    if constexpr (sizeof(T) == 2) {
-        const int64_t blocks = ceil_div(a.s.blocks, 2), row_blocks = ceil_div(a.M, 4 * MR * MT);
-        if (cut4(blocks, row_blocks, a.s.tiles, 2, 8).cost < cut4(blocks, row_blocks, a.s.tiles, 2, 16).cost)
-            return linear4_launch<T, STEPS, MR, MT, 2, 512, AGAIN>(a, x, y, st);
-    }
+    const int64_t blocks = ceil_div(a.s.blocks, 2), row_blocks = ceil_div(a.M, 4 * MR * MT);
+    if (cut4(blocks, row_blocks, a.s.tiles, 2, 8).cost < cut4(blocks, row_blocks, a.s.tiles, 2, 16).cost)
+        return linear4_launch<T, STEPS, MR, MT, 2, 512, AGAIN>(a, x, y, st);
     return linear4_launch<T, STEPS, MR, MT, 2, 1024, AGAIN>(a, x, y, st);
 }
 
@@ -527,8 +524,11 @@ static int linear4_rows(Args4 a, const T *x, T *y, hipStream_t st)
         if (a.M > 32) rc = linear4_sized<T, STEPS, 4, 2, true>(a, xs, ys, st);
         else if (a.M > 16) rc = linear4_sized<T, STEPS, 4, 2>(a, xs, ys, st);
         else if (a.M > 4) rc = linear4_sized<T, STEPS, 4, 1>(a, xs, ys, st);
+        // Up to four rows: two blocks a wavefront, or one where there are few outputs, for all the wavefronts that they are worth (one
+        // row of 131072 x 4096 bfloat16 55.5 us with one, 51.8 with two, of 24576 x 16384 45.7 and 39.6; of 16384 x 16384 27.8 and
+        // 29.0, of 4096 x 16384 10.4 and 14.7, four of 4096 x 4096 binary16 in groups of 32 6.6 and 7.8).
         else if (a.s.blocks >= 1024) rc = linear4_sized<T, STEPS, 1, 1>(a, xs, ys, st);
-        else rc = linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st);  // few outputs: all wavefronts that they are worth
+        else rc = linear4_launch<T, STEPS, 1, 1, 1, 1024>(a, xs, ys, st);
         if (rc != QADC_OK) return rc;
     }
     return QADC_OK;
