@@ -528,6 +528,7 @@ size_t qadc_token_logprobs_workspace_bytes(int64_t rows, int V, int k);
  *     dlogits[v] = scale * (sum_t dlogp[t] (1 if tokens[t] = v, else 0, - p[v]) - dentropy p[v] (x[v] - lse + entropy))
  * in float32, rounded once to `type`; unused slots give nothing, a token given twice gives both its shares.  A masked
  * token (logit -inf) has p = 0; a row with nothing left (lse = -inf) gets zeros.
+ * p = exp(x - lse) is as exact as lse: |lse| 2^-24 relative.
  *   lse, entropy [rows] f32 as qadc_token_logprobs wrote them (entropy is read only with dentropy)
  *   dlogp [rows][T] f32 (NULL when T = 0);  dentropy [rows] f32 or NULL
  *   dlogits [rows][ldd] of `type` (output; may be logits when ldd == ld)

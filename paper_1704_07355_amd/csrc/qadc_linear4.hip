@@ -12,14 +12,15 @@
 // and one and-or for a pair.  The matrix units multiply these with x and, once for all outputs, a column of ones with x; with p and
 // t the two sums over a group, the group adds s (p - (16 + z) t) to the output.  The sums are about ten times the result's size, which
 // the rounding of a 16-bit y hides and that of a float32 would not.  So a float32 x, the sum of three bfloat16 numbers, is multiplied
-// with q - z itself, a whole number that a bfloat16 holds: 24 vector instructions for 8 weights of each lane instead of 8.  Up to
-// four rows have their three parts in three rows of a matrix instruction, of whose 16 they need no more (one row of 131072 x 4096
-// 68 us, 91 with an instruction for each part; off by the sums' size, it was 75).
+// with q - z itself, a whole number that a bfloat16 holds: 24 vector instructions for 8 weights of each lane instead of 8 (16 rows
+// of 4096 x 4096 13.7 us, 12.9 with 16 + q).  Up to four rows have their three parts in three rows of a matrix instruction, of whose
+// 16 they need no more (one row of 131072 x 4096 68 us; with an instruction for each part 91, and 75 with 16 + q).
 
 // Bound by the weights' bytes for a few rows: one row of 131072 x 4096 bfloat16 49 us (277 MB at 5.6 TB/s), of 4096 x 4096
 // binary16 5.2, a launch and a round trip; beyond 16 rows by vector instructions (unpacking, 8 for 8 weights of each lane, and
-// what follows a group) and by x, which every workgroup brings into LDS: 24 rows of 10007 x 5000 in groups of 32 23 us, 64 rows of
-// 131072 x 4096 135 us.
+// what follows a group) and by x, which every workgroup brings into LDS: 24 rows of 10007 x 5000 in groups of 32 22 us.  (These are
+// the kernel's times by the profiler; figures elsewhere in this file are calls one after the other: 51, 7 and 21 us.)  64 rows of
+// 131072 x 4096 141 us, 2048 of 4096 x 4096 132 (0.52 P operations/s: each 32 rows unpack the weights anew).
 
 #include <algorithm>
 #include <mutex>
@@ -197,7 +198,8 @@ constexpr int X_PAD = 8;  // 16 bytes between the rows of x in LDS: a fragment's
 // A block of NT x 16 outputs and up to 4 MR MT rows of x: `split` wavefronts, each every split-th tile of the inputs; a workgroup
 // has as many blocks as it has wavefronts for, and brings x into LDS for all of them.  Of a matrix instruction's 16 rows,
 // 4 q + i, the first MR of every four are rows of x (MR = 1 for up to four rows: a quarter of the work behind the products); the
-// others repeat them, or hold the parts of a float32 (SPREAD).  STEPS: instructions per group.  AGAIN: there are further rows, whose workgroups read the same weights.
+// others repeat them, or hold the parts of a float32 (SPREAD).  STEPS: instructions per group.  AGAIN: there are further rows, whose
+// workgroups read the same weights.
 template <typename T, int STEPS, int MR, int MT, int NT, int THREADS, bool AGAIN>
 __global__ __launch_bounds__(THREADS, 4) void linear4_kernel(Args4 a, const T *__restrict__ x, T *__restrict__ y)
 {

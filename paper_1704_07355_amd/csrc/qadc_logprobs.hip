@@ -12,8 +12,9 @@
 // leaves five, 20 alternatives: 17 us; with all that reach the bound collected first 140, and 200 in a row, 50 of them, 374 for 24).
 //
 // Bound by memory where there are many rows: 4096 x 65536 bfloat16 86 us (537 MB at 6.2 TB/s), its gradient 171 (1.07 GB at
-// 6.3); by launches and round trips where there are few: 131072 logits with 20 alternatives 4 us for the parts and 10 for the
-// join, 64 x 50021 with 50 alternatives 5 and 13.
+// 6.3); where there are few by the join's one workgroup a row, which takes its steps one after the other: 131072 logits with 20
+// alternatives 4 us for the parts and 10 for the join, 64 x 50021 with 50 alternatives 5 and 13.  (The parts and joins are kernels'
+// times by the profiler; all other figures in this file are calls one after the other: 16 and 17.5 us for these two.)
 
 #include <algorithm>
 #include <type_traits>
@@ -100,7 +101,7 @@ __device__ __forceinline__ bool add_block(Stats &st, const float (&x)[LP_BLOCK],
 
 // The logits of block (chunk, thread): LP_BLOCK / N packs, those of a wavefront side by side.  Packs lie at multiples of 16
 // bytes in memory: a row that does not begin at one has its first pack begin `lead` logits before it (packs across those
-// multiples took a quarter longer: 4096 rows of 50021 bfloat16 logits 92 us, their gradient 199).
+// multiples took a quarter longer: 4096 rows of 50021 bfloat16 logits 92 us for 75).
 template <typename T>
 __device__ __forceinline__ int64_t pack_at(int64_t chunk, int u, int lead)
 {

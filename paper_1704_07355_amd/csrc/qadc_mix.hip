@@ -10,7 +10,7 @@
 // that (below e^-69) is added up again relative to its own largest.
 //
 // Bound by the gathers: 2048 rows of 1024 neighbours from 10 M values 47 us, 2 M reads of 4 bytes, each a line (246 MB fetched);
-// one row of 100 neighbours 5.4 us, three dependent round trips.
+// one row of 100 neighbours 5.4 us, three dependent round trips (kernel by the profiler; the call takes 10.8).
 
 #include <algorithm>
 
@@ -161,7 +161,7 @@ int neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const f
     const float log_keep = log1pf(-lambda), log_lambda = logf(lambda);
     // Rows of few neighbours and tokens have a wavefront each, where there are enough of them: 2048 rows of 128 neighbours and 32 tokens
     // 7.7 us (9.1 with a workgroup of 256 each), 4096 of 100 and 20 8.7 (14.7), of 256 and 64 20.1 (20.6); but 2048 of 256 and 64
-    // 16.4 (12.9), 3000 of 200 and 40 15.4 (14.6), and 1024 of 128 and 32 6.7 (6.0).
+    // 16.4 (12.9), 3000 of 200 and 40 15.4 (14.6), and 1024 of 128 and 32 6.7 (6.0); calls replayed from a graph.
     const int threads = R <= 256 && T <= 64 && rows >= (R > 128 && T > 16 ? 4096 : 2048) ? WAVE : 256;
     int at_once = 1;
     while (at_once < T && at_once < threads) at_once *= 2;
