@@ -15,7 +15,7 @@
 // with q - z itself, a whole number that a bfloat16 holds: 24 vector instructions for 8 weights of each lane instead of 8 (16 rows
 // of 4096 x 4096 13.7 us, 12.9 with 16 + q).  Up to four rows have their three parts in three rows of a matrix instruction, of whose
 // 16 they need no more (one row of 131072 x 4096 68 us; with an instruction for each part 91, and 75 with 16 + q).
-
+//
 // Bound by the weights' bytes for a few rows: one row of 131072 x 4096 bfloat16 49 us (277 MB at 5.6 TB/s), of 4096 x 4096
 // binary16 5.2, a launch and a round trip; beyond 16 rows by vector instructions (unpacking, 8 for 8 weights of each lane, and
 // what follows a group) and by x, which every workgroup brings into LDS: 24 rows of 10007 x 5000 in groups of 32 22 us.  (These are
