@@ -430,6 +430,7 @@ int qadc_rotate(const float *rot, int d, const float *x, int64_t n, float *y, vo
 #define QADC_TYPE_F32  0
 #define QADC_TYPE_F16  1  /* IEEE binary16 */
 #define QADC_TYPE_BF16 2  /* the upper half of a float32 */
+#define QADC_TYPE_E4M3 3  /* 8 bits: a sign, four of exponent, three of mantissa, up to 448, no infinity (qadc_rms_norm's y only) */
 
 /*
  * Layer norm.  For every row x of d elements
@@ -458,6 +459,41 @@ int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
                              int wtype, const float *mean, const float *rstd, int64_t rows, int d, void *dx,
                              float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
 size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
+
+/*
+ * Root-mean-square norm of a state, with the residual's addition before it and an output in 8 bits.  For every row
+ *     h = x + residual, rounded to `type` (without a residual h = x),
+ *     rstd = 1 / sqrt(sum h^2 / d + eps),  y[c] = h[c] * rstd * weight[c]
+ * in float32.  h, the stream that goes on, is written to `sum`; it is the rounded h that is normalised, which is what the
+ * backward pass reads.  y is rounded once to `type`, or, with `ytype` QADC_TYPE_E4M3, to 8 bits with a scale per row:
+ *     scale = max |y| / 448,  q = y * (448 / max |y|) to the nearest 8-bit number (ties to even); y is about q * scale.
+ * A row of zeros has scale 0.  A row that holds an infinity or a NaN becomes NaN, its scale too.  Squares are summed in float32: |h|
+ * up to 1e19 / sqrt(d); rows beyond become zeros.
+ *   x [rows][ldx], residual [rows][ldr] (or NULL) of `type`, 1 <= d <= 2^31 - 16385
+ *   weight [d] of `wtype`: QADC_TYPE_F32 or `type`, or NULL (1);  eps >= 0
+ *   sum [rows][ld_sum] of `type` (output, only with a residual; may be x or the residual with its row distance)
+ *   y [rows][d] of `type` or bytes (output; of `type` it may be x or the residual when that is dense; never `sum`)
+ *   scale [rows] f32 (output with QADC_TYPE_E4M3, else not written);  rstd [rows] f32 (output, nullable)
+ */
+int qadc_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int type, const void *weight, int wtype,
+                  int64_t rows, int d, float eps, void *sum, int64_t ld_sum, void *y, int ytype, float *scale, float *rstd,
+                  void *stream);
+
+/*
+ * Its backward pass, with n = h * rstd and g = dy * weight, and dsum the gradient that reaches h from the stream that went on:
+ *     dx = rstd * (g - n * (sum g n / d)) + dsum,  dweight = sum over rows of dy n
+ * in float32; dx, the gradient of x and of the residual alike, is rounded once to `type`.  The sums over rows are added in a fixed
+ * order: equal calls give equal bits.  With rows = 0 dweight is zero.
+ *   dy [rows][lddy], dsum [rows][ldds] (or NULL), h [rows][ldh] of `type`: h is `sum` of qadc_rms_norm, x where there was no residual
+ *   weight as above;  rstd [rows] f32 of the forward pass
+ *   dx [rows][d] of `type` (output, nullable; may be dy, dsum or h when that is dense);  dweight [d] f32 (output, nullable)
+ *   workspace >= qadc_rms_norm_workspace_bytes(rows, d), 16-byte aligned (0 and NULL without dweight); it need not be cleared
+ *   and is not left cleared, and serves fewer rows of the same d too.
+ */
+int qadc_rms_norm_backward(const void *dy, int64_t lddy, const void *dsum, int64_t ldds, const void *h, int64_t ldh, int type,
+                           const void *weight, int wtype, const float *rstd, int64_t rows, int d, void *dx, float *dweight,
+                           void *workspace, size_t workspace_bytes, void *stream);
+size_t qadc_rms_norm_workspace_bytes(int64_t rows, int d);
 
 /*
  * Products with 4-bit weights that share a scale by groups of `group` consecutive inputs:
@@ -579,7 +615,11 @@ int qadc_neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, co
 #define QADC_PROF_LINEAR4    11 /* kernels of qadc_linear4 */
 #define QADC_PROF_LOGPROBS   12 /* kernels of qadc_token_logprobs and its backward pass */
 #define QADC_PROF_MIX        13 /* kernel of qadc_neighbour_mix */
-#define QADC_PROF_COUNT  14
+#define QADC_PROF_RMS        14 /* kernels of qadc_rms_norm and its backward pass */
+#define QADC_PROF_ADJUST     15 /* kernel of qadc_adjust_logits */
+#define QADC_PROF_DISTILL    16 /* kernels of qadc_distill, its backward pass and qadc_distill_step */
+#define QADC_PROF_ADAPTERS   17 /* kernels of qadc_add_adapters */
+#define QADC_PROF_COUNT  18
 int qadc_profile_enable(int on);
 /* As qadc_profile_enable(1), but only the kernels of slot `which` carry events: their neighbours in
  * the stream are launched as in an untimed run. */

@@ -25,13 +25,15 @@ QADC_WS_SCAN_TOPK, QADC_WS_SCAN_F32_4BIT, QADC_WS_SCAN_F32_8BIT, QADC_WS_SEARCH,
 QADC_WS_SCAN_U8_6BIT = 5
 (QADC_PROF_SCAN, QADC_PROF_MERGE, QADC_PROF_SEED, QADC_PROF_IVF_INDEX, QADC_PROF_IVF_TABLES,
  QADC_PROF_TABLES, QADC_PROF_QUANTIZE, QADC_PROF_PREPARE, QADC_PROF_ROTATE, QADC_PROF_IVF_SHARED,
- QADC_PROF_NORM, QADC_PROF_LINEAR4, QADC_PROF_LOGPROBS, QADC_PROF_MIX) = range(14)
+ QADC_PROF_NORM, QADC_PROF_LINEAR4, QADC_PROF_LOGPROBS, QADC_PROF_MIX,
+ QADC_PROF_RMS, QADC_PROF_ADJUST, QADC_PROF_DISTILL, QADC_PROF_ADAPTERS) = range(18)
 QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
-QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16 = 0, 1, 2
+QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16, QADC_TYPE_E4M3 = 0, 1, 2, 3
 QADC_MAX_ALTERNATIVES = 128
 
 EXPORTS = (
     "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
+    "qadc_rms_norm", "qadc_rms_norm_backward", "qadc_rms_norm_workspace_bytes",
     "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
     "qadc_token_logprobs", "qadc_token_logprobs_workspace_bytes", "qadc_token_logprobs_backward", "qadc_neighbour_mix",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
@@ -150,6 +152,12 @@ def lib() -> ctypes.CDLL:
         L.qadc_layer_norm_backward.restype = i32
         L.qadc_layer_norm_workspace_bytes.argtypes = [i64, i32]
         L.qadc_layer_norm_workspace_bytes.restype = sz
+        L.qadc_rms_norm.argtypes = [vp, i64, vp, i64, i32, vp, i32, i64, i32, f32, vp, i64, vp, i32, vp, vp, vp]
+        L.qadc_rms_norm.restype = i32
+        L.qadc_rms_norm_backward.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, vp, vp, vp, sz, vp]
+        L.qadc_rms_norm_backward.restype = i32
+        L.qadc_rms_norm_workspace_bytes.argtypes = [i64, i32]
+        L.qadc_rms_norm_workspace_bytes.restype = sz
         L.qadc_weights4_bytes.argtypes = [i64, i32, i32, i32]
         L.qadc_weights4_bytes.restype = sz
         L.qadc_pack_weights4.argtypes = [vp, vp, i32, vp, i64, i32, i32, vp, vp]
@@ -706,6 +714,69 @@ def qadc_layer_norm_backward(dy, x, weight, mean, rstd, workspace=None, out=None
                                           _vector(mean, rows, torch.float32), _vector(rstd, rows, torch.float32), rows, d,
                                           _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, _stream()))
     return dx, dw, db
+
+
+def qadc_rms_norm(x, weight=None, residual=None, eps=1e-5, out_type=None, sum_out=None, out=None):
+    """x [rows][d] (f32, f16 or bf16; rows may lie apart), weight [d] (f32 or x's type) | None, residual like x | None,
+    out_type None (x's) or torch.float8_e4m3fn
+    -> (y [rows][d], x + residual [rows][d] of x's type | None, scale f32 [rows] | None, rstd f32 [rows])."""
+    rows, d = x.shape
+    xp, ldx = _matrix(x)
+    xtype = ytype = _type(x)
+    rp = sp = scale = None
+    ldr = ld_sum = d
+    if residual is not None:
+        if residual.shape != x.shape:
+            raise ValueError("residual must have x's shape")
+        rp, ldr = _matrix(residual, x.dtype)
+        if sum_out is None:
+            sum_out = _like(None, x)
+        elif sum_out.shape != x.shape:
+            raise ValueError(f"sum_out must be {tuple(x.shape)}")
+        sp, ld_sum = _matrix(sum_out, x.dtype)
+    elif sum_out is not None:
+        raise ValueError("sum_out needs a residual")
+    if out_type is None or out_type == x.dtype:
+        y = _like(out, x)
+    elif out_type == torch.float8_e4m3fn:
+        ytype = QADC_TYPE_E4M3
+        y = out if out is not None else torch.empty(rows, d, dtype=out_type, device=x.device)
+        if y.shape != x.shape or y.dtype != out_type or not y.is_cuda or not y.is_contiguous():
+            raise ValueError(f"output must be a contiguous {out_type} GPU tensor of {tuple(x.shape)}")
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    else:
+        raise ValueError(f"out_type must be {x.dtype} or torch.float8_e4m3fn")
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _check(lib().qadc_rms_norm(xp, ldx, rp, ldr, xtype, _vector(weight, d), _weight_type(weight, None, x), rows, d, eps, sp, ld_sum,
+                               y.data_ptr(), ytype, None if scale is None else scale.data_ptr(), rstd.data_ptr(), _stream()))
+    return y, sum_out, scale, rstd
+
+
+def qadc_rms_norm_workspace_bytes(rows: int, d: int) -> int:
+    return int(lib().qadc_rms_norm_workspace_bytes(rows, d))
+
+
+def qadc_rms_norm_backward(dy, h, weight, rstd, dsum=None, workspace=None, out=None, need_dx=True, need_weight=True):
+    """dy, h [rows][d] (h: x + residual of qadc_rms_norm, or its x), weight [d] | None, rstd f32 [rows], dsum like dy | None
+    -> (dx [rows][d] of h's type | None, dweight f32 [d] | None)."""
+    rows, d = h.shape
+    if tuple(dy.shape) != (rows, d) or (dsum is not None and tuple(dsum.shape) != (rows, d)):
+        raise ValueError("dy and dsum must have h's shape")
+    dyp, lddy = _matrix(dy, h.dtype)
+    hp, ldh = _matrix(h)
+    sp, lds = (None, d) if dsum is None else _matrix(dsum, h.dtype)
+    dx = _like(out, h) if need_dx else None
+    dw = None
+    size = 0
+    if need_weight:
+        dw = torch.empty(d, dtype=torch.float32, device=h.device)
+        workspace, size = _scratch(workspace, qadc_rms_norm_workspace_bytes, (rows, d), h.device)
+    else:
+        workspace = None
+    _check(lib().qadc_rms_norm_backward(dyp, lddy, sp, lds, hp, ldh, _type(h), _vector(weight, d), _weight_type(weight, None, h),
+                                        _vector(rstd, rows, torch.float32), rows, d, _ptr(dx), _ptr(dw), _ptr(workspace), size,
+                                        _stream()))
+    return dx, dw
 
 
 def qadc_weights4_bytes(N: int, K: int, group: int, has_zeros) -> int:

@@ -99,6 +99,11 @@ int layer_norm(const void *, int64_t, int, const void *, const void *, int, int6
 int layer_norm_backward(const void *, int64_t, const void *, int64_t, int, const void *, int, const float *, const float *,
                         int64_t, int, void *, float *, float *, void *, size_t, hipStream_t);
 size_t layer_norm_workspace(int64_t, int);
+int rms_norm(const void *, int64_t, const void *, int64_t, int, const void *, int, int64_t, int, float, void *, int64_t, void *, int,
+             float *, float *, hipStream_t);
+int rms_norm_backward(const void *, int64_t, const void *, int64_t, const void *, int64_t, int, const void *, int, const float *,
+                      int64_t, int, void *, float *, void *, size_t, hipStream_t);
+size_t rms_norm_workspace(int64_t, int);
 size_t weights4_bytes(int64_t, int, int, int);
 int pack_weights4(const uint8_t *, const void *, int, const uint8_t *, int64_t, int, int, void *, hipStream_t);
 int linear4(const qadc_weights4 *, const void *, int64_t, int, int64_t, const float *, void *, int64_t, hipStream_t);
@@ -309,6 +314,24 @@ int qadc_layer_norm_backward(const void *dy, int64_t lddy, const void *x, int64_
 }
 
 size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d) { return qadc::layer_norm_workspace(rows, d); }
+
+int qadc_rms_norm(const void *x, int64_t ldx, const void *residual, int64_t ldr, int type, const void *weight, int wtype,
+                  int64_t rows, int d, float eps, void *sum, int64_t ld_sum, void *y, int ytype, float *scale, float *rstd,
+                  void *stream)
+{
+    return qadc::rms_norm(x, ldx, residual, ldr, type, weight, wtype, rows, d, eps, sum, ld_sum, y, ytype, scale, rstd,
+                          (hipStream_t)stream);
+}
+
+int qadc_rms_norm_backward(const void *dy, int64_t lddy, const void *dsum, int64_t ldds, const void *h, int64_t ldh, int type,
+                           const void *weight, int wtype, const float *rstd, int64_t rows, int d, void *dx, float *dweight,
+                           void *workspace, size_t workspace_bytes, void *stream)
+{
+    return qadc::rms_norm_backward(dy, lddy, dsum, ldds, h, ldh, type, weight, wtype, rstd, rows, d, dx, dweight, workspace,
+                                   workspace_bytes, (hipStream_t)stream);
+}
+
+size_t qadc_rms_norm_workspace_bytes(int64_t rows, int d) { return qadc::rms_norm_workspace(rows, d); }
 
 size_t qadc_weights4_bytes(int64_t N, int K, int group, int has_zeros)
 {

@@ -1,0 +1,41 @@
+"""The norms, logit rules, distillation and adapters check their arguments on the host, before anything is launched (no GPU needed)."""
+
+import paper_1704_07355_amd as Q
+
+PTR = 256  # stands for a device pointer: every call below is refused before it is used
+
+
+def test_rms_norm():
+    L = Q.lib()
+    ok = dict(x=PTR, ldx=8, res=None, ldr=0, type=0, w=None, wtype=0, rows=3, d=8, eps=1e-5, sum=None, ld_sum=0, y=2 * PTR, ytype=0,
+              scale=None, rstd=None, stream=None)
+
+    def f(**k):
+        return L.qadc_rms_norm(*dict(ok, **k).values())
+
+    assert f(x=None, y=None, rows=0) == Q.QADC_OK  # nothing to do
+    for bad in (dict(x=None), dict(y=None), dict(type=3), dict(type=-1), dict(wtype=2), dict(rows=-1), dict(d=0), dict(d=2 ** 31 - 1),
+                dict(ldx=7), dict(eps=float("nan")), dict(eps=-1.0), dict(ytype=1), dict(ytype=3), dict(ytype=3, y=PTR, scale=PTR),
+                dict(res=3 * PTR, ldr=8), dict(res=3 * PTR, ldr=7, sum=4 * PTR, ld_sum=8), dict(res=3 * PTR, ldr=8, sum=4 * PTR, ld_sum=7),
+                dict(res=3 * PTR, ldr=9, sum=3 * PTR, ld_sum=8), dict(res=3 * PTR, ldr=8, sum=PTR, ld_sum=9),
+                dict(res=3 * PTR, ldr=8, sum=2 * PTR, ld_sum=8), dict(y=PTR, ldx=9), dict(res=2 * PTR, ldr=9, sum=4 * PTR, ld_sum=8)):
+        assert f(**bad) == Q.QADC_EINVAL, bad
+    assert b"qadc_rms_norm" in L.qadc_last_error()
+
+
+def test_rms_norm_backward():
+    L = Q.lib()
+    need = Q.qadc_rms_norm_workspace_bytes(100, 8)
+    assert need > 0 and Q.qadc_rms_norm_workspace_bytes(-1, 8) == 0 and Q.qadc_rms_norm_workspace_bytes(4, 0) == 0
+    ok = dict(dy=PTR, lddy=8, ds=None, ldds=0, h=2 * PTR, ldh=8, type=0, w=None, wtype=0, rstd=PTR, rows=100, d=8, dx=3 * PTR, dw=PTR,
+              ws=PTR, size=need, stream=None)
+
+    def f(**k):
+        return L.qadc_rms_norm_backward(*dict(ok, **k).values())
+
+    assert f(size=0) == Q.QADC_ENOMEM and f(ws=None) == Q.QADC_ENOMEM
+    for bad in (dict(dy=None), dict(h=None), dict(rstd=None), dict(lddy=7), dict(ldh=7), dict(ds=PTR, ldds=7), dict(type=3),
+                dict(wtype=1), dict(rows=-1), dict(d=0), dict(dx=PTR, lddy=9), dict(dx=2 * PTR, ldh=9),
+                dict(ds=3 * PTR, ldds=9), dict(ws=PTR + 8)):
+        assert f(**bad) == Q.QADC_EINVAL, bad
+    assert b"qadc_rms_norm_backward" in L.qadc_last_error()
