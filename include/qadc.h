@@ -574,6 +574,30 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
                                  const float *dentropy, void *dlogits, int64_t ldd, void *stream);
 
 /*
+ * Rules on logits, before their log probabilities are taken: penalties for repeated tokens, biases, and the tokens that a
+ * grammar allows.  For every row, with x[v] = logits[v], and in this order:
+ *     a token anywhere in the row's history:  x = x > 0 ? x / repetition : x * repetition
+ *     a token said n > 0 times behind the prompt:  x -= frequency * n + presence
+ *     a token with biases:  x += their sum, in the order in which they are given
+ *     a token that the row's mask does not allow:  x = -inf, whatever it was
+ * in float32, rounded once to `type`; other tokens' logits are copied bit by bit (in place: not touched).
+ *   logits [rows][ld] of `type`, V <= ld of them per row, 1 <= V <= 2^31 - 65537
+ *   history [rows][H] i32, 0 <= H <= QADC_MAX_HISTORY, NULL when H = 0: entries outside [0, V) are passed over
+ *   lengths [rows] i32 or NULL: how many entries of a row's history are used, 0 to H (H); prompt [rows] i32 or NULL: how many of
+ *   the first ones are the prompt (0)
+ *   repetition (> 0), presence, frequency [rows] f32, each or NULL (1, 0, 0)
+ *   bias_tokens [rows][B] i32, bias [rows][B] f32, 0 <= B <= QADC_MAX_R, NULL when B = 0: an entry outside [0, V) is an unused slot
+ *   masks [states][mask_ld] u32 or NULL, mask_ld >= ceil(V / 32): token v is allowed where bit v % 32 of word v / 32 is set
+ *   mask_of [rows] i32: which of the masks is a row's; a number outside [0, states): none.  NULL: row r has mask r, states >= rows
+ *   out [rows][ldo] of `type` (output; may be logits when ldo == ld: then only what changes is written)
+ */
+#define QADC_MAX_HISTORY (1 << 24)
+int qadc_adjust_logits(const void *logits, int64_t ld, int type, int64_t rows, int V, const int32_t *history, int H,
+                       const int32_t *lengths, const int32_t *prompt, const float *repetition, const float *presence,
+                       const float *frequency, const int32_t *bias_tokens, const float *bias, int B, const uint32_t *masks,
+                       int64_t mask_ld, int states, const int32_t *mask_of, void *out, int64_t ldo, void *stream);
+
+/*
  * The tokens of the nearest stored states, mixed into a model's log probabilities.  Every neighbour i of a row votes for
  * values[ids[i]] with a weight that falls with its distance:
  *     P(t) = sum_i w_i (values[ids[i]] = t),  w = softmax over the row of -beta * distance

@@ -30,12 +30,14 @@ QADC_WS_SCAN_U8_6BIT = 5
 QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
 QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16, QADC_TYPE_E4M3 = 0, 1, 2, 3
 QADC_MAX_ALTERNATIVES = 128
+QADC_MAX_HISTORY = 1 << 24
 
 EXPORTS = (
     "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
     "qadc_rms_norm", "qadc_rms_norm_backward", "qadc_rms_norm_workspace_bytes",
     "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
     "qadc_token_logprobs", "qadc_token_logprobs_workspace_bytes", "qadc_token_logprobs_backward", "qadc_neighbour_mix",
+    "qadc_adjust_logits",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
     "qadc_profile_enable", "qadc_profile_only", "qadc_profile_read", "qadc_workspace_bytes", "qadc_workspace_init",
@@ -172,6 +174,8 @@ def lib() -> ctypes.CDLL:
         L.qadc_token_logprobs_backward.restype = i32
         L.qadc_neighbour_mix.argtypes = [vp, vp, i32, vp, i64, i32, vp, i64, f32, vp, i32, vp, f32, vp, vp, vp]
         L.qadc_neighbour_mix.restype = i32
+        L.qadc_adjust_logits.argtypes = [vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp]
+        L.qadc_adjust_logits.restype = i32
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -863,6 +867,42 @@ def qadc_token_logprobs_backward(logits, tokens, lse, entropy, dlogp, dentropy=N
                                               _vector(entropy, rows, torch.float32),
                                               _vector(dlogp, rows * T, torch.float32) if T else None,
                                               _vector(dentropy, rows, torch.float32), op, ldd, _stream()))
+    return out
+
+
+def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetition=None, presence=None, frequency=None,
+                       bias_tokens=None, bias=None, masks=None, mask_of=None, out=None):
+    """logits [rows][V] (f32, f16 or bf16; rows may lie apart), history i32 [rows][H], lengths, prompt i32 [rows], repetition,
+    presence, frequency f32 [rows], bias_tokens i32 and bias f32 [rows][B], masks i32 or u32 [states][>= ceil(V/32)], mask_of
+    i32 [rows], each | None -> adjusted logits [rows][V] of their type."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    hp, H = _tokens(history, rows)
+    bp, B = _tokens(bias_tokens, rows)
+    if (bias is None) != (bias_tokens is None):
+        raise ValueError("bias and bias_tokens belong together")
+    if history is None and not (lengths is prompt is repetition is presence is frequency is None):
+        raise ValueError("lengths, prompt and penalties need a history")
+    mp, ldm, states = None, 0, 0
+    if masks is not None:
+        if masks.dtype not in (torch.int32, torch.uint32):
+            raise ValueError(f"expected masks of 32-bit words, got {masks.dtype}")
+        mp, ldm = _matrix(masks)
+        states = masks.shape[0]
+        if masks.shape[1] < -(-V // 32):
+            raise ValueError(f"expected masks of {-(-V // 32)} words")
+    elif mask_of is not None:
+        raise ValueError("mask_of needs masks")
+    if out is None:
+        out = _like(None, logits)
+    elif tuple(out.shape) != (rows, V):
+        raise ValueError(f"output must be {(rows, V)}")
+    op, ldo = _matrix(out, logits.dtype)
+    f32, i32 = torch.float32, torch.int32
+    _check(lib().qadc_adjust_logits(xp, ld, _type(logits), rows, V, hp, H, _vector(lengths, rows, i32), _vector(prompt, rows, i32),
+                                    _vector(repetition, rows, f32), _vector(presence, rows, f32), _vector(frequency, rows, f32), bp,
+                                    _vector(bias, rows * B, f32), B, mp, ldm, states, _vector(mask_of, rows, i32), op, ldo,
+                                    _stream()))
     return out
 
 

@@ -112,6 +112,9 @@ int token_logprobs(const void *, int64_t, int, int64_t, int, float, const int32_
 size_t token_logprobs_workspace(int64_t, int, int);
 int token_logprobs_backward(const void *, int64_t, int, int64_t, int, float, const int32_t *, int, const float *, const float *,
                             const float *, const float *, void *, int64_t, hipStream_t);
+int adjust_logits(const void *, int64_t, int, int64_t, int, const int32_t *, int, const int32_t *, const int32_t *, const float *,
+                  const float *, const float *, const int32_t *, const float *, int, const uint32_t *, int64_t, int, const int32_t *,
+                  void *, int64_t, hipStream_t);
 int neighbour_mix(const uint32_t *, const void *, int, const float *, int64_t, int, const int32_t *, int64_t, float,
                   const int32_t *, int, const float *, float, float *, float *, hipStream_t);
 int workspace_init(void *, size_t, hipStream_t);
@@ -366,6 +369,15 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
 {
     return qadc::token_logprobs_backward(logits, ld, type, rows, V, scale, tokens, T, lse, entropy, dlogp, dentropy, dlogits,
                                          ldd, (hipStream_t)stream);
+}
+
+int qadc_adjust_logits(const void *logits, int64_t ld, int type, int64_t rows, int V, const int32_t *history, int H,
+                       const int32_t *lengths, const int32_t *prompt, const float *repetition, const float *presence,
+                       const float *frequency, const int32_t *bias_tokens, const float *bias, int B, const uint32_t *masks,
+                       int64_t mask_ld, int states, const int32_t *mask_of, void *out, int64_t ldo, void *stream)
+{
+    return qadc::adjust_logits(logits, ld, type, rows, V, history, H, lengths, prompt, repetition, presence, frequency, bias_tokens,
+                               bias, B, masks, mask_ld, states, mask_of, out, ldo, (hipStream_t)stream);
 }
 
 int qadc_neighbour_mix(const uint32_t *ids, const void *dist, int dist_bytes, const float *step, int64_t rows, int R,

@@ -39,3 +39,20 @@ def test_rms_norm_backward():
                 dict(ds=3 * PTR, ldds=9), dict(ws=PTR + 8)):
         assert f(**bad) == Q.QADC_EINVAL, bad
     assert b"qadc_rms_norm_backward" in L.qadc_last_error()
+
+
+def test_adjust_logits():
+    L = Q.lib()
+    ok = dict(x=PTR, ld=64, type=0, rows=3, V=64, history=None, H=0, lengths=None, prompt=None, rep=None, pres=None, freq=None,
+              bt=None, bias=None, B=0, masks=None, ldm=0, states=0, of=None, out=2 * PTR, ldo=64, stream=None)
+
+    def f(**k):
+        return L.qadc_adjust_logits(*dict(ok, **k).values())
+
+    assert f(x=None, out=None, rows=0) == Q.QADC_OK
+    for bad in (dict(x=None), dict(out=None), dict(type=3), dict(rows=-1), dict(V=0), dict(V=2 ** 31 - 1, ld=2 ** 31, ldo=2 ** 31),
+                dict(ld=63), dict(ldo=63), dict(H=5), dict(H=-1), dict(H=Q.QADC_MAX_HISTORY + 1, history=PTR), dict(B=2, bt=PTR),
+                dict(B=2, bias=PTR), dict(B=Q.QADC_MAX_R + 1, bt=PTR, bias=PTR), dict(B=-1), dict(masks=PTR, ldm=1, states=3),
+                dict(masks=PTR, ldm=2, states=0), dict(masks=PTR, ldm=2, states=2), dict(out=PTR, ldo=65)):
+        assert f(**bad) == Q.QADC_EINVAL, bad
+    assert b"qadc_adjust_logits" in L.qadc_last_error()
