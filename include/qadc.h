@@ -574,6 +574,50 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
                                  const float *dentropy, void *dlogits, int64_t ldd, void *stream);
 
 /*
+ * Distillation: how far a student's distribution is from that of a teacher of which the likeliest tokens were stored, as
+ * qadc_token_logprobs writes them (top_idx, top_logp).  For every row, with x[v] = scale * logits[v], q = exp(x - lse) and
+ * p[i] = exp top_logp[i], P = sum p:
+ *   tail != 0: what the teacher has left, r = max(0, 1 - P), is compared as a whole with what the student gives to all tokens that
+ *     were not stored, Q:  loss = sum_i p[i] (top_logp[i] - log q[top_idx[i]]) + r (log r - log Q);
+ *   tail == 0: the stored tokens are taken for all of the teacher's distribution, p / P, and r = 0.
+ * Terms with p = 0 or r = 0 are 0; a row whose teacher is empty (P = 0, tail == 0) has loss 0.  Where Q is 0 (every token is
+ * stored, a mask of -inf leaves no other, or it is below 1e-37) the tail's term is left out.  A stored token that the student's mask
+ * excludes makes the loss +inf.  A token that is stored twice has both its terms, and counts once for the student.  A row that
+ * holds a NaN or +inf has loss NaN; a row with nothing left lse = log Q = -inf.
+ * Sums over the vocabulary are in float32, the teacher's probabilities and the loss in float64, rounded to float32.
+ *   logits [rows][ld] of `type`, V <= ld of them per row, 1 <= V <= 2^31 - 65537;  0 < scale <= 2e38
+ *   top_idx [rows][k] u32, top_logp [rows][k] f32, 0 <= k <= QADC_MAX_ALTERNATIVES: an index >= V (0xFFFFFFFF) is an unused slot
+ *   loss, lse, log_tail (log Q) [rows] f32 (outputs; lse and log_tail, for the backward pass, nullable)
+ *   workspace >= qadc_distill_workspace_bytes(rows, V), 16-byte aligned; it need not be cleared and is not left cleared, and
+ *   serves fewer rows and tokens too
+ */
+int qadc_distill(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                 const float *top_logp, int k, int tail, float *loss, float *lse, float *log_tail, void *workspace,
+                 size_t workspace_bytes, void *stream);
+size_t qadc_distill_workspace_bytes(int64_t rows, int V);
+
+/*
+ * The gradient of sum dloss loss with respect to the logits, T being P + r with the tail and 1 without:
+ *     dlogits[v] = scale * dloss * (T q[v] - (p of v if it is stored, else r q[v] / Q))
+ * in float32, rounded once to `type`.  A row with dloss = 0 gets zeros and is not read; a row with nothing left gets zeros.
+ * q = exp(x - lse) is as exact as lse: |lse| 2^-24 relative.
+ *   lse, log_tail [rows] f32 as qadc_distill wrote them;  dloss [rows] f32
+ *   dlogits [rows][ldd] of `type` (output; may be logits when ldd == ld)
+ */
+int qadc_distill_backward(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                          const float *top_logp, int k, int tail, const float *lse, const float *log_tail, const float *dloss,
+                          void *dlogits, int64_t ldd, void *stream);
+
+/*
+ * Loss and gradient in one call, where every row's share of the loss is known beforehand: loss as qadc_distill writes it, dlogits
+ * as qadc_distill_backward with dloss = weight.  Rows of up to 256 KB are read and written once.
+ *   weight [rows] f32;  workspace as for qadc_distill (always needed)
+ */
+int qadc_distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                      const float *top_logp, int k, int tail, const float *weight, float *loss, void *dlogits, int64_t ldd,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Rules on logits, before their log probabilities are taken: penalties for repeated tokens, biases, and the tokens that a
  * grammar allows.  For every row, with x[v] = logits[v], and in this order:
  *     a token anywhere in the row's history:  x = x > 0 ? x / repetition : x * repetition

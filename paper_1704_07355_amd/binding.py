@@ -37,7 +37,7 @@ EXPORTS = (
     "qadc_rms_norm", "qadc_rms_norm_backward", "qadc_rms_norm_workspace_bytes",
     "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
     "qadc_token_logprobs", "qadc_token_logprobs_workspace_bytes", "qadc_token_logprobs_backward", "qadc_neighbour_mix",
-    "qadc_adjust_logits",
+    "qadc_adjust_logits", "qadc_distill", "qadc_distill_workspace_bytes", "qadc_distill_backward", "qadc_distill_step",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
     "qadc_profile_enable", "qadc_profile_only", "qadc_profile_read", "qadc_workspace_bytes", "qadc_workspace_init",
@@ -176,6 +176,14 @@ def lib() -> ctypes.CDLL:
         L.qadc_neighbour_mix.restype = i32
         L.qadc_adjust_logits.argtypes = [vp, i64, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, i32, vp, vp, i64, vp]
         L.qadc_adjust_logits.restype = i32
+        L.qadc_distill.argtypes = [vp, i64, i32, i64, i32, f32, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.qadc_distill.restype = i32
+        L.qadc_distill_workspace_bytes.argtypes = [i64, i32]
+        L.qadc_distill_workspace_bytes.restype = sz
+        L.qadc_distill_backward.argtypes = [vp, i64, i32, i64, i32, f32, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.qadc_distill_backward.restype = i32
+        L.qadc_distill_step.argtypes = [vp, i64, i32, i64, i32, f32, vp, vp, i32, i32, vp, vp, vp, i64, vp, sz, vp]
+        L.qadc_distill_step.restype = i32
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -868,6 +876,69 @@ def qadc_token_logprobs_backward(logits, tokens, lse, entropy, dlogp, dentropy=N
                                               _vector(dlogp, rows * T, torch.float32) if T else None,
                                               _vector(dentropy, rows, torch.float32), op, ldd, _stream()))
     return out
+
+
+def _teacher(top_idx, top_logp, rows):
+    """Pointers and number per row of a teacher's stored tokens and log probabilities."""
+    if top_idx.dim() != 2 or top_idx.shape[0] != rows or top_logp.shape != top_idx.shape:
+        raise ValueError(f"expected top_idx and top_logp [{rows}][k]")
+    if top_idx.dtype not in (torch.int32, torch.uint32):
+        raise ValueError(f"expected 32-bit indexes, got {top_idx.dtype}")
+    return _ptr(top_idx), _ptr(top_logp, torch.float32), top_idx.shape[1]
+
+
+def qadc_distill_workspace_bytes(rows: int, V: int) -> int:
+    return int(lib().qadc_distill_workspace_bytes(rows, V))
+
+
+def qadc_distill(logits, top_idx, top_logp, scale=1.0, tail=True, workspace=None):
+    """logits [rows][V] (f32, f16 or bf16; rows may lie apart), top_idx i32-bits-of-u32 and top_logp f32 [rows][k] of a teacher
+    (qadc_token_logprobs) -> (loss f32 [rows], lse f32 [rows], log_tail f32 [rows])."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    loss, lse = _pair(logits.device, rows)
+    log_tail = torch.empty_like(loss)
+    workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
+    _check(lib().qadc_distill(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), loss.data_ptr(), lse.data_ptr(),
+                              log_tail.data_ptr(), _ptr(workspace), size, _stream()))
+    return loss, lse, log_tail
+
+
+def _gradient_like(out, logits):
+    """The caller's matrix for a gradient with respect to the logits, or a new one; its pointer and row distance."""
+    if out is None:
+        out = _like(None, logits)
+    elif out.shape != logits.shape:
+        raise ValueError(f"output must be {tuple(logits.shape)}")
+    return (out, *_matrix(out, logits.dtype))
+
+
+def qadc_distill_backward(logits, top_idx, top_logp, lse, log_tail, dloss, scale=1.0, tail=True, out=None):
+    """lse, log_tail f32 [rows] of qadc_distill, dloss f32 [rows] -> the gradient with respect to the logits, [rows][V] of their
+    type."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    out, op, ldd = _gradient_like(out, logits)
+    f32 = torch.float32
+    _check(lib().qadc_distill_backward(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), _vector(lse, rows, f32),
+                                       _vector(log_tail, rows, f32), _vector(dloss, rows, f32), op, ldd, _stream()))
+    return out
+
+
+def qadc_distill_step(logits, top_idx, top_logp, weight, scale=1.0, tail=True, out=None, workspace=None):
+    """qadc_distill and, with dloss = weight f32 [rows], qadc_distill_backward in one call
+    -> (loss f32 [rows], gradient [rows][V] of the logits' type)."""
+    rows, V = logits.shape
+    xp, ld = _matrix(logits)
+    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    out, op, ldd = _gradient_like(out, logits)
+    loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
+    _check(lib().qadc_distill_step(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)),
+                                   _vector(weight, rows, torch.float32), loss.data_ptr(), op, ldd, _ptr(workspace), size, _stream()))
+    return loss, out
 
 
 def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetition=None, presence=None, frequency=None,

@@ -112,6 +112,13 @@ int token_logprobs(const void *, int64_t, int, int64_t, int, float, const int32_
 size_t token_logprobs_workspace(int64_t, int, int);
 int token_logprobs_backward(const void *, int64_t, int, int64_t, int, float, const int32_t *, int, const float *, const float *,
                             const float *, const float *, void *, int64_t, hipStream_t);
+int distill(const void *, int64_t, int, int64_t, int, float, const uint32_t *, const float *, int, int, float *, float *, float *, void *,
+            size_t, hipStream_t);
+size_t distill_workspace(int64_t, int);
+int distill_backward(const void *, int64_t, int, int64_t, int, float, const uint32_t *, const float *, int, int, const float *,
+                     const float *, const float *, void *, int64_t, hipStream_t);
+int distill_step(const void *, int64_t, int, int64_t, int, float, const uint32_t *, const float *, int, int, const float *, float *,
+                 void *, int64_t, void *, size_t, hipStream_t);
 int adjust_logits(const void *, int64_t, int, int64_t, int, const int32_t *, int, const int32_t *, const int32_t *, const float *,
                   const float *, const float *, const int32_t *, const float *, int, const uint32_t *, int64_t, int, const int32_t *,
                   void *, int64_t, hipStream_t);
@@ -369,6 +376,32 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
 {
     return qadc::token_logprobs_backward(logits, ld, type, rows, V, scale, tokens, T, lse, entropy, dlogp, dentropy, dlogits,
                                          ldd, (hipStream_t)stream);
+}
+
+int qadc_distill(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                 const float *top_logp, int k, int tail, float *loss, float *lse, float *log_tail, void *workspace,
+                 size_t workspace_bytes, void *stream)
+{
+    return qadc::distill(logits, ld, type, rows, V, scale, top_idx, top_logp, k, tail, loss, lse, log_tail, workspace,
+                         workspace_bytes, (hipStream_t)stream);
+}
+
+size_t qadc_distill_workspace_bytes(int64_t rows, int V) { return qadc::distill_workspace(rows, V); }
+
+int qadc_distill_backward(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                          const float *top_logp, int k, int tail, const float *lse, const float *log_tail, const float *dloss,
+                          void *dlogits, int64_t ldd, void *stream)
+{
+    return qadc::distill_backward(logits, ld, type, rows, V, scale, top_idx, top_logp, k, tail, lse, log_tail, dloss, dlogits, ldd,
+                                  (hipStream_t)stream);
+}
+
+int qadc_distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
+                      const float *top_logp, int k, int tail, const float *weight, float *loss, void *dlogits, int64_t ldd,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    return qadc::distill_step(logits, ld, type, rows, V, scale, top_idx, top_logp, k, tail, weight, loss, dlogits, ldd, workspace,
+                              workspace_bytes, (hipStream_t)stream);
 }
 
 int qadc_adjust_logits(const void *logits, int64_t ld, int type, int64_t rows, int V, const int32_t *history, int H,

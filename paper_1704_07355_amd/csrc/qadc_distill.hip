@@ -1,0 +1,638 @@
+// Distillation from a teacher's likeliest tokens: the loss of every row, its gradient, and both in one call, on gfx950.
+//
+// With x = scale logits, m = max x, e = exp(x - m) over the row, own = sum of e over the stored tokens and others = sum over all
+// others: log q_t = x_t - m - log(own + others), and the student's probability of everything that was not stored is
+// Q = others / (own + others), log Q = -log(1 + own / others).  The stored tokens are left out of the running sum by a bit each in
+// LDS, so that neither others nor log Q is a difference of nearly equal numbers.  What is computed once a row, the teacher's
+// probabilities and the loss itself (a difference of logarithms that are nearly equal), is held in 64 bits.
+//
+// Gradient: with T the teacher's whole probability and r what it has outside the stored tokens,
+// dx_v = scale w ((T - r / Q [v not stored]) q_v - p_v [v stored]): every token but the stored ones gets one factor times q_v.
+#include <algorithm>
+
+#include "qadc_logits.h"
+#include "qadc_profile.h"
+
+namespace qadc {
+
+namespace {
+
+constexpr int DS_MARKED = 16;  // chunks whose stored tokens are marked at a time: 131072 tokens, 16 KB of LDS
+constexpr int DS_WAVES = QADC_MAX_ALTERNATIVES / WAVE;  // wavefronts with stored tokens, one a thread
+static_assert(QADC_MAX_ALTERNATIVES % WAVE == 0 && QADC_MAX_ALTERNATIVES <= LP_WG, "a thread per stored token");
+
+struct Teacher {
+    const uint32_t *idx;  // [rows][k]
+    const float *logp;    // [rows][k]
+    int k;
+    bool tail;
+};
+
+// A part of a row without its stored tokens: the largest logit and the sum of 2^(c (logit - m)).
+struct Part2 {
+    float m, s;
+};
+__device__ __forceinline__ void raise(Part2 &a, float to, float c)
+{
+    a.s *= exp2_fast(shift_of(a.m, to, c));
+    a.m = to;
+}
+__device__ __forceinline__ Part2 join(Part2 a, Part2 b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    raise(a, m, c);
+    raise(b, m, c);
+    return {m, a.s + b.s};
+}
+__device__ __forceinline__ void add_block(Part2 &a, const float (&x)[LP_BLOCK], float c)
+{
+    float v = x[0];
+#pragma unroll
+    for (int e = 1; e < LP_BLOCK; ++e) v = fmaxf(v, x[e]);
+    const float m = fmaxf(a.m, v), m0 = m == -INFINITY ? 0.0f : m;
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < LP_BLOCK; ++i) s[i & 1] += exp2_fast(c * (x[i] - m0));
+    raise(a, m, c);
+    a.s += s[0] + s[1];
+}
+
+// The stored token of this thread, as it is in the row.
+struct Stored {
+    int token;   // -1: none
+    float logit, logp;
+};
+template <typename T>
+__device__ __forceinline__ Stored stored_of(const T *row, int64_t r, int V, const Teacher &t)
+{
+    Stored s = {-1, -INFINITY, -INFINITY};
+    if ((int)threadIdx.x < t.k) {
+        const uint32_t i = t.idx[r * t.k + threadIdx.x];
+        if (i < (uint32_t)V) {
+            s.token = (int)i;
+            s.logit = (float)row[i];
+            s.logp = t.logp[r * t.k + threadIdx.x];
+        }
+    }
+    return s;
+}
+
+__device__ __forceinline__ double wave_sum64(double v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+struct FinishLds {
+    double mass[DS_WAVES], loss[DS_WAVES];
+    float most[DS_WAVES], own[DS_WAVES];
+    int tokens[QADC_MAX_ALTERNATIVES];
+    float total, share, log_tail;
+};
+
+// Of the teacher's probabilities p of a row: their sum, and with the tail what is left.
+struct Mass {
+    double P, rest;
+};
+// What the thread's stored token has, and all of them: every thread comes here.
+__device__ __forceinline__ Mass mass_of(double p, bool tail, FinishLds &lds)
+{
+    if (threadIdx.x < QADC_MAX_ALTERNATIVES) {
+        p = wave_sum64(p);
+        if (lane_id() == 0) lds.mass[threadIdx.x >> 6] = p;
+    }
+    __syncthreads();
+    double P = 0.0;
+#pragma unroll
+    for (int w = 0; w < DS_WAVES; ++w) P += lds.mass[w];
+    return {P, tail && P < 1.0 ? 1.0 - P : 0.0};
+}
+// The teacher's whole probability as the gradient takes it, and the factor of what was not stored, where log Q is `log_tail`.
+__device__ __forceinline__ void shares(const Mass &a, bool tail, double log_tail, float &total, float &share)
+{
+    const double rest = log_tail == -INFINITY ? 0.0 : a.rest;  // (nothing is left to the student there)
+    const double T = tail ? a.P + rest : a.P > 0.0 ? 1.0 : 0.0;
+    total = (float)T;
+    share = (float)(rest > 0.0 ? T - rest * exp(-log_tail) : T);
+}
+
+struct Loss {
+    float *loss, *lse, *log_tail;  // lse and log_tail nullable
+};
+
+// The row's loss from what its other tokens have, by all threads of the workgroup; total and share land in lds.
+// m: the row's largest logit of any token, and own its stored tokens' sum, come back.
+__device__ __forceinline__ void finish_row(Part2 others, const Stored &st, int64_t r, float scale, const Teacher &t, const Loss &o,
+                                           FinishLds &lds, float &m, float &sum)
+{
+    const float c = scale * LOG2E;
+    const int wave = threadIdx.x >> 6;
+    if (wave < DS_WAVES) {
+        const float most = wave_max(st.logit);
+        if (lane_id() == 0) lds.most[wave] = most;
+        lds.tokens[threadIdx.x] = st.token;
+    }
+    __syncthreads();
+    m = others.m;
+#pragma unroll
+    for (int w = 0; w < DS_WAVES; ++w) m = fmaxf(m, lds.most[w]);
+    const bool none = m == -INFINITY;
+    if (wave < DS_WAVES) {
+        bool first = st.token >= 0;  // a token that is stored twice counts once for the student
+        for (int i = 0; i < (int)threadIdx.x && i < t.k; ++i) first = first && lds.tokens[i] != st.token;
+        const float own = wave_sum(first && !none ? exp2_fast(c * (st.logit - m)) : 0.0f);
+        if (lane_id() == 0) lds.own[wave] = own;
+    }
+    const double p = st.token < 0 ? 0.0 : exp((double)st.logp);
+    const Mass mass = mass_of(p, t.tail, lds);  // (a barrier)
+    float own = 0.0f;
+#pragma unroll
+    for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
+    const float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
+    sum = own + rest;
+    if (wave < DS_WAVES) {
+        const double log_s = log((double)own + (double)rest);
+        double l = 0.0;
+        if (p > 0.0 || p != p) {
+            const double log_q = none ? -INFINITY : (double)scale * ((double)st.logit - (double)m) - log_s;
+            l = t.tail ? p * ((double)st.logp - log_q) : p / mass.P * ((double)st.logp - log(mass.P) - log_q);
+        }
+        l = wave_sum64(l);
+        if (lane_id() == 0) lds.loss[wave] = l;
+        if (threadIdx.x == 0) {
+            const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
+            if (o.lse) {
+                const float lse = (float)((double)scale * (double)m + log_s);  // (no float holds it: NaN)
+                o.lse[r] = none ? -INFINITY : fabsf(lse) < INFINITY ? lse : NAN;
+            }
+            if (o.log_tail) o.log_tail[r] = (float)log_tail;
+            shares(mass, t.tail, log_tail, lds.total, lds.share);
+            lds.log_tail = (float)log_tail;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double l = 0.0;
+#pragma unroll
+        for (int w = 0; w < DS_WAVES; ++w) l += lds.loss[w];
+        if (mass.rest > 0.0 && lds.log_tail != -INFINITY) l += mass.rest * (log(mass.rest) - (double)lds.log_tail);
+        o.loss[r] = (float)l;
+    }
+}
+
+// Marks the stored token if it lies in chunks j0 .. j1 - 1 of the row, whose first token is at `lead`; a barrier before and behind.
+__device__ __forceinline__ void mark(uint32_t *marks, const Stored &st, int64_t j0, int64_t j1, int lead, int threads)
+{
+    __syncthreads();
+    for (int64_t w = threadIdx.x; w < (j1 - j0) * (LP_CHUNK / 32); w += threads) marks[w] = 0;
+    __syncthreads();
+    const int64_t at = (int64_t)st.token + lead - j0 * LP_CHUNK;
+    if (st.token >= 0 && at >= 0 && at < (j1 - j0) * LP_CHUNK) atomicOr(&marks[at / 32], 1u << (at % 32));
+    __syncthreads();
+}
+// The marks of the N tokens from position `at` on, a multiple of N.
+template <int N>
+__device__ __forceinline__ unsigned marks_at(const uint32_t *marks, int at)
+{
+    const unsigned b = reinterpret_cast<const uint8_t *>(marks)[at / 8];
+    return N == 8 ? b : b >> (at % 8) & 15u;
+}
+
+// What chunks j0 .. j1 - 1 of a row have, joined over the workgroup.
+template <typename T>
+__device__ __forceinline__ Part2 chunks_part(const T *row, int64_t j0, int64_t j1, int V, int lead, float c, const Stored &st,
+                                             uint32_t *marks, Part2 *waves)
+{
+    constexpr int N = Pack<T>::N;
+    Part2 a = {-INFINITY, 0.0f};
+    for (int64_t j = j0; j < j1; ++j) {
+        const int at = (int)((j - j0) % DS_MARKED);
+        if (at == 0) mark(marks, st, j, min(j + DS_MARKED, j1), lead, LP_WG);
+        float x[LP_BLOCK];
+        load_block(row, j, V, lead, x);
+#pragma unroll
+        for (int u = 0; u < LP_BLOCK / N; ++u) {
+            const unsigned b = marks_at<N>(marks, at * LP_CHUNK + (u * LP_WG + (int)threadIdx.x) * N);
+            if (b)
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (b >> e & 1) x[u * N + e] = -INFINITY;
+        }
+        add_block(a, x, c);
+    }
+    const float m = wave_max(a.m);
+    raise(a, m, c);
+    a.s = wave_sum(a.s);
+    __syncthreads();
+    if (lane_id() == 0) waves[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = waves[0];
+#pragma unroll
+    for (int w = 1; w < LP_WG / WAVE; ++w) a = join(a, waves[w], c);
+    return a;
+}
+
+// A workgroup per row.
+template <typename T>
+__global__ __launch_bounds__(LP_WG) void distill_row_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V, float scale,
+                                                            Teacher t, Loss o)
+{
+    __shared__ uint32_t marks[DS_MARKED * LP_CHUNK / 32];
+    __shared__ Part2 waves[LP_WG / WAVE];
+    __shared__ FinishLds lds;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const T *row = logits + r * ld;
+        const int lead = lead_of(row);
+        const Stored st = stored_of(row, r, V, t);
+        const Part2 a = chunks_part(row, 0, chunks_of(V, lead), V, lead, scale * LOG2E, st, marks, waves);
+        float m, sum;
+        finish_row(a, st, r, scale, t, o, lds, m, sum);
+    }
+}
+
+// A workgroup per `per` chunks of a row, into the workspace.
+template <typename T>
+__global__ __launch_bounds__(LP_WG) void distill_part_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V, float scale,
+                                                             Teacher t, int parts, int per, Part2 *__restrict__ stats)
+{
+    __shared__ uint32_t marks[DS_MARKED * LP_CHUNK / 32];
+    __shared__ Part2 waves[LP_WG / WAVE];
+    for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
+        const int64_t r = i / parts, j0 = i % parts * per;
+        const T *row = logits + r * ld;
+        const int lead = lead_of(row);
+        Stored st = {-1, 0.0f, 0.0f};
+        if ((int)threadIdx.x < t.k) {
+            const uint32_t v = t.idx[r * t.k + threadIdx.x];
+            if (v < (uint32_t)V) st.token = (int)v;
+        }
+        const Part2 a = chunks_part(row, j0, min(j0 + per, chunks_of(V, lead)), V, lead, scale * LOG2E, st, marks, waves);
+        if (threadIdx.x == 0) stats[i] = a;
+    }
+}
+template <typename T>
+__global__ __launch_bounds__(LP_WG) void distill_join_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V, float scale,
+                                                             Teacher t, int parts, const Part2 *__restrict__ stats, Loss o)
+{
+    __shared__ Part2 waves[LP_WG / WAVE];
+    __shared__ FinishLds lds;
+    const float c = scale * LOG2E;
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
+        const Stored st = stored_of(logits + r * ld, r, V, t);
+        Part2 a = {-INFINITY, 0.0f};
+        for (int p = threadIdx.x; p < parts; p += LP_WG) a = join(a, stats[r * parts + p], c);
+        const float m = wave_max(a.m);
+        raise(a, m, c);
+        a.s = wave_sum(a.s);
+        __syncthreads();
+        if (lane_id() == 0) waves[threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = waves[0];
+#pragma unroll
+        for (int w = 1; w < LP_WG / WAVE; ++w) a = join(a, waves[w], c);
+        float most, sum;
+        finish_row(a, st, r, scale, t, o, lds, most, sum);
+    }
+}
+
+// The stored tokens' gradients, each token once: value(logit) is what a stored token has from the student, own the teacher's share.
+struct GradLds {
+    int tokens[QADC_MAX_ALTERNATIVES];
+    float p[QADC_MAX_ALTERNATIVES];
+};
+template <typename T, typename F>
+__device__ __forceinline__ void write_stored(T *out, const Stored &st, int k, const GradLds &lds, F value)
+{
+    if (st.token < 0) return;
+    float p = 0.0f;
+    bool first = true;
+    for (int i = 0; i < k; ++i)
+        if (lds.tokens[i] == st.token) {
+            first = first && i >= (int)threadIdx.x;
+            p += lds.p[i];
+        }
+    if (first) out[st.token] = (T)value(st.logit, p);
+}
+
+// A workgroup per `per` chunks of a row: first every token's share as if it was not stored, then the stored tokens.
+template <typename T>
+__global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, int64_t ld, int64_t rows, int V, float scale, Teacher t,
+                                                             int parts, int per, const float *__restrict__ lse,
+                                                             const float *__restrict__ log_tail, const float *__restrict__ dloss,
+                                                             T *dlogits, int64_t ldd)
+{
+    constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
+    __shared__ FinishLds lds;
+    __shared__ GradLds grad;
+    for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
+        const int64_t r = i / parts;
+        const T *row = logits + r * ld;
+        T *out = dlogits + r * ldd;
+        const int lead = lead_of(out);
+        const int64_t j0 = i % parts * per, j1 = min(j0 + per, chunks_of(V, lead));
+        const int64_t v0 = max((int64_t)0, j0 * LP_CHUNK - lead), v1 = min(j1 * LP_CHUNK - lead, (int64_t)V);
+        const float l = lse[r], w = scale * dloss[r];
+        const bool zero = w == 0.0f || l == -INFINITY;  // (a row without a share of the loss is not read)
+        Stored st = {-1, -INFINITY, -INFINITY};
+        double p = 0.0;
+        if ((int)threadIdx.x < t.k && !zero) {
+            const uint32_t v = t.idx[r * t.k + threadIdx.x];
+            if (v < (uint32_t)V) {
+                p = exp((double)t.logp[r * t.k + threadIdx.x]);
+                if ((int64_t)v >= v0 && (int64_t)v < v1) {
+                    st.token = (int)v;
+                    st.logit = (float)row[v];
+                }
+            }
+        }
+        const Mass mass = mass_of(p, t.tail, lds);
+        float total, share;
+        shares(mass, t.tail, (double)log_tail[r], total, share);
+        if ((int)threadIdx.x < t.k) {
+            grad.tokens[threadIdx.x] = st.token;
+            grad.p[threadIdx.x] = (float)(t.tail ? p : mass.P > 0.0 ? p / mass.P : 0.0);
+        }
+        const float f = w * share;
+        const auto value = [&](float logit) { return zero ? 0.0f : f * exp_of<T>(fmaf(scale, logit, -l)); };
+        for (int64_t j = j0; j < j1; ++j) {
+            typename Pack<T>::V q[PACKS];
+            if ((j > 0 || lead == 0) && (j + 1) * LP_CHUNK - lead <= v1) {
+                if (!zero)
+#pragma unroll
+                    for (int u = 0; u < PACKS; ++u)
+                        q[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T>::V *>(row + pack_at<T>(j, u, lead)));
+#pragma unroll
+                for (int u = 0; u < PACKS; ++u) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) q[u][e] = (T)value((float)q[u][e]);
+                    *reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead)) = q[u];
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < PACKS; ++u) q[u] = load_edge(row, pack_at<T>(j, u, lead), v1, 0.0f);
+#pragma unroll
+                for (int u = 0; u < PACKS; ++u) {
+                    const int64_t at = pack_at<T>(j, u, lead);
+                    if (at >= v1) continue;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) q[u][e] = (T)value((float)q[u][e]);
+                    if (at >= 0 && at + N <= v1) {
+                        *reinterpret_cast<typename Pack<T>::V *>(out + at) = q[u];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < N; ++e)
+                            if (at + e >= 0 && at + e < v1) out[at + e] = q[u][e];
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        write_stored(out, st, t.k, grad, [&](float logit, float own) { return w * fmaf(total, exp_of<T>(fmaf(scale, logit, -l)), -own); });
+        __syncthreads();
+    }
+}
+
+// Loss and gradient of a row whose logits stay in the registers of its workgroup: PACKS packs a thread, read and written once.
+template <typename T, int THREADS, int PACKS>
+__global__ __launch_bounds__(THREADS) void distill_step_kernel(const T *logits, int64_t ld, int V, float scale, Teacher t,
+                                                               const float *__restrict__ weight, Loss o, T *dlogits, int64_t ldd)
+{
+    constexpr int N = Pack<T>::N, W = THREADS / WAVE;
+    typedef typename Pack<T>::V P;
+    __shared__ uint32_t marks[THREADS * PACKS * N / 32];
+    __shared__ float waves[2][W];
+    __shared__ FinishLds lds;
+    __shared__ GradLds grad;
+    const int64_t r = blockIdx.x;
+    const T *row = logits + r * ld;
+    T *out = dlogits + r * ldd;
+    const int lead = lead_of(row);
+    const float c = scale * LOG2E;
+    P x[PACKS];
+#pragma unroll
+    for (int u = 0; u < PACKS; ++u) {
+        const int at = (u * THREADS + (int)threadIdx.x) * N - lead;
+        x[u] = load_edge(row, at, V, -INFINITY);
+    }
+    Stored st = stored_of(row, r, V, t);
+    for (int i = threadIdx.x; i < THREADS * PACKS * N / 32; i += THREADS) marks[i] = 0;
+    __syncthreads();
+    if (st.token >= 0) atomicOr(&marks[(st.token + lead) / 32], 1u << ((st.token + lead) % 32));
+    __syncthreads();
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < PACKS; ++u) {
+        const unsigned b = marks_at<N>(marks, (u * THREADS + (int)threadIdx.x) * N);
+        if (b)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (b >> e & 1) x[u][e] = (T)-INFINITY;
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = fmaxf(m, (float)x[u][e]);
+    }
+    m = wave_max(m);
+    if (lane_id() == 0) waves[0][threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = waves[0][0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, waves[0][w]);
+    const float m0 = m == -INFINITY ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int u = 0; u < PACKS; ++u) {
+        float part = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) part += exp2_fast(c * ((float)x[u][e] - m0));
+        s += part;
+    }
+    s = wave_sum(s);
+    if (lane_id() == 0) waves[1][threadIdx.x >> 6] = s;
+    __syncthreads();
+    s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) s += waves[1][w];
+    float most, sum;
+    finish_row({m, s}, st, r, scale, t, o, lds, most, sum);
+    __syncthreads();
+    const float w = scale * weight[r];
+    const bool zero = w == 0.0f || most == -INFINITY;
+    if (threadIdx.x < QADC_MAX_ALTERNATIVES && (int)threadIdx.x < t.k) {
+        double P = 0.0;
+#pragma unroll
+        for (int i = 0; i < DS_WAVES; ++i) P += lds.mass[i];
+        const double p = st.token < 0 ? 0.0 : exp((double)st.logp);
+        grad.tokens[threadIdx.x] = st.token;
+        grad.p[threadIdx.x] = (float)(t.tail ? p : P > 0.0 ? p / P : 0.0);
+    }
+    const float f = w * lds.share / sum;
+    const auto q_of = [&](float logit) { return exp2_fast(c * (logit - most)); };
+#pragma unroll
+    for (int u = 0; u < PACKS; ++u) {
+        const int at = (u * THREADS + (int)threadIdx.x) * N - lead;
+        if (at >= V) continue;
+        P g;
+#pragma unroll
+        for (int e = 0; e < N; ++e) g[e] = (T)(zero ? 0.0f : f * q_of((float)x[u][e]));
+        if (at >= 0 && at + N <= V) {
+            __builtin_nontemporal_store(g, reinterpret_cast<P *>(out + at));
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (at + e >= 0 && at + e < V) out[at + e] = g[e];
+        }
+    }
+    __syncthreads();
+    if (!zero) write_stored(out, st, t.k, grad, [&](float logit, float own) { return w * fmaf(lds.total, q_of(logit) / sum, -own); });
+}
+
+int check_distill(const char *who, int type, int64_t ld, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k)
+{
+    if (!type_ok(type)) return fail(QADC_EINVAL, "%s: unknown type %d", who, type);
+    // (tokens are counted in an int, a chunk past the last one)
+    if (rows < 0 || V < 1 || V > INT32_MAX - 65536 || ld < V)
+        return fail(QADC_EINVAL, "%s: rows=%lld V=%d ld=%lld", who, (long long)rows, V, (long long)ld);
+    if (!(scale > 0.0f) || !(scale * LOG2E < INFINITY)) return fail(QADC_EINVAL, "%s: scale=%g", who, (double)scale);
+    if (k < 0 || k > QADC_MAX_ALTERNATIVES) return fail(QADC_EINVAL, "%s: k=%d", who, k);
+    if (rows > 0 && k > 0 && (!idx || !logp)) return fail(QADC_EINVAL, "%s: null pointer", who);
+    return QADC_OK;
+}
+
+// How the loss of a call is cut: a row per workgroup where the rows alone nearly fill the chip, parts of rows otherwise.
+constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024;
+struct Cut {
+    int parts, per;
+};
+Cut cut_of(int64_t rows, int V)
+{
+    const int64_t chunks = ceil_div((int64_t)V + 7, LP_CHUNK);  // (a row begins up to seven logits into its first pack)
+    const int64_t want = rows >= DS_WHOLE ? 1 : ceil_div(DS_PARTS, std::max<int64_t>(1, rows));
+    const int per = (int)ceil_div(chunks, std::min(chunks, want));
+    return {(int)ceil_div(chunks, per), per};
+}
+
+}  // namespace
+
+// Parts of rows, then lse and log Q for a gradient that follows: enough for these rows and for any fewer, and for shorter ones.
+static size_t part_bytes(int64_t rows, int V)
+{
+    const int64_t chunks = ceil_div((int64_t)V + 7, LP_CHUNK), few = std::min(rows, DS_WHOLE - 1);
+    return align_up((size_t)std::min(few * chunks, DS_PARTS + few) * sizeof(Part2), 256);
+}
+size_t distill_workspace(int64_t rows, int V)
+{
+    if (rows < 1 || V < 1 || V > INT32_MAX - 65536) return 0;
+    return part_bytes(rows, V) + 2 * align_up((size_t)rows * sizeof(float), 256);
+}
+
+template <typename T>
+static void launch_loss(const void *logits, int64_t ld, int64_t rows, int V, float scale, const Teacher &t, const Loss &o, void *workspace,
+                        hipStream_t st)
+{
+    const Cut p = cut_of(rows, V);
+    const dim3 grid((unsigned)std::min<int64_t>(rows, 1 << 20));
+    if (p.parts == 1) {
+        launch(QADC_PROF_DISTILL, distill_row_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows, V, scale, t, o);
+        return;
+    }
+    launch(QADC_PROF_DISTILL, distill_part_kernel<T>, dim3((unsigned)std::min<int64_t>(rows * p.parts, 1 << 20)), dim3(LP_WG), 0, st,
+           (const T *)logits, ld, rows, V, scale, t, p.parts, p.per, (Part2 *)workspace);
+    launch(QADC_PROF_DISTILL, distill_join_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows, V, scale, t, p.parts,
+           (const Part2 *)workspace, o);
+}
+
+template <typename T>
+static void launch_grad(const void *logits, int64_t ld, int64_t rows, int V, float scale, const Teacher &t, const float *lse,
+                        const float *log_tail, const float *dloss, void *dlogits, int64_t ldd, hipStream_t st)
+{
+    // (where rows begin off 16 bytes, up to seven logits into their first pack)
+    const bool even = (uintptr_t)dlogits % 16 == 0 && (size_t)ldd * sizeof(T) % 16 == 0;
+    const int64_t chunks = ceil_div((int64_t)V + (even ? 0 : 7), LP_CHUNK);
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));
+    const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
+    launch(QADC_PROF_DISTILL, distill_grad_kernel<T>, dim3((unsigned)std::min<int64_t>(rows * parts, 1 << 22)), dim3(LP_WG), 0, st,
+           (const T *)logits, ld, rows, V, scale, t, parts, per, lse, log_tail, dloss, (T *)dlogits, ldd);
+}
+
+int distill(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k,
+            int tail, float *loss, float *lse, float *log_tail, void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    const char *who = "qadc_distill";
+    if (const int rc = check_distill(who, type, ld, rows, V, scale, idx, logp, k)) return rc;
+    if (rows == 0) return QADC_OK;
+    if (!logits || !loss) return fail(QADC_EINVAL, "%s: null pointer", who);
+    const Cut p = cut_of(rows, V);
+    const size_t need = p.parts > 1 ? (size_t)rows * p.parts * sizeof(Part2) : 0;
+    if (need && (!workspace || workspace_bytes < need))
+        return fail(QADC_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, need);
+    if (need && (uintptr_t)workspace % 16) return fail(QADC_EINVAL, "%s: workspace is not aligned to 16 bytes", who);
+    const Teacher t = {idx, logp, k, tail != 0};
+    QADC_BY_TYPE(type, (launch_loss<T>(logits, ld, rows, V, scale, t, {loss, lse, log_tail}, workspace, st)));
+    QADC_HIP_TRY(hipGetLastError());
+    return QADC_OK;
+}
+
+int distill_backward(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp,
+                     int k, int tail, const float *lse, const float *log_tail, const float *dloss, void *dlogits, int64_t ldd,
+                     hipStream_t st)
+{
+    const char *who = "qadc_distill_backward";
+    if (const int rc = check_distill(who, type, ld, rows, V, scale, idx, logp, k)) return rc;
+    if (ldd < V) return fail(QADC_EINVAL, "%s: ldd=%lld", who, (long long)ldd);
+    if (rows == 0) return QADC_OK;
+    if (!logits || !lse || !log_tail || !dloss || !dlogits) return fail(QADC_EINVAL, "%s: null pointer", who);
+    if (logits == dlogits && ld != ldd) return fail(QADC_EINVAL, "%s: in place needs equal row distances", who);
+    const Teacher t = {idx, logp, k, tail != 0};
+    QADC_BY_TYPE(type, (launch_grad<T>(logits, ld, rows, V, scale, t, lse, log_tail, dloss, dlogits, ldd, st)));
+    QADC_HIP_TRY(hipGetLastError());
+    return QADC_OK;
+}
+
+template <typename T, int THREADS, int PACKS>
+static void launch_step(const void *logits, int64_t ld, int64_t rows, int V, float scale, const Teacher &t, const float *weight,
+                        const Loss &o, void *dlogits, int64_t ldd, hipStream_t st)
+{
+    launch(QADC_PROF_DISTILL, distill_step_kernel<T, THREADS, PACKS>, dim3((unsigned)rows), dim3(THREADS), 0, st, (const T *)logits, ld, V,
+           scale, t, weight, o, (T *)dlogits, ldd);
+}
+
+int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k,
+                 int tail, const float *weight, float *loss, void *dlogits, int64_t ldd, void *workspace, size_t workspace_bytes,
+                 hipStream_t st)
+{
+    const char *who = "qadc_distill_step";
+    if (const int rc = check_distill(who, type, ld, rows, V, scale, idx, logp, k)) return rc;
+    if (ldd < V) return fail(QADC_EINVAL, "%s: ldd=%lld", who, (long long)ldd);
+    if (rows == 0) return QADC_OK;
+    if (!logits || !weight || !loss || !dlogits) return fail(QADC_EINVAL, "%s: null pointer", who);
+    if (logits == dlogits && ld != ldd) return fail(QADC_EINVAL, "%s: in place needs equal row distances", who);
+    const Cut p = cut_of(rows, V);
+    const size_t stats = align_up(p.parts > 1 ? (size_t)rows * p.parts * sizeof(Part2) : 0, 256), each = align_up((size_t)rows * 4, 256);
+    if (!workspace || workspace_bytes < stats + 2 * each)
+        return fail(QADC_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, stats + 2 * each);
+    if ((uintptr_t)workspace % 16) return fail(QADC_EINVAL, "%s: workspace is not aligned to 16 bytes", who);
+    const Teacher t = {idx, logp, k, tail != 0};
+    float *lse = (float *)((char *)workspace + stats), *log_tail = (float *)((char *)workspace + stats + each);
+    const size_t e = type_bytes(type);
+    const bool even = (uintptr_t)logits % 16 == 0 && (size_t)ld * e % 16 == 0;
+    const size_t bytes = ((size_t)V + (even ? 0 : 16 / e - 1)) * e;
+    if (rows >= 128 && rows < 1 << 30 && bytes <= 262144) {
+        QADC_BY_TYPE(type, {
+            const Loss o = {loss, nullptr, nullptr};
+            if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+            else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+            else if (bytes <= 65536) launch_step<T, 256, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+            else if (bytes <= 131072) launch_step<T, 512, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+            else launch_step<T, 1024, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+        });
+    } else {
+        QADC_BY_TYPE(type, {
+            launch_loss<T>(logits, ld, rows, V, scale, t, {loss, lse, log_tail}, workspace, st);
+            launch_grad<T>(logits, ld, rows, V, scale, t, lse, log_tail, weight, dlogits, ldd, st);
+        });
+    }
+    QADC_HIP_TRY(hipGetLastError());
+    return QADC_OK;
+}
+
+}  // namespace qadc

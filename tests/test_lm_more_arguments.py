@@ -56,3 +56,28 @@ def test_adjust_logits():
                 dict(masks=PTR, ldm=2, states=0), dict(masks=PTR, ldm=2, states=2), dict(out=PTR, ldo=65)):
         assert f(**bad) == Q.QADC_EINVAL, bad
     assert b"qadc_adjust_logits" in L.qadc_last_error()
+
+
+def test_distill():
+    L = Q.lib()
+    need = Q.qadc_distill_workspace_bytes(3, 100000)
+    assert need > 0 and Q.qadc_distill_workspace_bytes(0, 10) == 0 and Q.qadc_distill_workspace_bytes(3, 0) == 0
+    ok = dict(x=PTR, ld=100000, type=0, rows=3, V=100000, scale=1.0, idx=PTR, logp=PTR, k=5, tail=1)
+    loss = dict(loss=PTR, lse=PTR, log_tail=PTR, ws=PTR, size=need, stream=None)
+    grad = dict(lse=PTR, log_tail=PTR, dloss=PTR, out=2 * PTR, ldo=100000, stream=None)
+    step = dict(weight=PTR, loss=PTR, out=2 * PTR, ldo=100000, ws=PTR, size=need, stream=None)
+    for name, more, own in (("qadc_distill", loss, (dict(loss=None),)),
+                            ("qadc_distill_backward", grad, (dict(lse=None), dict(log_tail=None), dict(dloss=None), dict(out=None),
+                                                             dict(ldo=99999), dict(out=PTR, ldo=100001))),
+                            ("qadc_distill_step", step, (dict(weight=None), dict(loss=None), dict(out=None), dict(ldo=99999),
+                                                         dict(out=PTR, ldo=100001)))):
+        def f(**k):
+            return getattr(L, name)(*{**ok, **more, **k}.values())
+
+        assert f(x=None, rows=0) == Q.QADC_OK
+        for bad in (dict(x=None), dict(type=3), dict(rows=-1), dict(V=0), dict(V=2 ** 31 - 1, ld=2 ** 31), dict(ld=99999), dict(scale=0.0),
+                    dict(scale=float("nan")), dict(scale=3e38), dict(k=-1), dict(k=129), dict(idx=None), dict(logp=None)) + own:
+            assert f(**bad) == Q.QADC_EINVAL, (name, bad)
+        assert name.encode() + b":" in L.qadc_last_error()
+        if "ws" in more:
+            assert f(ws=None) == Q.QADC_ENOMEM and f(size=16) == Q.QADC_ENOMEM and f(ws=PTR + 8) == Q.QADC_EINVAL
