@@ -535,6 +535,42 @@ int qadc_linear4(const qadc_weights4 *w, const void *x, int64_t ldx, int type, i
                  int64_t ldy, void *stream);
 
 /*
+ * Low-rank adapters of many requests beside a projection that they share (qadc_linear4's output as `base`): row i of the batch has
+ * the adapter ids[i], and
+ *     y[i][n] = base[i][n] + scale * sum_j b[n][j] (sum_k a[j][k] x[i][k])
+ * with sums in float32, rounded once to `type`.  Between the two products the sums over k are kept to 2^-16 of their value
+ * (bfloat16), to 2^-22 of it and 2^-35 of the row's largest (binary16), or in float32.  Adapters lie in a pool with room for `rank` ranks each:
+ *   a [count][rank][K], b [count][N][rank] of `type`;  scales [count] f32 or NULL (1)
+ *   ranks [count] i32 or NULL: how many of an adapter's ranks are used, 0 to rank (rank); what lies beyond is not looked at
+ *   type  of the pool, x, base and y;  1 <= N <= 2^30, 1 <= K <= 2^24, 1 <= rank <= QADC_MAX_RANK, 1 <= count <= 2^20
+ * The struct lives in host memory, its pointers are device pointers.
+ */
+#define QADC_MAX_RANK 128
+typedef struct qadc_adapters {
+    const void *a, *b;
+    const float *scales;
+    const int32_t *ranks;
+    int64_t N;  /* outputs */
+    int K;      /* inputs */
+    int rank;
+    int count;
+    int type;
+} qadc_adapters;
+
+/*
+ *   ids [M] i32: a number outside [0, count) is a row without an adapter, y = base
+ *   x [M][ldx], base [M][ldb] (or NULL: 0) of `type`, 0 <= M <= 2^24, (M / 256) * (N / 2048) at most about 2^20
+ *   y [M][ldy] of `type` (output; may be base when ldb == ldy: then rows without an adapter are not touched; must not overlap x)
+ *   workspace >= qadc_adapters_workspace_bytes(adapters, M), 16-byte aligned; it need not be cleared and is not left cleared, and
+ *   serves fewer rows too
+ * Rows are independent of each other: an infinity or a NaN in one (it gives NaN or infinities) does not reach the others, and
+ * sums are added in a fixed order: equal calls give equal bits.
+ */
+int qadc_add_adapters(const qadc_adapters *adapters, const int32_t *ids, const void *x, int64_t ldx, int64_t M, const void *base,
+                      int64_t ldb, void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+size_t qadc_adapters_workspace_bytes(const qadc_adapters *adapters, int64_t M);
+
+/*
  * Log probabilities of given tokens, with the entropy and the likeliest alternatives.  For every row, with
  * x[v] = scale * logits[v]:
  *     lse = log sum_v exp x[v],  logp[t] = x[tokens[t]] - lse,  entropy = lse - sum_v p[v] x[v],  p = exp(x - lse),

@@ -31,12 +31,14 @@ QADC_LAYOUT_STANDARD, QADC_LAYOUT_TRANSPOSED = 0, 1
 QADC_TYPE_F32, QADC_TYPE_F16, QADC_TYPE_BF16, QADC_TYPE_E4M3 = 0, 1, 2, 3
 QADC_MAX_ALTERNATIVES = 128
 QADC_MAX_HISTORY = 1 << 24
+QADC_MAX_RANK = 128
 
 EXPORTS = (
     "qadc_layer_norm", "qadc_layer_norm_backward", "qadc_layer_norm_workspace_bytes",
     "qadc_rms_norm", "qadc_rms_norm_backward", "qadc_rms_norm_workspace_bytes",
     "qadc_weights4_bytes", "qadc_pack_weights4", "qadc_linear4",
     "qadc_token_logprobs", "qadc_token_logprobs_workspace_bytes", "qadc_token_logprobs_backward", "qadc_neighbour_mix",
+    "qadc_add_adapters", "qadc_adapters_workspace_bytes",
     "qadc_adjust_logits", "qadc_distill", "qadc_distill_workspace_bytes", "qadc_distill_backward", "qadc_distill_step",
     "qadc_build_luts", "qadc_quantize_luts", "qadc_quantize_luts_8bit", "qadc_quantize_luts_6bit", "qadc_scan_topk", "qadc_search", "qadc_ivf_search",
     "qadc_ivf_workspace_bytes", "qadc_pq_encode", "qadc_pq_train", "qadc_rotate",
@@ -63,6 +65,22 @@ class qadc_weights4(ctypes.Structure):
     """Mirror of the C struct (include/qadc.h); `tensor` keeps the packed weights alive."""
     _fields_ = [("packed", ctypes.c_void_p), ("N", ctypes.c_int64), ("K", ctypes.c_int), ("group", ctypes.c_int),
                 ("stype", ctypes.c_int), ("has_zeros", ctypes.c_int)]
+
+
+class qadc_adapters(ctypes.Structure):
+    """Mirror of the C struct (include/qadc.h), made of a pool: a [count][rank][K] and b [count][N][rank] (f32, f16 or bf16), scales
+    f32 [count] | None, ranks i32 [count] | None; `tensors` keeps them alive."""
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ranks", ctypes.c_void_p),
+                ("N", ctypes.c_int64), ("K", ctypes.c_int), ("rank", ctypes.c_int), ("count", ctypes.c_int), ("type", ctypes.c_int)]
+
+    def __init__(self, a, b, scales=None, ranks=None):
+        if a.dim() != 3 or b.dim() != 3 or (b.shape[0], b.shape[2]) != (a.shape[0], a.shape[1]):
+            raise ValueError("expected a [count][rank][K] and b [count][N][rank]")
+        count, rank, K = a.shape
+        _ptr(a), _ptr(b, a.dtype)
+        super().__init__(a.data_ptr(), b.data_ptr(), _vector(scales, count, torch.float32), _vector(ranks, count, torch.int32),
+                         b.shape[1], K, rank, count, _type(a))
+        self.dtype, self.tensors = a.dtype, (a, b, scales, ranks)
 
 
 class QadcError(RuntimeError):
@@ -184,6 +202,10 @@ def lib() -> ctypes.CDLL:
         L.qadc_distill_backward.restype = i32
         L.qadc_distill_step.argtypes = [vp, i64, i32, i64, i32, f32, vp, vp, i32, i32, vp, vp, vp, i64, vp, sz, vp]
         L.qadc_distill_step.restype = i32
+        L.qadc_add_adapters.argtypes = [ctypes.POINTER(qadc_adapters), vp, vp, i64, i64, vp, i64, vp, i64, vp, sz, vp]
+        L.qadc_add_adapters.restype = i32
+        L.qadc_adapters_workspace_bytes.argtypes = [ctypes.POINTER(qadc_adapters), i64]
+        L.qadc_adapters_workspace_bytes.restype = sz
         L.qadc_last_error.restype = ctypes.c_char_p
         L.qadc_version.restype = ctypes.c_char_p
         _lib = L
@@ -875,6 +897,34 @@ def qadc_token_logprobs_backward(logits, tokens, lse, entropy, dlogp, dentropy=N
                                               _vector(entropy, rows, torch.float32),
                                               _vector(dlogp, rows * T, torch.float32) if T else None,
                                               _vector(dentropy, rows, torch.float32), op, ldd, _stream()))
+    return out
+
+
+def qadc_adapters_workspace_bytes(adapters, M: int) -> int:
+    return int(lib().qadc_adapters_workspace_bytes(ctypes.byref(adapters), M))
+
+
+def qadc_add_adapters(adapters, ids, x, base=None, out=None, workspace=None):
+    """adapters: a qadc_adapters, ids i32 [M], x [M][K] and base [M][N] | None of the pool's type (rows may lie apart)
+    -> y [M][N]: base + each row's own adapter's product with x (out may be base)."""
+    M, K = x.shape
+    if K != adapters.K:
+        raise ValueError(f"adapters of {adapters.K} inputs, x of {K}")
+    xp, ldx = _matrix(x, adapters.dtype)
+    bp, ldb = None, adapters.N
+    if base is not None:
+        if tuple(base.shape) != (M, adapters.N):
+            raise ValueError(f"base must be {(M, adapters.N)}")
+        bp, ldb = _matrix(base, adapters.dtype)
+    if out is None:
+        out = torch.empty(M, adapters.N, dtype=adapters.dtype, device=x.device)
+    elif tuple(out.shape) != (M, adapters.N):
+        raise ValueError(f"output must be {(M, adapters.N)}")
+    yp, ldy = _matrix(out, adapters.dtype)
+    if workspace is None:
+        workspace = torch.empty((max(256, qadc_adapters_workspace_bytes(adapters, M)),), dtype=torch.uint8, device=x.device)
+    _check(lib().qadc_add_adapters(ctypes.byref(adapters), _vector(ids, M, torch.int32), xp, ldx, M, bp, ldb, yp, ldy, _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream()))
     return out
 
 

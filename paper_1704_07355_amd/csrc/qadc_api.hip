@@ -112,6 +112,9 @@ int token_logprobs(const void *, int64_t, int, int64_t, int, float, const int32_
 size_t token_logprobs_workspace(int64_t, int, int);
 int token_logprobs_backward(const void *, int64_t, int, int64_t, int, float, const int32_t *, int, const float *, const float *,
                             const float *, const float *, void *, int64_t, hipStream_t);
+int add_adapters(const qadc_adapters *, const int32_t *, const void *, int64_t, int64_t, const void *, int64_t, void *, int64_t, void *,
+                 size_t, hipStream_t);
+size_t adapters_workspace(const qadc_adapters *, int64_t);
 int distill(const void *, int64_t, int, int64_t, int, float, const uint32_t *, const float *, int, int, float *, float *, float *, void *,
             size_t, hipStream_t);
 size_t distill_workspace(int64_t, int);
@@ -377,6 +380,14 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
     return qadc::token_logprobs_backward(logits, ld, type, rows, V, scale, tokens, T, lse, entropy, dlogp, dentropy, dlogits,
                                          ldd, (hipStream_t)stream);
 }
+
+int qadc_add_adapters(const qadc_adapters *adapters, const int32_t *ids, const void *x, int64_t ldx, int64_t M, const void *base,
+                      int64_t ldb, void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return qadc::add_adapters(adapters, ids, x, ldx, M, base, ldb, y, ldy, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+size_t qadc_adapters_workspace_bytes(const qadc_adapters *adapters, int64_t M) { return qadc::adapters_workspace(adapters, M); }
 
 int qadc_distill(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,
                  const float *top_logp, int k, int tail, float *loss, float *lse, float *log_tail, void *workspace,

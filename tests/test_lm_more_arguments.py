@@ -81,3 +81,36 @@ def test_distill():
         assert name.encode() + b":" in L.qadc_last_error()
         if "ws" in more:
             assert f(ws=None) == Q.QADC_ENOMEM and f(size=16) == Q.QADC_ENOMEM and f(ws=PTR + 8) == Q.QADC_EINVAL
+
+
+def test_add_adapters():
+    import ctypes
+    L = Q.lib()
+
+    def pool(**k):
+        w = Q.qadc_adapters.__new__(Q.qadc_adapters)
+        for name, v in dict(dict(a=PTR, b=PTR, N=500, K=3000, rank=16, count=4, type=1), **k).items():
+            setattr(w, name, v)
+        return w
+
+    w = pool()
+    need = Q.qadc_adapters_workspace_bytes(w, 64)
+    assert need > 0 and Q.qadc_adapters_workspace_bytes(w, 0) == 0
+    assert all(Q.qadc_adapters_workspace_bytes(w, m) <= Q.qadc_adapters_workspace_bytes(w, 5000) for m in range(1, 5000, 37))
+    ok = dict(w=w, ids=PTR, x=PTR, ldx=3000, M=64, base=2 * PTR, ldb=500, y=3 * PTR, ldy=500, ws=PTR, size=need, stream=None)
+
+    def f(**k):
+        a = dict(ok, **k)
+        a["w"] = None if a["w"] is None else ctypes.byref(a["w"])
+        return L.qadc_add_adapters(*a.values())
+
+    assert f(M=0, ids=None, x=None, y=None) == Q.QADC_OK
+    for bad in (dict(w=None), dict(ids=None), dict(x=None), dict(y=None), dict(ldx=2999), dict(ldb=499), dict(ldy=499), dict(M=-1),
+                dict(M=(1 << 24) + 1), dict(y=2 * PTR, ldb=501), dict(ws=PTR + 8)):
+        assert f(**bad) == Q.QADC_EINVAL, bad
+    for k, v in (("a", None), ("b", None), ("N", 0), ("N", (1 << 30) + 1), ("K", 0), ("rank", 0), ("rank", 129), ("count", 0), ("type", 3)):
+        assert f(w=pool(**{k: v}), ldx=1 << 25, ldb=1 << 31, ldy=1 << 31) == Q.QADC_EINVAL, (k, v)
+    assert f(ws=None) == Q.QADC_ENOMEM and f(size=16) == Q.QADC_ENOMEM
+    assert b"qadc_add_adapters" in L.qadc_last_error()
+    # more workgroups than a launch takes
+    assert f(w=pool(N=1 << 30, count=300), M=1 << 24, ldb=1 << 30, ldy=1 << 30, size=1 << 40) == Q.QADC_EINVAL
