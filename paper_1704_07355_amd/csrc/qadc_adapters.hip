@@ -18,20 +18,24 @@ namespace qadc {
 namespace {
 
 constexpr int AD_WG = 256, AD_TILE = 256;  // threads; rows of a tile, one a thread
+constexpr int64_t AD_MANY = 1024;          // rows from which on an item has 64 of them, if each adapter has as many
 constexpr int AD_COLS = 64;                // outputs of a wavefront at a time
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
 
-// Eight consecutive elements, of which n are there; zeros behind.
+// Eight consecutive elements.
 template <typename T>
 struct Eight {
     typedef T V __attribute__((ext_vector_type(8)));
     typedef T Raw __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     typedef T Lds __attribute__((ext_vector_type(8), aligned(16)));
     static __device__ __forceinline__ V zero() { return (V)(T)0.0f; }
+    static __device__ __forceinline__ V load(const T *p) { return *reinterpret_cast<const Raw *>(p); }
+    // n of them are there, zeros behind
     static __device__ __forceinline__ V load(const T *p, int n)
     {
-        if (n >= 8) return *reinterpret_cast<const Raw *>(p);
+        if (n >= 8) return load(p);
         V v = zero();
 #pragma unroll
         for (int e = 0; e < 7; ++e)
@@ -57,70 +61,97 @@ __device__ __forceinline__ f32x4 mma(Eight<float>::V a, Eight<float>::V b, f32x4
     return c;
 }
 
-// A tile's rows by adapter: thread i has row i of the tile in item `item` at `place`; items are numbered by their first rows.
-struct Items {
-    int item, place;
+// A tile's rows by adapter, by each wavefront for itself: lane l has the adapters of rows l, 64 + l, 128 + l and 192 + l, and the rows of
+// one adapter are the bits of four ballots.
+struct Tile {
+    static constexpr int W = AD_TILE / WAVE;
+    int id[W];                      // -1: none
+    unsigned long long left[W];     // rows that are there and belong to no item so far
 };
-struct ItemsLds {
-    __attribute__((aligned(16))) int ids[AD_TILE];
-    int number[AD_TILE];  // of the item that a row opens
-    int id[AD_TILE];      // of an item
-    int opened[AD_TILE / WAVE];
-    int16_t rows[64];     // of the item at hand, -1: none
+struct Item {
+    int id;
+    unsigned long long rows[Tile::W];
+    int count;
 };
-
-// ROWS of them to an item; -1 as id: no adapter.  Returns the number of items.
-template <int ROWS>
-__device__ __forceinline__ int group_rows(const int32_t *ids, int64_t first, int rows, int count, Items &mine, ItemsLds &lds)
+__device__ __forceinline__ Tile load_tile(const int32_t *ids, int64_t first, int rows, int count)
 {
-    const int i = threadIdx.x;
-    int id = -2;  // behind the last row
-    if (i < rows) {
-        id = ids[first + i];
+    Tile t;
+#pragma unroll
+    for (int w = 0; w < Tile::W; ++w) {
+        const int i = w * WAVE + lane_id();
+        int id = i < rows ? ids[first + i] : -1;
         if (id < 0 || id >= count) id = -1;
+        t.id[w] = id;
+        t.left[w] = __ballot(i < rows);
     }
-    lds.ids[i] = id;
-    __syncthreads();
-    int before = 0, opener = i;
-    for (int j = 0; j < i && j < rows; j += 4) {
-        const int4 v = *reinterpret_cast<const int4 *>(&lds.ids[j]);
-        const int w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (w[e] == id && j + e < i) {
-                if (before % ROWS == 0) opener = j + e;
-                ++before;
-            }
-    }
-    const bool opens = i < rows && before % ROWS == 0;
-    if (opens) opener = i;
-    const unsigned long long m = __ballot(opens);
-    if (lane_id() == 0) lds.opened[i >> 6] = __popcll(m);
-    __syncthreads();
-    int number = (int)rank_in_mask(m), total = 0;
-#pragma unroll
-    for (int w = 0; w < AD_TILE / WAVE; ++w) {
-        if (w < i >> 6) number += lds.opened[w];
-        total += lds.opened[w];
-    }
-    if (opens) {
-        lds.number[i] = number;
-        lds.id[number] = id;
-    }
-    __syncthreads();
-    mine.item = i < rows ? lds.number[opener] : -1;
-    mine.place = before % ROWS;
-    return total;
+    return t;
 }
-// The rows of an item into lds.rows; a barrier before and behind.  Returns how many there are.
-template <int ROWS>
-__device__ __forceinline__ void rows_of(int item, const Items &mine, ItemsLds &lds)
+// The rows left that have the adapter of row i, one of them.
+__device__ __forceinline__ Item same_as(const Tile &t, int i)
 {
-    __syncthreads();
-    if (threadIdx.x < ROWS) lds.rows[threadIdx.x] = -1;
-    __syncthreads();
-    if (mine.item == item) lds.rows[mine.place] = (int16_t)threadIdx.x;
-    __syncthreads();
+    Item it = {0, {}, 0};
+#pragma unroll
+    for (int w = 0; w < Tile::W; ++w)
+        if (w == i / WAVE) it.id = (int)lane_value((unsigned)t.id[w], i % WAVE);
+#pragma unroll
+    for (int w = 0; w < Tile::W; ++w) {
+        it.rows[w] = __ballot(t.id[w] == it.id) & t.left[w];
+        it.count += __popcll(it.rows[w]);
+    }
+    return it;
+}
+// The first ROWS rows of an item, into the wavefront's list in LDS (-1 behind); the item keeps these only.
+template <int ROWS>
+__device__ __forceinline__ void list_rows(Item &it, int16_t *list)
+{
+    if (lane_id() < ROWS) list[lane_id()] = -1;
+    __builtin_amdgcn_wave_barrier();
+    int before = 0;
+#pragma unroll
+    for (int w = 0; w < Tile::W; ++w) {
+        const int place = before + (int)rank_in_mask(it.rows[w]);
+        const bool in = (it.rows[w] >> lane_id() & 1) && place < ROWS;
+        if (in) list[place] = (int16_t)(w * WAVE + lane_id());
+        before += __popcll(it.rows[w]);
+        it.rows[w] = __ballot(in);
+    }
+    it.count = min(it.count, ROWS);
+    __builtin_amdgcn_wave_barrier();
+}
+// f(item) for the workgroup's items.  As many slots as rows: a workgroup has an item where its row is the first, or the one behind ROWS
+// others, ... of its adapter.  Fewer: it counts the items up, and takes every slots-th.
+template <int ROWS, typename F>
+__device__ __forceinline__ void each_item(Tile t, int slot, int slots, int rows, int16_t *list, F f)
+{
+    if (slots >= rows) {
+        if (slot >= rows) return;
+        Item it = same_as(t, slot);
+        int before = 0;
+#pragma unroll
+        for (int w = 0; w < Tile::W; ++w) {
+            const unsigned long long below = w < slot / WAVE ? ~0ull : w > slot / WAVE ? 0ull : (1ull << slot % WAVE) - 1;
+            before += __popcll(it.rows[w] & below);
+            it.rows[w] &= ~below;
+        }
+        if (before % ROWS) return;
+        it.count -= before;
+        list_rows<ROWS>(it, list);
+        f(it);
+        return;
+    }
+    for (int n = 0;; ++n) {
+        int i = AD_TILE;
+#pragma unroll
+        for (int w = Tile::W - 1; w >= 0; --w)
+            if (t.left[w]) i = w * WAVE + __ffsll((long long)t.left[w]) - 1;
+        if (i == AD_TILE) return;
+        Item it = same_as(t, i);
+        const bool own = n % slots == slot;
+        if (own || it.count > ROWS) list_rows<ROWS>(it, list);
+#pragma unroll
+        for (int w = 0; w < Tile::W; ++w) t.left[w] &= ~it.rows[w];
+        if (own) f(it);
+    }
 }
 
 struct Pool {
@@ -140,24 +171,25 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
                                                               float *__restrict__ part)
 {
     typedef Eight<T> E;
-    __shared__ ItemsLds lds;
+    __shared__ int16_t lists[AD_WG / WAVE][16 * RB];
     __shared__ f32x4 red[AD_WG / WAVE][RT][WAVE];
     const int split = blockIdx.x % splits, slot = blockIdx.x / splits % slots;
     const int64_t first = (int64_t)(blockIdx.x / splits / slots) * AD_TILE;
     const int wave = threadIdx.x >> 6, l = lane_id() % 16, g = lane_id() / 16;
-    Items mine;
-    const int items = group_rows<16 * RB>(ids, first, (int)min((int64_t)AD_TILE, M - first), pool.count, mine, lds);
+    const int rows = (int)min((int64_t)AD_TILE, M - first);
+    int16_t *list = lists[wave];
     const int steps = (pool.K + 31) / 32, s0 = min(steps, (split * 4 + wave) * per), s1 = min(steps, s0 + per);
-    for (int item = slot; item < items; item += slots) {
-        const int id = lds.id[item];
-        if (id < 0) continue;
-        rows_of<16 * RB>(item, mine, lds);
+    const int whole = min(s1, pool.K / 32);  // steps whose inputs are all there
+    constexpr int DEEP = RB * RT >= 16 ? 2 : 4;
+    each_item<16 * RB>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+        const int id = it.id;
+        if (id < 0) return;
         const int r = rank_of(pool, id);
         const T *xr[RB];
         int row[RB];
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
-            row[b] = lds.rows[b * 16 + l];
+            row[b] = list[b * 16 + l];
             xr[b] = x + (first + max(row[b], 0)) * ldx;
         }
         for (int p = 0; p < r; p += 16 * RT) {
@@ -165,17 +197,39 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
             const T *ar[RT];
 #pragma unroll
             for (int t = 0; t < RT; ++t) ar[t] = (const T *)pool.a + ((int64_t)id * pool.rank + min(p + 16 * t + l, r - 1)) * pool.K;
-            for (int s = s0; s < s1; ++s) {
-                const int k = 32 * s + 8 * g, n = pool.K - k;
-                typename E::V av[RT], xv[RB];
+            // (rows and ranks that are not there stand for others: their results are not looked at)
+            typename E::V av[DEEP][RT], xv[DEEP][RB];
+            const auto load = [&](int s, int u) {
+                const int k = 32 * s + 8 * g;
 #pragma unroll
-                for (int t = 0; t < RT; ++t) av[t] = p + 16 * t + l < r ? E::load(ar[t] + k, n) : E::zero();
+                for (int t = 0; t < RT; ++t) av[u][t] = E::load(ar[t] + k);
 #pragma unroll
-                for (int b = 0; b < RB; ++b) xv[b] = row[b] >= 0 ? E::load(xr[b] + k, n) : E::zero();
+                for (int b = 0; b < RB; ++b) xv[u][b] = E::load(xr[b] + k);
+            };
+            const auto multiply = [&](int u) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) acc[t][b] = mma(av[t], xv[b], acc[t][b]);
+                    for (int b = 0; b < RB; ++b) acc[t][b] = mma(av[u][t], xv[u][b], acc[t][b]);
+            };
+            int s = s0;
+            for (; s + DEEP <= whole; s += DEEP) {
+#pragma unroll
+                for (int u = 0; u < DEEP; ++u) load(s + u, u);
+#pragma unroll
+                for (int u = 0; u < DEEP; ++u) multiply(u);
+            }
+            for (; s < whole; ++s) {
+                load(s, 0);
+                multiply(0);
+            }
+            if (s < s1) {  // the last inputs
+                const int k = 32 * s + 8 * g, n = pool.K - k;
+#pragma unroll
+                for (int t = 0; t < RT; ++t) av[0][t] = E::load(ar[t] + k, n);
+#pragma unroll
+                for (int b = 0; b < RB; ++b) xv[0][b] = E::load(xr[b] + k, n);
+                multiply(0);
             }
 #pragma unroll
             for (int b = 0; b < RB; ++b) {
@@ -193,7 +247,7 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
                 }
             }
         }
-    }
+    });
 }
 
 // A power of two that takes `most` to 2^10 .. 2^11, and its inverse.
@@ -204,47 +258,112 @@ __device__ __forceinline__ float into_half(float most, float &back)
     return __uint_as_float((unsigned)(127 - e) << 23);
 }
 
-// y of the rows of an item, `blocks` times 64 outputs a wavefront.
-template <typename T, int RB>
-__global__ __launch_bounds__(AD_WG) void adapters_up_kernel(Pool pool, const int32_t *__restrict__ ids, int64_t M, int slots, int chunks,
-                                                            int blocks, int splits, int wide, const float *__restrict__ part,
-                                                            const T *base, int64_t ldb, T *y, int64_t ldy)
+// A result of 16 rows x 64 outputs goes through LDS to where eight lanes have a row's outputs side by side: loads and stores of 16 bytes from
+// 16 rows at once, four lanes of each, reached 2 TB/s.
+constexpr int AD_TURN = 68;  // floats from row to row
+
+// Ranks go in eights.  Of a pool whose rank is no multiple of eight the last eight begin at rank - 8, and those of them that the eight
+// before have too are zero in u.
+__device__ __forceinline__ int eight_at(int rank, int j) { return min(j, max(rank - 8, 0)); }
+
+// y of the rows of an item, `blocks` times 64 outputs a wavefront; STEPS times 32 ranks at most.  The last block of outputs begins 64
+// before the end, and writes what no other has.  SMALL: fewer than eight ranks or 64 outputs, read and written one by one.  What the
+// first outputs need of the pool and of base is on its way while u is added up.
+template <typename T, int RB, int STEPS, bool SMALL>
+__global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 : 2) void adapters_up_kernel(Pool pool, const int32_t *__restrict__ ids, int64_t M, int slots, int chunks,
+                                                               int blocks, int splits, int wide, const float *__restrict__ part,
+                                                               const T *base, int64_t ldb, T *y, int64_t ldy)
 {
     typedef Eight<T> E;
-    constexpr int ROWS = 16 * RB, SHARE = AD_WG / ROWS, QUADS = QADC_MAX_RANK / 4 / SHARE;
+    typedef typename E::V V;
+    constexpr int ROWS = 16 * RB, SHARE = AD_WG / ROWS, QUADS = (8 * STEPS + SHARE - 1) / SHARE;
     constexpr bool TWO = sizeof(T) == 2;
-    __shared__ ItemsLds lds;
+    constexpr bool KEPT = sizeof(T) * STEPS <= 8;  // the weights of 64 outputs stay in registers for all rows
+    __shared__ int16_t lists[AD_WG / WAVE][ROWS];
     __shared__ float back[ROWS];
+    __shared__ f32x4 turn[AD_WG / WAVE][16 * AD_TURN / 4];
     extern __shared__ __attribute__((aligned(16))) char raw[];
-    const int pad = (pool.rank + 31) / 32 * 32, stride = pad + 16 / (int)sizeof(T);
+    constexpr int stride = 32 * STEPS + 16 / (int)sizeof(T);
     T *hi = (T *)raw, *lo = hi + ROWS * stride;
     const int chunk = blockIdx.x % chunks, slot = blockIdx.x / chunks % slots;
     const int64_t first = (int64_t)(blockIdx.x / chunks / slots) * AD_TILE;
     const int wave = threadIdx.x >> 6, l = lane_id() % 16, g = lane_id() / 16;
-    Items mine;
-    const int items = group_rows<ROWS>(ids, first, (int)min((int64_t)AD_TILE, M - first), pool.count, mine, lds);
-    for (int item = slot; item < items; item += slots) {
-        const int id = lds.id[item];
-        if (id < 0 && base == y) continue;
-        rows_of<ROWS>(item, mine, lds);
+    const int rows = (int)min((int64_t)AD_TILE, M - first);
+    int16_t *list = lists[wave];
+    each_item<ROWS>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+        const int id = it.id;
+        if (id < 0 && base == y) return;
         const int r = id < 0 ? 0 : rank_of(pool, id), steps = (r + 31) / 32;
+        const T *b0 = (const T *)pool.b + (int64_t)max(id, 0) * pool.N * pool.rank;
+        const auto block_at = [&](int c) { return ((int64_t)(chunk * blocks + c) * (AD_WG / WAVE) + wave) * AD_COLS; };
+        const auto weights = [&](int64_t n0, int s, int t) {
+            const T *from = b0 + (n0 + 16 * t + l) * pool.rank;
+            const int j = eight_at(pool.rank, 32 * s + 8 * g);
+            V v;
+            if constexpr (!SMALL) {
+                v = E::load(from + j);
+            } else {
+                from = b0 + min(n0 + 16 * t + l, pool.N - 1) * pool.rank;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = from[min(j + e, pool.rank - 1)];
+            }
+            return v;
+        };
+        const auto cleared = [&](V v, int s) {  // (what lies beyond the rank may be anything)
+            const int j = eight_at(pool.rank, 32 * s + 8 * g), there = 32 * s + 8 * g < r ? r - j : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < there ? v[e] : (T)0.0f;
+            return v;
+        };
+        const auto old_at = [&](int row, int64_t n) {
+            V v = E::zero();
+            if (base) {
+                const T *from = base + (first + max(row, 0)) * ldb;
+                if constexpr (!SMALL) {
+                    v = E::load(from + n);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = from[min(n + e, pool.N - 1)];
+                }
+            }
+            return v;
+        };
+        V w[KEPT ? STEPS : 1][4], old[RB][2];
+        const auto fetch = [&](int64_t n0) {
+            if constexpr (!SMALL) n0 = min(n0, pool.N - AD_COLS);
+            if constexpr (KEPT) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) w[s][t] = weights(n0, s, t);
+            }
+#pragma unroll
+            for (int b = 0; b < RB; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) old[b][h] = old_at(list[b * 16 + 8 * h + lane_id() / 8], n0 + lane_id() % 8 * 8);
+        };
+        if (block_at(0) < pool.N) fetch(block_at(0));
+        __syncthreads();  // (the item before has been read)
         // u of the rows, SHARE threads a row
         {
-            const int i = threadIdx.x / SHARE, row = lds.rows[i];
+            const int i = threadIdx.x / SHARE, own = list[i];
             const float scale = id >= 0 && pool.scales ? pool.scales[id] : 1.0f;
             f32x4 u[QUADS];
             float most = 0.0f;
 #pragma unroll
             for (int q = 0; q < QUADS; ++q) {
-                const int j = 4 * (q * SHARE + (int)threadIdx.x % SHARE);
+                // places at .. at + 3 of the row hold the ranks j .. j + 3, of which the first may belong to the eight before
+                const int at = 4 * (q * SHARE + (int)threadIdx.x % SHARE), j = eight_at(pool.rank, at / 8 * 8) + at % 8;
                 u[q] = (f32x4)0.0f;
-                if (j >= 32 * steps) continue;
-                if (row >= 0 && j < r)
-                    for (int s = 0; s < splits; ++s)
-                        u[q] += *reinterpret_cast<const f32x4 *>(part + ((int64_t)s * M + first + row) * wide + j);
+                if (at >= 32 * steps) continue;
+                if (own >= 0 && j < r) {
+                    const float *from = part + (first + own) * wide + j;
+#pragma unroll 4
+                    for (int s = 0; s < splits; ++s) u[q] += *reinterpret_cast<const Quad *>(from + (int64_t)s * M * wide);
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    u[q][e] = j + e < r ? u[q][e] * scale : 0.0f;
+                    u[q][e] = j + e < r && j + e >= at / 8 * 8 ? u[q][e] * scale : 0.0f;
                     most = fmaxf(most, fabsf(u[q][e]));
                 }
             }
@@ -270,68 +389,67 @@ __global__ __launch_bounds__(AD_WG) void adapters_up_kernel(Pool pool, const int
             }
         }
         __syncthreads();
-        int row[RB];
-        float times[RB];
-#pragma unroll
-        for (int b = 0; b < RB; ++b) {
-            row[b] = lds.rows[b * 16 + l];
-            times[b] = std::is_same<T, _Float16>::value ? back[b * 16 + l] : 1.0f;
-        }
         for (int c = 0; c < blocks; ++c) {
-            // outputs n0 + 16 g + 4 t + e of this lane; the weights' rows go in so that the lane's sixteen lie side by side
-            const int64_t n0 = ((int64_t)(chunk * blocks + c) * (AD_WG / WAVE) + wave) * AD_COLS;
-            if (n0 >= pool.N) break;
-            const int64_t n = n0 + 16 * g;
-            const int there = (int)min((int64_t)16, pool.N - n);
-            typename E::V old[RB][2];
+            const int64_t from = block_at(c), n0 = SMALL ? from : min(from, pool.N - AD_COLS), n = n0 + lane_id() % 8 * 8;
+            if (from >= pool.N) break;
+            if (c) fetch(from);
+            if constexpr (KEPT)
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
+                for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    old[b][h] = base && row[b] >= 0 ? E::load(base + (first + row[b]) * ldb + n + 8 * h, there - 8 * h) : E::zero();
-            f32x4 acc[4][RB] = {};
-            for (int s = 0; s < steps; ++s) {
-                const int j = 32 * s + 8 * g;
-                typename E::V w[4], uh[RB], ul[RB];
+                    for (int t = 0; t < 4; ++t) w[s][t] = cleared(w[s][t], s);
+            const auto rows16 = [&](auto block) {
+                constexpr int b = decltype(block)::value;
+                f32x4 acc[4] = {};
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int64_t of = n0 + 16 * (l / 4) + 4 * t + l % 4;
-                    w[t] = of < pool.N ? E::load((const T *)pool.b + ((int64_t)id * pool.N + of) * pool.rank + j, r - j) : E::zero();
-                }
+                for (int s = 0; s < STEPS; ++s)
+                    if (s < steps) {
+                        const int at = (b * 16 + l) * stride + 32 * s + 8 * g;
+                        const V uh = *reinterpret_cast<const typename E::Lds *>(hi + at);
+                        V ul;
+                        if constexpr (TWO) ul = *reinterpret_cast<const typename E::Lds *>(lo + at);
 #pragma unroll
-                for (int b = 0; b < RB; ++b) {
-                    uh[b] = *reinterpret_cast<const typename E::Lds *>(hi + (b * 16 + l) * stride + j);
-                    if constexpr (TWO) ul[b] = *reinterpret_cast<const typename E::Lds *>(lo + (b * 16 + l) * stride + j);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        acc[t][b] = mma(w[t], uh[b], acc[t][b]);
-                        if constexpr (TWO) acc[t][b] = mma(w[t], ul[b], acc[t][b]);
+                        for (int t = 0; t < 4; ++t) {
+                            V v;
+                            if constexpr (KEPT) v = w[s][t];
+                            else v = cleared(weights(n0, s, t), s);
+                            acc[t] = mma(v, uh, acc[t]);
+                            if constexpr (TWO) acc[t] = mma(v, ul, acc[t]);
+                        }
                     }
-            }
+                const float times = std::is_same<T, _Float16>::value ? back[b * 16 + l] : 1.0f;
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                if (row[b] < 0) continue;
-                T *to = y + (first + row[b]) * ldy + n;
+                for (int t = 0; t < 4; ++t) turn[wave][(l * AD_TURN + 16 * t) / 4 + g] = acc[t] * times;
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    typename E::V v;
+                    const int place = 8 * h + lane_id() / 8, row = list[b * 16 + place];
+                    const f32x4 *sum = &turn[wave][(place * AD_TURN + lane_id() % 8 * 8) / 4];
+                    const f32x4 low = sum[0], high = sum[1];
+                    if (row < 0) continue;
+                    V v = old[b][h];
+                    if (r)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] = r ? (T)fmaf(acc[2 * h + e / 4][b][e % 4], times[b], (float)old[b][h][e]) : old[b][h][e];
-                    if (there >= 8 * h + 8) {
-                        *reinterpret_cast<typename E::Raw *>(to + 8 * h) = v;
+                        for (int e = 0; e < 8; ++e) v[e] = (T)((e < 4 ? low[e % 4] : high[e % 4]) + (float)v[e]);
+                    T *to = y + (first + row) * ldy + n;
+                    if (!SMALL && n >= from) {
+                        *reinterpret_cast<typename E::Raw *>(to) = v;
                     } else {
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
-                            if (8 * h + e < there) to[8 * h + e] = v[e];
+                            if (n + e >= from && n + e < pool.N) to[e] = v[e];
                     }
                 }
+            };
+            rows16(std::integral_constant<int, 0>());
+            if constexpr (RB > 1) {
+                if (it.count > 16) rows16(std::integral_constant<int, 1>());
+                if (it.count > 32) rows16(std::integral_constant<int, 2>());
+                if (it.count > 48) rows16(std::integral_constant<int, 3>());
             }
         }
-    }
+    });
 }
 
 struct AdPlan {
@@ -343,22 +461,25 @@ struct AdPlan {
 AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
 {
     AdPlan p;
-    p.many = M >= 64 * (int64_t)count && M >= 256;
+    p.many = M >= 64 * (int64_t)count && M >= AD_MANY;
     const int each = p.many ? 64 : 16;
     p.tiles = (int)ceil_div(M, AD_TILE);
     const int rows = (int)std::min<int64_t>(M, AD_TILE);
-    const int bound = std::min(rows, std::min(count + 1, rows) + rows / each);  // items of a tile at most
-    p.slots = std::min(p.many ? std::min(bound, 8) : bound, std::max(1, 16384 / p.tiles));
+    const int bound = std::min(rows, count + 1) + rows / each;  // items of a tile at most
+    p.slots = p.many ? std::min(bound, 6) : bound <= std::min(20, rows / 2) ? bound : rows;
+    p.slots = std::min(p.slots, std::max(1, 65536 / p.tiles));
     p.wide = (rank + 15) / 16 * 16;
+    // items, where a batch's adapters are about as many as there may be
+    const int64_t items = (int64_t)p.tiles * (p.many ? rows / 64 : std::min(rows, std::min(count, rows) + rows / 16));
     const int steps = (K + 31) / 32;
-    const int64_t wgs = (int64_t)p.tiles * std::min(bound, std::max(1, rows / each) + (p.many ? 0 : std::min(count, rows)));
-    const int most = std::max(1, steps / 8);  // two steps a wavefront at least
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(most, 512 / std::max<int64_t>(1, wgs)));
+    const int least = std::max(1, steps / 8);  // two steps a wavefront at least
+    const int read = std::max(1, 65536 / (each * p.wide * 4));  // what every workgroup of the second product reads of the first
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(least, read), 768 / std::max<int64_t>(1, items)));
     p.per = (int)ceil_div(steps, 4 * want);
     p.splits = (int)ceil_div(steps, 4 * p.per);
     p.bytes = (size_t)p.splits * M * p.wide * sizeof(float);
     const int64_t cols = ceil_div(N, AD_COLS * (AD_WG / WAVE));
-    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, cols * wgs / 1024));
+    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, cols * items / 768));
     p.chunks = (int)ceil_div(cols, p.blocks);
     return p;
 }
@@ -375,9 +496,9 @@ static bool pool_ok(const qadc_adapters *w)
 size_t adapters_workspace(const qadc_adapters *w, int64_t M)
 {
     if (!pool_ok(w) || M < 1 || M > 1 << 24) return 0;
-    // (m rows are cut into at most 512 / (m / 256) splits, or what leaves each two steps)
+    // (m rows are cut into at most 768 / (m / 256) splits, or what leaves each two steps)
     const int64_t most = std::max(1, (w->K + 31) / 32 / 8);
-    return (size_t)std::min(most * M, std::max<int64_t>(M, 512 * AD_TILE)) * ((w->rank + 15) / 16 * 16) * sizeof(float);
+    return (size_t)std::min(most * M, std::max<int64_t>(M, 768 * AD_TILE)) * ((w->rank + 15) / 16 * 16) * sizeof(float);
 }
 
 template <typename T, int RB>
@@ -391,9 +512,18 @@ static void launch_adapters(const AdPlan &p, const Pool &pool, const int32_t *id
     else
         launch(QADC_PROF_ADAPTERS, adapters_down_kernel<T, 4, RB>, down, dim3(AD_WG), 0, st, pool, ids, (const T *)x, ldx, M, p.slots,
                p.splits, p.per, p.wide, part);
-    const size_t pad = (pool.rank + 31) / 32 * 32, lds = 16 * RB * (pad + 16 / sizeof(T)) * sizeof(T) * (sizeof(T) == 2 ? 2 : 1);
-    launch(QADC_PROF_ADAPTERS, adapters_up_kernel<T, RB>, dim3((unsigned)(p.tiles * p.slots * p.chunks)), dim3(AD_WG), lds, st, pool, ids, M,
-           p.slots, p.chunks, p.blocks, p.splits, p.wide, (const float *)part, (const T *)base, ldb, (T *)y, ldy);
+    const auto up = [&](auto steps, auto small) {
+        constexpr int S = decltype(steps)::value;
+        const size_t lds = 16 * RB * (32 * S + 16 / sizeof(T)) * sizeof(T) * (sizeof(T) == 2 ? 2 : 1);
+        launch(QADC_PROF_ADAPTERS, adapters_up_kernel<T, RB, S, decltype(small)::value>, dim3((unsigned)(p.tiles * p.slots * p.chunks)),
+               dim3(AD_WG), lds, st, pool, ids, M, p.slots, p.chunks, p.blocks, p.splits, p.wide, (const float *)part, (const T *)base, ldb,
+               (T *)y, ldy);
+    };
+    if (pool.N < AD_COLS) up(std::integral_constant<int, 4>(), std::true_type());
+    else if (pool.rank < 8) up(std::integral_constant<int, 1>(), std::true_type());
+    else if (pool.rank <= 32) up(std::integral_constant<int, 1>(), std::false_type());
+    else if (pool.rank <= 64) up(std::integral_constant<int, 2>(), std::false_type());
+    else up(std::integral_constant<int, 4>(), std::false_type());
 }
 
 int add_adapters(const qadc_adapters *w, const int32_t *ids, const void *x, int64_t ldx, int64_t M, const void *base, int64_t ldb, void *y,
