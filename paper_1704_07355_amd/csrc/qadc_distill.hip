@@ -84,10 +84,31 @@ __device__ __forceinline__ double wave_sum64(double v)
     return v;
 }
 
+// The share of this thread's stored token in the row's loss; m: the row's largest logit, log_s: the logarithm of its sum.
+__device__ __forceinline__ double loss_of(const Stored &st, double p, double P, bool tail, bool none, float scale, float m, double log_s)
+{
+    if (!(p > 0.0) && p == p) return 0.0;
+    const double log_q = none ? -INFINITY : (double)scale * ((double)st.logit - (double)m) - log_s;
+    return tail ? p * ((double)st.logp - log_q) : p / P * ((double)st.logp - log(P) - log_q);
+}
+
+// Whether no thread before this one has its token.
+__device__ __forceinline__ bool first_of(const int *tokens, int token, int k)
+{
+    bool first = true;
+    for (int i = 0; i < k; i += 4) {
+        const int4 v = *reinterpret_cast<const int4 *>(&tokens[i]);
+        const int before = (int)threadIdx.x - i;
+        first = first && !((v.x == token && before > 0) || (v.y == token && before > 1) || (v.z == token && before > 2) ||
+                           (v.w == token && before > 3));
+    }
+    return first;
+}
+
 struct FinishLds {
     double mass[DS_WAVES], loss[DS_WAVES];
     float most[DS_WAVES], own[DS_WAVES];
-    int tokens[QADC_MAX_ALTERNATIVES];
+    __attribute__((aligned(16))) int tokens[QADC_MAX_ALTERNATIVES];
     float total, share, log_tail;
 };
 
@@ -140,7 +161,7 @@ __device__ __forceinline__ void finish_row(Part2 others, const Stored &st, int64
     const bool none = m == -INFINITY;
     if (wave < DS_WAVES) {
         bool first = st.token >= 0;  // a token that is stored twice counts once for the student
-        for (int i = 0; i < (int)threadIdx.x && i < t.k; ++i) first = first && lds.tokens[i] != st.token;
+        first = first && first_of(lds.tokens, st.token, t.k);
         const float own = wave_sum(first && !none ? exp2_fast(c * (st.logit - m)) : 0.0f);
         if (lane_id() == 0) lds.own[wave] = own;
     }
@@ -153,12 +174,7 @@ __device__ __forceinline__ void finish_row(Part2 others, const Stored &st, int64
     sum = own + rest;
     if (wave < DS_WAVES) {
         const double log_s = log((double)own + (double)rest);
-        double l = 0.0;
-        if (p > 0.0 || p != p) {
-            const double log_q = none ? -INFINITY : (double)scale * ((double)st.logit - (double)m) - log_s;
-            l = t.tail ? p * ((double)st.logp - log_q) : p / mass.P * ((double)st.logp - log(mass.P) - log_q);
-        }
-        l = wave_sum64(l);
+        const double l = wave_sum64(loss_of(st, p, mass.P, t.tail, none, scale, m, log_s));
         if (lane_id() == 0) lds.loss[wave] = l;
         if (threadIdx.x == 0) {
             const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
@@ -298,7 +314,7 @@ __global__ __launch_bounds__(LP_WG) void distill_join_kernel(const T *__restrict
 
 // The stored tokens' gradients, each token once: value(logit) is what a stored token has from the student, own the teacher's share.
 struct GradLds {
-    int tokens[QADC_MAX_ALTERNATIVES];
+    __attribute__((aligned(16))) int tokens[QADC_MAX_ALTERNATIVES];
     float p[QADC_MAX_ALTERNATIVES];
 };
 template <typename T, typename F>
@@ -393,97 +409,142 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
     }
 }
 
-// Loss and gradient of a row whose logits stay in the registers of its workgroup: PACKS packs a thread, read and written once.
+struct StepLds {
+    double mass[DS_WAVES], loss[DS_WAVES];
+    float most[16], others[16], own[DS_WAVES];
+    GradLds grad;
+};
+
+// Loss and gradient of a row whose logits stay in the registers of its workgroup: PACKS packs a thread, read and written once, and the
+// up to seven logits at either end that fill no pack of 16 bytes one a thread.  What the gradient needs (the largest logit, the two
+// sums, the teacher's mass) comes first, the loss after the stores.  128 registers: half of them hold the row.
 template <typename T, int THREADS, int PACKS>
-__global__ __launch_bounds__(THREADS) void distill_step_kernel(const T *logits, int64_t ld, int V, float scale, Teacher t,
-                                                               const float *__restrict__ weight, Loss o, T *dlogits, int64_t ldd)
+__global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logits, int64_t ld, int V, float scale, Teacher t,
+                                                                  const float *__restrict__ weight, float *__restrict__ loss, T *dlogits,
+                                                                  int64_t ldd)
 {
     constexpr int N = Pack<T>::N, W = THREADS / WAVE;
     typedef typename Pack<T>::V P;
-    __shared__ uint32_t marks[THREADS * PACKS * N / 32];
-    __shared__ float waves[2][W];
-    __shared__ FinishLds lds;
-    __shared__ GradLds grad;
+    __shared__ uint32_t marks[THREADS * PACKS * N / 32 + 1];  // (and the pack before the first whole one)
+    __shared__ StepLds lds;
     const int64_t r = blockIdx.x;
     const T *row = logits + r * ld;
     T *out = dlogits + r * ldd;
-    const int lead = lead_of(row);
+    const int lead = lead_of(row), wave = threadIdx.x >> 6, tid = threadIdx.x;
     const float c = scale * LOG2E;
+    const Stored st = stored_of(row, r, V, t);
+    // whole packs begin .. end - 1 from the 16 bytes that hold the row's first logit on; this thread's at begin + u THREADS + tid
+    const int begin = lead ? 1 : 0, end = (V + lead) / N, here = end - begin - tid;  // (u THREADS < here: there is one)
+    const int head = lead ? min(N - lead, V) : 0, tail = max(end * N - lead, head);
+    const int edge = tid < head ? tid : tail + tid - head;  // < V: this thread's logit at an end
+    const T *from = row + (begin + tid) * N - lead;
+    T *to = out + (begin + tid) * N - lead;
     P x[PACKS];
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
-        const int at = (u * THREADS + (int)threadIdx.x) * N - lead;
-        x[u] = load_edge(row, at, V, -INFINITY);
+        x[u] = (T)-INFINITY;
+        if (u * THREADS < here) x[u] = __builtin_nontemporal_load(reinterpret_cast<const P *>(from + u * THREADS * N));
     }
-    Stored st = stored_of(row, r, V, t);
-    for (int i = threadIdx.x; i < THREADS * PACKS * N / 32; i += THREADS) marks[i] = 0;
+    const float at_edge = edge < V ? (float)row[edge] : -INFINITY;
+    // the teacher, while the row comes in
+    for (int i = threadIdx.x; i < THREADS * PACKS * N / 32 + 1; i += THREADS) marks[i] = 0;
+    double p = 0.0;
+    if (wave < DS_WAVES) {
+        p = st.token < 0 ? 0.0 : exp((double)st.logp);
+        const double mass = wave_sum64(p);
+        if (lane_id() == 0) lds.mass[wave] = mass;
+        lds.grad.tokens[threadIdx.x] = st.token;
+    }
     __syncthreads();
-    if (st.token >= 0) atomicOr(&marks[(st.token + lead) / 32], 1u << ((st.token + lead) % 32));
-    __syncthreads();
-    float m = -INFINITY;
+    Mass mass = {0.0, 0.0};
+#pragma unroll
+    for (int w = 0; w < DS_WAVES; ++w) mass.P += lds.mass[w];
+    mass.rest = t.tail && mass.P < 1.0 ? 1.0 - mass.P : 0.0;
+    bool first = st.token >= 0;  // a token that is stored twice counts once for the student
+    if (wave < DS_WAVES) {
+        if (st.token >= 0) atomicOr(&marks[(st.token + lead) / 32], 1u << ((st.token + lead) % 32));
+        first = first && first_of(lds.grad.tokens, st.token, t.k);
+        lds.grad.p[threadIdx.x] = (float)(t.tail ? p : mass.P > 0.0 ? p / mass.P : 0.0);
+    }
+    float m = at_edge;
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
-        const unsigned b = marks_at<N>(marks, (u * THREADS + (int)threadIdx.x) * N);
-        if (b)
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (b >> e & 1) x[u][e] = (T)-INFINITY;
 #pragma unroll
         for (int e = 0; e < N; ++e) m = fmaxf(m, (float)x[u][e]);
+        asm volatile("" : "+v"(m));  // (pack after pack: otherwise all are held as float32 at once, beyond 128 registers)
     }
     m = wave_max(m);
-    if (lane_id() == 0) waves[0][threadIdx.x >> 6] = m;
+    if (lane_id() == 0) lds.most[wave] = m;
     __syncthreads();
-    m = waves[0][0];
+    m = lds.most[0];
 #pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, waves[0][w]);
-    const float m0 = m == -INFINITY ? 0.0f : m;
-    float s = 0.0f;
+    for (int w = 1; w < W; ++w) m = fmaxf(m, lds.most[w]);
+    const bool none = m == -INFINITY;
+    const float m0 = none ? 0.0f : m;
+    float s = edge < V && !(marks[(edge + lead) / 32] >> ((edge + lead) % 32) & 1) ? exp2_fast(c * (at_edge - m0)) : 0.0f;
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
-        float part = 0.0f;
+        asm volatile("" : "+v"(x[u]));  // (converted again rather than kept)
+        const unsigned b = u * THREADS < here ? marks_at<N>(marks, (begin + u * THREADS + tid) * N) : 0u;
+        float e[N], part = 0.0f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) part += exp2_fast(c * ((float)x[u][e] - m0));
+        for (int i = 0; i < N; ++i) e[i] = exp2_fast(c * ((float)x[u][i] - m0));
+        if (b)
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = b >> i & 1 ? 0.0f : e[i];
+#pragma unroll
+        for (int i = 0; i < N; ++i) part += e[i];
         s += part;
+        asm volatile("" : "+v"(s));
     }
     s = wave_sum(s);
-    if (lane_id() == 0) waves[1][threadIdx.x >> 6] = s;
-    __syncthreads();
-    s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) s += waves[1][w];
-    float most, sum;
-    finish_row({m, s}, st, r, scale, t, o, lds, most, sum);
-    __syncthreads();
-    const float w = scale * weight[r];
-    const bool zero = w == 0.0f || most == -INFINITY;
-    if (threadIdx.x < QADC_MAX_ALTERNATIVES && (int)threadIdx.x < t.k) {
-        double P = 0.0;
-#pragma unroll
-        for (int i = 0; i < DS_WAVES; ++i) P += lds.mass[i];
-        const double p = st.token < 0 ? 0.0 : exp((double)st.logp);
-        grad.tokens[threadIdx.x] = st.token;
-        grad.p[threadIdx.x] = (float)(t.tail ? p : P > 0.0 ? p / P : 0.0);
+    if (lane_id() == 0) lds.others[wave] = s;
+    if (wave < DS_WAVES) {
+        const float own = wave_sum(first && !none ? exp2_fast(c * (st.logit - m)) : 0.0f);
+        if (lane_id() == 0) lds.own[wave] = own;
     }
-    const float f = w * lds.share / sum;
-    const auto q_of = [&](float logit) { return exp2_fast(c * (logit - most)); };
+    __syncthreads();
+    float others = 0.0f, own = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) others += lds.others[w];
+#pragma unroll
+    for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
+    const float sum = own + others;
+    // r / Q, left out where the student has nothing left
+    const bool rest = mass.rest > 0.0 && others != 0.0f;
+    const double whole = t.tail ? mass.P + (rest ? mass.rest : 0.0) : mass.P > 0.0 ? 1.0 : 0.0;
+    const float total = (float)whole;
+    const float share = rest ? (float)(whole - mass.rest * (1.0 + (double)own / (double)others)) : total;
+    const float w = scale * weight[r];
+    const bool zero = w == 0.0f || none;
+    const float f = zero ? 0.0f : w * share / sum;
+    const auto value = [&](float logit) { return zero ? 0.0f : f * exp2_fast(c * (logit - m0)); };
+    if (edge < V) out[edge] = (T)value(at_edge);
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
-        const int at = (u * THREADS + (int)threadIdx.x) * N - lead;
-        if (at >= V) continue;
+        asm volatile("" : "+v"(x[u]));
         P g;
 #pragma unroll
-        for (int e = 0; e < N; ++e) g[e] = (T)(zero ? 0.0f : f * q_of((float)x[u][e]));
-        if (at >= 0 && at + N <= V) {
-            __builtin_nontemporal_store(g, reinterpret_cast<P *>(out + at));
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (at + e >= 0 && at + e < V) out[at + e] = g[e];
-        }
+        for (int e = 0; e < N; ++e) g[e] = (T)value((float)x[u][e]);
+        if (u * THREADS < here) __builtin_nontemporal_store(g, reinterpret_cast<P *>(to + u * THREADS * N));
+        __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
-    if (!zero) write_stored(out, st, t.k, grad, [&](float logit, float own) { return w * fmaf(lds.total, q_of(logit) / sum, -own); });
+    if (wave < DS_WAVES) {
+        if (!zero)
+            write_stored(out, st, t.k, lds.grad,
+                         [&](float logit, float p) { return w * fmaf(total, exp2_fast(c * (logit - m)) / sum, -p); });
+        const double l = wave_sum64(loss_of(st, p, mass.P, t.tail, none, scale, m, log((double)own + (double)others)));
+        if (lane_id() == 0) lds.loss[wave] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double l = 0.0;
+#pragma unroll
+        for (int v = 0; v < DS_WAVES; ++v) l += lds.loss[v];
+        if (rest) l += mass.rest * (log(mass.rest) + log1p((double)own / (double)others));
+        loss[r] = (float)l;
+    }
 }
 
 int check_distill(const char *who, int type, int64_t ld, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k)
@@ -590,10 +651,10 @@ int distill_backward(const void *logits, int64_t ld, int type, int64_t rows, int
 
 template <typename T, int THREADS, int PACKS>
 static void launch_step(const void *logits, int64_t ld, int64_t rows, int V, float scale, const Teacher &t, const float *weight,
-                        const Loss &o, void *dlogits, int64_t ldd, hipStream_t st)
+                        float *loss, void *dlogits, int64_t ldd, hipStream_t st)
 {
     launch(QADC_PROF_DISTILL, distill_step_kernel<T, THREADS, PACKS>, dim3((unsigned)rows), dim3(THREADS), 0, st, (const T *)logits, ld, V,
-           scale, t, weight, o, (T *)dlogits, ldd);
+           scale, t, weight, loss, (T *)dlogits, ldd);
 }
 
 int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k,
@@ -614,16 +675,14 @@ int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, 
     const Teacher t = {idx, logp, k, tail != 0};
     float *lse = (float *)((char *)workspace + stats), *log_tail = (float *)((char *)workspace + stats + each);
     const size_t e = type_bytes(type);
-    const bool even = (uintptr_t)logits % 16 == 0 && (size_t)ld * e % 16 == 0;
-    const size_t bytes = ((size_t)V + (even ? 0 : 16 / e - 1)) * e;
+    const size_t bytes = (size_t)V * e;
     if (rows >= 128 && rows < 1 << 30 && bytes <= 262144) {
         QADC_BY_TYPE(type, {
-            const Loss o = {loss, nullptr, nullptr};
-            if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
-            else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
-            else if (bytes <= 65536) launch_step<T, 256, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
-            else if (bytes <= 131072) launch_step<T, 512, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
-            else launch_step<T, 1024, 16>(logits, ld, rows, V, scale, t, weight, o, dlogits, ldd, st);
+            if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
+            else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
+            else if (bytes <= 65536) launch_step<T, 256, 16>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
+            else if (bytes <= 131072) launch_step<T, 512, 16>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
+            else launch_step<T, 1024, 16>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
         });
     } else {
         QADC_BY_TYPE(type, {
