@@ -57,21 +57,22 @@ __device__ __forceinline__ void add_block(Part2 &a, const float (&x)[LP_BLOCK], 
     a.s += s[0] + s[1];
 }
 
-// The stored token of this thread, as it is in the row.
+// A stored token as it is in the row.
 struct Stored {
     int token;   // -1: none
     float logit, logp;
 };
 template <typename T>
-__device__ __forceinline__ Stored stored_of(const T *row, int64_t r, int V, const Teacher &t)
+__device__ __forceinline__ Stored stored_of(const T *row, int64_t r, int V, const Teacher &t, int at)
 {
     Stored s = {-1, -INFINITY, -INFINITY};
-    if ((int)threadIdx.x < t.k) {
-        const uint32_t i = t.idx[r * t.k + threadIdx.x];
+    if (at < t.k) {
+        const uint32_t i = t.idx[r * t.k + at];
+        const float logp = t.logp[r * t.k + at];
         if (i < (uint32_t)V) {
             s.token = (int)i;
             s.logit = (float)row[i];
-            s.logp = t.logp[r * t.k + threadIdx.x];
+            s.logp = logp;
         }
     }
     return s;
@@ -92,43 +93,24 @@ __device__ __forceinline__ double loss_of(const Stored &st, double p, double P, 
     return tail ? p * ((double)st.logp - log_q) : p / P * ((double)st.logp - log(P) - log_q);
 }
 
-// Whether no thread before this one has its token.
-__device__ __forceinline__ bool first_of(const int *tokens, int token, int k)
+// Whether none of the tokens before number `at` is `token`.
+__device__ __forceinline__ bool first_of(const int *tokens, int token, int k, int at)
 {
     bool first = true;
     for (int i = 0; i < k; i += 4) {
         const int4 v = *reinterpret_cast<const int4 *>(&tokens[i]);
-        const int before = (int)threadIdx.x - i;
+        const int before = at - i;
         first = first && !((v.x == token && before > 0) || (v.y == token && before > 1) || (v.z == token && before > 2) ||
                            (v.w == token && before > 3));
     }
     return first;
 }
 
-struct FinishLds {
-    double mass[DS_WAVES], loss[DS_WAVES];
-    float most[DS_WAVES], own[DS_WAVES];
-    __attribute__((aligned(16))) int tokens[QADC_MAX_ALTERNATIVES];
-    float total, share, log_tail;
-};
-
 // Of the teacher's probabilities p of a row: their sum, and with the tail what is left.
 struct Mass {
     double P, rest;
 };
-// What the thread's stored token has, and all of them: every thread comes here.
-__device__ __forceinline__ Mass mass_of(double p, bool tail, FinishLds &lds)
-{
-    if (threadIdx.x < QADC_MAX_ALTERNATIVES) {
-        p = wave_sum64(p);
-        if (lane_id() == 0) lds.mass[threadIdx.x >> 6] = p;
-    }
-    __syncthreads();
-    double P = 0.0;
-#pragma unroll
-    for (int w = 0; w < DS_WAVES; ++w) P += lds.mass[w];
-    return {P, tail && P < 1.0 ? 1.0 - P : 0.0};
-}
+__device__ __forceinline__ Mass mass_of(double P, bool tail) { return {P, tail && P < 1.0 ? 1.0 - P : 0.0}; }
 // The teacher's whole probability as the gradient takes it, and the factor of what was not stored, where log Q is `log_tail`.
 __device__ __forceinline__ void shares(const Mass &a, bool tail, double log_tail, float &total, float &share)
 {
@@ -142,69 +124,77 @@ struct Loss {
     float *loss, *lse, *log_tail;  // lse and log_tail nullable
 };
 
-// The row's loss from what its other tokens have, by all threads of the workgroup; total and share land in lds.
-// m: the row's largest logit of any token, and own its stored tokens' sum, come back.
-__device__ __forceinline__ void finish_row(Part2 others, const Stored &st, int64_t r, float scale, const Teacher &t, const Loss &o,
-                                           FinishLds &lds, float &m, float &sum)
+// The stored tokens of a wavefront's row, a few a lane.
+struct WaveStored {
+    Stored at[DS_WAVES];
+};
+template <typename T>
+__device__ __forceinline__ WaveStored wave_stored(const T *row, int64_t r, int V, const Teacher &t)
+{
+    WaveStored s;
+#pragma unroll
+    for (int i = 0; i < DS_WAVES; ++i) s.at[i] = stored_of(row, r, V, t, i * WAVE + lane_id());
+    return s;
+}
+
+// The row's loss from what its other tokens have, by one wavefront.  tokens: a place for the row's stored tokens.
+__device__ __forceinline__ void finish_row(Part2 others, const WaveStored &st, int64_t r, float scale, const Teacher &t, const Loss &o,
+                                           int *tokens)
 {
     const float c = scale * LOG2E;
-    const int wave = threadIdx.x >> 6;
-    if (wave < DS_WAVES) {
-        const float most = wave_max(st.logit);
-        if (lane_id() == 0) lds.most[wave] = most;
-        lds.tokens[threadIdx.x] = st.token;
-    }
-    __syncthreads();
-    m = others.m;
+    double p[DS_WAVES], P = 0.0;
+    float most = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < DS_WAVES; ++w) m = fmaxf(m, lds.most[w]);
-    const bool none = m == -INFINITY;
-    if (wave < DS_WAVES) {
-        bool first = st.token >= 0;  // a token that is stored twice counts once for the student
-        first = first && first_of(lds.tokens, st.token, t.k);
-        const float own = wave_sum(first && !none ? exp2_fast(c * (st.logit - m)) : 0.0f);
-        if (lane_id() == 0) lds.own[wave] = own;
+    for (int i = 0; i < DS_WAVES; ++i) {
+        tokens[i * WAVE + lane_id()] = st.at[i].token;
+        p[i] = st.at[i].token < 0 ? 0.0 : exp((double)st.at[i].logp);
+        P += p[i];
+        most = fmaxf(most, st.at[i].logit);
     }
-    const double p = st.token < 0 ? 0.0 : exp((double)st.logp);
-    const Mass mass = mass_of(p, t.tail, lds);  // (a barrier)
+    __builtin_amdgcn_wave_barrier();
+    const Mass mass = mass_of(wave_sum64(P), t.tail);
+    const float m = fmaxf(others.m, wave_max(most));
+    const bool none = m == -INFINITY;
     float own = 0.0f;
 #pragma unroll
-    for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
-    const float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
-    sum = own + rest;
-    if (wave < DS_WAVES) {
-        const double log_s = log((double)own + (double)rest);
-        const double l = wave_sum64(loss_of(st, p, mass.P, t.tail, none, scale, m, log_s));
-        if (lane_id() == 0) lds.loss[wave] = l;
-        if (threadIdx.x == 0) {
-            const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
-            if (o.lse) {
-                const float lse = (float)((double)scale * (double)m + log_s);  // (no float holds it: NaN)
-                o.lse[r] = none ? -INFINITY : fabsf(lse) < INFINITY ? lse : NAN;
-            }
-            if (o.log_tail) o.log_tail[r] = (float)log_tail;
-            shares(mass, t.tail, log_tail, lds.total, lds.share);
-            lds.log_tail = (float)log_tail;
-        }
+    for (int i = 0; i < DS_WAVES; ++i) {  // a token that is stored twice counts once for the student
+        const bool first = st.at[i].token >= 0 && first_of(tokens, st.at[i].token, t.k, i * WAVE + lane_id());
+        own += first && !none ? exp2_fast(c * (st.at[i].logit - m)) : 0.0f;
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        double l = 0.0;
+    own = wave_sum(own);
+    const float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
+    const double log_s = log((double)own + (double)rest);
+    const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
+    double l = 0.0;
 #pragma unroll
-        for (int w = 0; w < DS_WAVES; ++w) l += lds.loss[w];
-        if (mass.rest > 0.0 && lds.log_tail != -INFINITY) l += mass.rest * (log(mass.rest) - (double)lds.log_tail);
+    for (int i = 0; i < DS_WAVES; ++i) l += loss_of(st.at[i], p[i], mass.P, t.tail, none, scale, m, log_s);
+    l = wave_sum64(l);
+    if (lane_id() == 0) {
+        if (mass.rest > 0.0 && log_tail != -INFINITY) l += mass.rest * (log(mass.rest) - log_tail);
         o.loss[r] = (float)l;
+        if (o.lse) {
+            const float lse = (float)((double)scale * (double)m + log_s);  // (no float holds it: NaN)
+            o.lse[r] = none ? -INFINITY : fabsf(lse) < INFINITY ? lse : NAN;
+        }
+        if (o.log_tail) o.log_tail[r] = (float)log_tail;
     }
 }
 
+// The stored token of this thread, -1: none.
+__device__ __forceinline__ int token_of(int64_t r, int V, const Teacher &t)
+{
+    const uint32_t v = (int)threadIdx.x < t.k ? t.idx[r * t.k + threadIdx.x] : ~0u;
+    return v < (uint32_t)V ? (int)v : -1;
+}
+
 // Marks the stored token if it lies in chunks j0 .. j1 - 1 of the row, whose first token is at `lead`; a barrier before and behind.
-__device__ __forceinline__ void mark(uint32_t *marks, const Stored &st, int64_t j0, int64_t j1, int lead, int threads)
+__device__ __forceinline__ void mark(uint32_t *marks, int token, int64_t j0, int64_t j1, int lead, int threads)
 {
     __syncthreads();
     for (int64_t w = threadIdx.x; w < (j1 - j0) * (LP_CHUNK / 32); w += threads) marks[w] = 0;
     __syncthreads();
-    const int64_t at = (int64_t)st.token + lead - j0 * LP_CHUNK;
-    if (st.token >= 0 && at >= 0 && at < (j1 - j0) * LP_CHUNK) atomicOr(&marks[at / 32], 1u << (at % 32));
+    const int64_t at = (int64_t)token + lead - j0 * LP_CHUNK;
+    if (token >= 0 && at >= 0 && at < (j1 - j0) * LP_CHUNK) atomicOr(&marks[at / 32], 1u << (at % 32));
     __syncthreads();
 }
 // The marks of the N tokens from position `at` on, a multiple of N.
@@ -217,16 +207,16 @@ __device__ __forceinline__ unsigned marks_at(const uint32_t *marks, int at)
 
 // What chunks j0 .. j1 - 1 of a row have, joined over the workgroup.
 template <typename T>
-__device__ __forceinline__ Part2 chunks_part(const T *row, int64_t j0, int64_t j1, int V, int lead, float c, const Stored &st,
+__device__ __forceinline__ Part2 chunks_part(const T *row, int64_t j0, int64_t j1, int V, int lead, float c, int token,
                                              uint32_t *marks, Part2 *waves)
 {
     constexpr int N = Pack<T>::N;
     Part2 a = {-INFINITY, 0.0f};
     for (int64_t j = j0; j < j1; ++j) {
         const int at = (int)((j - j0) % DS_MARKED);
-        if (at == 0) mark(marks, st, j, min(j + DS_MARKED, j1), lead, LP_WG);
         float x[LP_BLOCK];
         load_block(row, j, V, lead, x);
+        if (at == 0) mark(marks, token, j, min(j + DS_MARKED, j1), lead, LP_WG);
 #pragma unroll
         for (int u = 0; u < LP_BLOCK / N; ++u) {
             const unsigned b = marks_at<N>(marks, at * LP_CHUNK + (u * LP_WG + (int)threadIdx.x) * N);
@@ -256,14 +246,13 @@ __global__ __launch_bounds__(LP_WG) void distill_row_kernel(const T *__restrict_
 {
     __shared__ uint32_t marks[DS_MARKED * LP_CHUNK / 32];
     __shared__ Part2 waves[LP_WG / WAVE];
-    __shared__ FinishLds lds;
+    __shared__ __attribute__((aligned(16))) int tokens[QADC_MAX_ALTERNATIVES];
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *row = logits + r * ld;
         const int lead = lead_of(row);
-        const Stored st = stored_of(row, r, V, t);
-        const Part2 a = chunks_part(row, 0, chunks_of(V, lead), V, lead, scale * LOG2E, st, marks, waves);
-        float m, sum;
-        finish_row(a, st, r, scale, t, o, lds, m, sum);
+        const int token = token_of(r, V, t);
+        const Part2 a = chunks_part(row, 0, chunks_of(V, lead), V, lead, scale * LOG2E, token, marks, waves);
+        if (threadIdx.x < WAVE) finish_row(a, wave_stored(row, r, V, t), r, scale, t, o, tokens);
     }
 }
 
@@ -278,37 +267,27 @@ __global__ __launch_bounds__(LP_WG) void distill_part_kernel(const T *__restrict
         const int64_t r = i / parts, j0 = i % parts * per;
         const T *row = logits + r * ld;
         const int lead = lead_of(row);
-        Stored st = {-1, 0.0f, 0.0f};
-        if ((int)threadIdx.x < t.k) {
-            const uint32_t v = t.idx[r * t.k + threadIdx.x];
-            if (v < (uint32_t)V) st.token = (int)v;
-        }
-        const Part2 a = chunks_part(row, j0, min(j0 + per, chunks_of(V, lead)), V, lead, scale * LOG2E, st, marks, waves);
+        const Part2 a = chunks_part(row, j0, min(j0 + per, chunks_of(V, lead)), V, lead, scale * LOG2E, token_of(r, V, t), marks, waves);
         if (threadIdx.x == 0) stats[i] = a;
     }
 }
+// A wavefront per row: no barriers.
 template <typename T>
 __global__ __launch_bounds__(LP_WG) void distill_join_kernel(const T *__restrict__ logits, int64_t ld, int64_t rows, int V, float scale,
                                                              Teacher t, int parts, const Part2 *__restrict__ stats, Loss o)
 {
-    __shared__ Part2 waves[LP_WG / WAVE];
-    __shared__ FinishLds lds;
+    __shared__ __attribute__((aligned(16))) int tokens[LP_WG / WAVE][QADC_MAX_ALTERNATIVES];
     const float c = scale * LOG2E;
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const Stored st = stored_of(logits + r * ld, r, V, t);
+    const int wave = threadIdx.x >> 6;
+    for (int64_t r = (int64_t)blockIdx.x * (LP_WG / WAVE) + wave; r < rows; r += (int64_t)gridDim.x * (LP_WG / WAVE)) {
+        const WaveStored st = wave_stored(logits + r * ld, r, V, t);
         Part2 a = {-INFINITY, 0.0f};
-        for (int p = threadIdx.x; p < parts; p += LP_WG) a = join(a, stats[r * parts + p], c);
+        for (int p = lane_id(); p < parts; p += WAVE) a = join(a, stats[r * parts + p], c);
         const float m = wave_max(a.m);
         raise(a, m, c);
         a.s = wave_sum(a.s);
-        __syncthreads();
-        if (lane_id() == 0) waves[threadIdx.x >> 6] = a;
-        __syncthreads();
-        a = waves[0];
-#pragma unroll
-        for (int w = 1; w < LP_WG / WAVE; ++w) a = join(a, waves[w], c);
-        float most, sum;
-        finish_row(a, st, r, scale, t, o, lds, most, sum);
+        a.m = m;
+        finish_row(a, st, r, scale, t, o, tokens[wave]);
     }
 }
 
@@ -339,7 +318,7 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
                                                              T *dlogits, int64_t ldd)
 {
     constexpr int N = Pack<T>::N, PACKS = LP_BLOCK / N;
-    __shared__ FinishLds lds;
+    __shared__ double masses[DS_WAVES];
     __shared__ GradLds grad;
     for (int64_t i = blockIdx.x; i < rows * parts; i += gridDim.x) {
         const int64_t r = i / parts;
@@ -362,7 +341,15 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
                 }
             }
         }
-        const Mass mass = mass_of(p, t.tail, lds);
+        if (threadIdx.x < QADC_MAX_ALTERNATIVES) {
+            const double P = wave_sum64(p);
+            if (lane_id() == 0) masses[threadIdx.x >> 6] = P;
+        }
+        __syncthreads();
+        double P = 0.0;
+#pragma unroll
+        for (int w = 0; w < DS_WAVES; ++w) P += masses[w];
+        const Mass mass = mass_of(P, t.tail);
         float total, share;
         shares(mass, t.tail, (double)log_tail[r], total, share);
         if ((int)threadIdx.x < t.k) {
@@ -432,7 +419,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     T *out = dlogits + r * ldd;
     const int lead = lead_of(row), wave = threadIdx.x >> 6, tid = threadIdx.x;
     const float c = scale * LOG2E;
-    const Stored st = stored_of(row, r, V, t);
+    const Stored st = stored_of(row, r, V, t, tid);
     // whole packs begin .. end - 1 from the 16 bytes that hold the row's first logit on; this thread's at begin + u THREADS + tid
     const int begin = lead ? 1 : 0, end = (V + lead) / N, here = end - begin - tid;  // (u THREADS < here: there is one)
     const int head = lead ? min(N - lead, V) : 0, tail = max(end * N - lead, head);
@@ -456,14 +443,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
         lds.grad.tokens[threadIdx.x] = st.token;
     }
     __syncthreads();
-    Mass mass = {0.0, 0.0};
+    double P64 = 0.0;
 #pragma unroll
-    for (int w = 0; w < DS_WAVES; ++w) mass.P += lds.mass[w];
-    mass.rest = t.tail && mass.P < 1.0 ? 1.0 - mass.P : 0.0;
+    for (int w = 0; w < DS_WAVES; ++w) P64 += lds.mass[w];
+    const Mass mass = mass_of(P64, t.tail);
     bool first = st.token >= 0;  // a token that is stored twice counts once for the student
     if (wave < DS_WAVES) {
         if (st.token >= 0) atomicOr(&marks[(st.token + lead) / 32], 1u << ((st.token + lead) % 32));
-        first = first && first_of(lds.grad.tokens, st.token, t.k);
+        first = first && first_of(lds.grad.tokens, st.token, t.k, tid);
         lds.grad.p[threadIdx.x] = (float)(t.tail ? p : mass.P > 0.0 ? p / mass.P : 0.0);
     }
     float m = at_edge;
@@ -534,7 +521,9 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
         if (!zero)
             write_stored(out, st, t.k, lds.grad,
                          [&](float logit, float p) { return w * fmaf(total, exp2_fast(c * (logit - m)) / sum, -p); });
-        const double l = wave_sum64(loss_of(st, p, mass.P, t.tail, none, scale, m, log((double)own + (double)others)));
+        double l = loss_of(st, p, mass.P, t.tail, none, scale, m, log((double)own + (double)others));
+        if (tid == 0 && rest) l += mass.rest * (log(mass.rest) + log1p((double)own / (double)others));
+        l = wave_sum64(l);
         if (lane_id() == 0) lds.loss[wave] = l;
     }
     __syncthreads();
@@ -542,7 +531,6 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
         double l = 0.0;
 #pragma unroll
         for (int v = 0; v < DS_WAVES; ++v) l += lds.loss[v];
-        if (rest) l += mass.rest * (log(mass.rest) + log1p((double)own / (double)others));
         loss[r] = (float)l;
     }
 }
@@ -598,8 +586,8 @@ static void launch_loss(const void *logits, int64_t ld, int64_t rows, int V, flo
     }
     launch(QADC_PROF_DISTILL, distill_part_kernel<T>, dim3((unsigned)std::min<int64_t>(rows * p.parts, 1 << 20)), dim3(LP_WG), 0, st,
            (const T *)logits, ld, rows, V, scale, t, p.parts, p.per, (Part2 *)workspace);
-    launch(QADC_PROF_DISTILL, distill_join_kernel<T>, grid, dim3(LP_WG), 0, st, (const T *)logits, ld, rows, V, scale, t, p.parts,
-           (const Part2 *)workspace, o);
+    launch(QADC_PROF_DISTILL, distill_join_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(rows, LP_WG / WAVE), 1 << 20)), dim3(LP_WG), 0,
+           st, (const T *)logits, ld, rows, V, scale, t, p.parts, (const Part2 *)workspace, o);
 }
 
 template <typename T>
