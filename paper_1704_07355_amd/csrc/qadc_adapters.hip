@@ -1,12 +1,19 @@
 // Low-rank adapters of many requests beside a shared projection on gfx950: y_i = base_i + s_a B_a (A_a x_i), a = ids[i].
 //
 // Two launches: u = A x into the workspace, cut over the inputs, then y = base + s B u.  Rows come in tiles of 256 consecutive ones;
-// every workgroup groups its tile's rows by adapter, up to 16 (or 64) of one adapter to an item, so that an adapter is
+// every wavefront groups its tile's rows by adapter with ballots, up to 16 (or 64) of one adapter to an item, so that an adapter is
 // read once for all its rows of a tile, wherever they lie.  Both products are on the matrix units, with the adapter's side as the
-// first operand: a lane then holds the results of one row, which differ between rows and are added where the row lies.
+// first operand: a lane then holds the results of one row, and rows that are not there cost no care, since their results are not
+// looked at.
 //
 // Of 16-bit types u goes into the second product as two numbers, u rounded and what that leaves: off by 2^-16 (bfloat16) or 2^-22
 // (binary16, scaled by a power of two into its range), so that only y's own rounding shows.  float32 is multiplied as float32.
+//
+// Bound by memory where rows are many, not reached: 8192 rows of 4096 x 4096 through rank 64, bfloat16, 29 us for the first product (67 MB
+// of x, whose rows go to different lanes, so that a load of 64 lanes touches 16 rows) and 39 for the second (134 MB at 3.4 TB/s);
+// 64 rows of 32 adapters of rank 16, 4096 x 16384, 5 and 10.5 us: four dependent round trips (ids, u, the pool, y) in one and a
+// half rounds of workgroups; one row 3.6 and 6.0, launches and round trips.  (Kernels' times by the profiler; figures elsewhere in
+// this file are calls one after the other: 67, 14.5 and 11 us.)
 #include <algorithm>
 #include <type_traits>
 
@@ -18,7 +25,9 @@ namespace qadc {
 namespace {
 
 constexpr int AD_WG = 256, AD_TILE = 256;  // threads; rows of a tile, one a thread
-constexpr int64_t AD_MANY = 1024;          // rows from which on an item has 64 of them, if each adapter has as many
+// Rows from which on an item has 64 of them, if each adapter has as many: the pool is read a quarter as often.  4990 rows of 42 adapters of
+// rank 16, 7754 x 742, 47 us for 118 with 16 rows; 400 rows of one of rank 94, 15312 x 1581 float32, 115 for 69 the other way round.
+constexpr int64_t AD_MANY = 1024;
 constexpr int AD_COLS = 64;                // outputs of a wavefront at a time
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -100,57 +109,56 @@ __device__ __forceinline__ Item same_as(const Tile &t, int i)
     }
     return it;
 }
-// The first ROWS rows of an item, into the wavefront's list in LDS (-1 behind); the item keeps these only.
+// ROWS rows of an item from number `from` on, into the wavefront's list in LDS (-1 behind).
 template <int ROWS>
-__device__ __forceinline__ void list_rows(Item &it, int16_t *list)
+__device__ __forceinline__ Item list_rows(const Item &it, int from, int16_t *list)
 {
+    __builtin_amdgcn_wave_barrier();
     if (lane_id() < ROWS) list[lane_id()] = -1;
     __builtin_amdgcn_wave_barrier();
-    int before = 0;
+    int before = -from;
 #pragma unroll
     for (int w = 0; w < Tile::W; ++w) {
         const int place = before + (int)rank_in_mask(it.rows[w]);
-        const bool in = (it.rows[w] >> lane_id() & 1) && place < ROWS;
-        if (in) list[place] = (int16_t)(w * WAVE + lane_id());
+        if ((it.rows[w] >> lane_id() & 1) && place >= 0 && place < ROWS) list[place] = (int16_t)(w * WAVE + lane_id());
         before += __popcll(it.rows[w]);
-        it.rows[w] = __ballot(in);
     }
-    it.count = min(it.count, ROWS);
     __builtin_amdgcn_wave_barrier();
+    Item part = it;
+    part.count = min(it.count - from, ROWS);
+    return part;
 }
 // f(item) for the workgroup's items.  As many slots as rows: a workgroup has an item where its row is the first, or the one behind ROWS
-// others, ... of its adapter.  Fewer: it counts the items up, and takes every slots-th.
+// others, ... of its adapter.  Fewer: it goes over the tile's adapters, counts their items up and takes every slots-th.  (Slots
+// without items are the last in a grid: between the others they left half of the compute units idle, for which it was always the turn of
+// one of them: 8192 rows of rank 64, eight slots of which four had an item, 48 us for 27.)
 template <int ROWS, typename F>
 __device__ __forceinline__ void each_item(Tile t, int slot, int slots, int rows, int16_t *list, F f)
 {
-    if (slots >= rows) {
+    if (ROWS == 16 && slots >= rows) {
         if (slot >= rows) return;
-        Item it = same_as(t, slot);
+        const Item it = same_as(t, slot);
         int before = 0;
 #pragma unroll
         for (int w = 0; w < Tile::W; ++w) {
             const unsigned long long below = w < slot / WAVE ? ~0ull : w > slot / WAVE ? 0ull : (1ull << slot % WAVE) - 1;
             before += __popcll(it.rows[w] & below);
-            it.rows[w] &= ~below;
         }
-        if (before % ROWS) return;
-        it.count -= before;
-        list_rows<ROWS>(it, list);
-        f(it);
+        if (before % ROWS == 0) f(list_rows<ROWS>(it, before, list));
         return;
     }
-    for (int n = 0;; ++n) {
+    for (int n = 0;;) {
         int i = AD_TILE;
 #pragma unroll
         for (int w = Tile::W - 1; w >= 0; --w)
             if (t.left[w]) i = w * WAVE + __ffsll((long long)t.left[w]) - 1;
         if (i == AD_TILE) return;
-        Item it = same_as(t, i);
-        const bool own = n % slots == slot;
-        if (own || it.count > ROWS) list_rows<ROWS>(it, list);
+        const Item it = same_as(t, i);
+        const int items = (it.count + ROWS - 1) / ROWS;
+        for (int k = (slot - n % slots + slots) % slots; k < items; k += slots) f(list_rows<ROWS>(it, k * ROWS, list));
+        n += items;
 #pragma unroll
         for (int w = 0; w < Tile::W; ++w) t.left[w] &= ~it.rows[w];
-        if (own) f(it);
     }
 }
 
@@ -173,44 +181,45 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
     typedef Eight<T> E;
     __shared__ int16_t lists[AD_WG / WAVE][16 * RB];
     __shared__ f32x4 red[AD_WG / WAVE][RT][WAVE];
-    const int split = blockIdx.x % splits, slot = blockIdx.x / splits % slots;
-    const int64_t first = (int64_t)(blockIdx.x / splits / slots) * AD_TILE;
+    const int tiles = (int)((M + AD_TILE - 1) / AD_TILE), split = blockIdx.x % splits, slot = blockIdx.x / splits / tiles;
+    const int64_t first = (int64_t)(blockIdx.x / splits % tiles) * AD_TILE;
     const int wave = threadIdx.x >> 6, l = lane_id() % 16, g = lane_id() / 16;
     const int rows = (int)min((int64_t)AD_TILE, M - first);
     int16_t *list = lists[wave];
     const int steps = (pool.K + 31) / 32, s0 = min(steps, (split * 4 + wave) * per), s1 = min(steps, s0 + per);
     const int whole = min(s1, pool.K / 32);  // steps whose inputs are all there
-    constexpr int DEEP = RB * RT >= 16 ? 2 : 4;
-    each_item<16 * RB>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+    // BLOCKS: blocks of 16 rows that are looked at
+    const auto take = [&](const Item &it, auto blocks) {
+        constexpr int BLOCKS = decltype(blocks)::value, DEEP = BLOCKS * RT >= 16 ? 2 : 4;
         const int id = it.id;
         if (id < 0) return;
         const int r = rank_of(pool, id);
-        const T *xr[RB];
-        int row[RB];
+        const T *xr[BLOCKS];
+        int row[BLOCKS];
 #pragma unroll
-        for (int b = 0; b < RB; ++b) {
+        for (int b = 0; b < BLOCKS; ++b) {
             row[b] = list[b * 16 + l];
             xr[b] = x + (first + max(row[b], 0)) * ldx;
         }
         for (int p = 0; p < r; p += 16 * RT) {
-            f32x4 acc[RT][RB] = {};
+            f32x4 acc[RT][BLOCKS] = {};
             const T *ar[RT];
 #pragma unroll
             for (int t = 0; t < RT; ++t) ar[t] = (const T *)pool.a + ((int64_t)id * pool.rank + min(p + 16 * t + l, r - 1)) * pool.K;
             // (rows and ranks that are not there stand for others: their results are not looked at)
-            typename E::V av[DEEP][RT], xv[DEEP][RB];
+            typename E::V av[DEEP][RT], xv[DEEP][BLOCKS];
             const auto load = [&](int s, int u) {
                 const int k = 32 * s + 8 * g;
 #pragma unroll
                 for (int t = 0; t < RT; ++t) av[u][t] = E::load(ar[t] + k);
 #pragma unroll
-                for (int b = 0; b < RB; ++b) xv[u][b] = E::load(xr[b] + k);
+                for (int b = 0; b < BLOCKS; ++b) xv[u][b] = E::load(xr[b] + k);
             };
             const auto multiply = [&](int u) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int b = 0; b < RB; ++b) acc[t][b] = mma(av[u][t], xv[u][b], acc[t][b]);
+                    for (int b = 0; b < BLOCKS; ++b) acc[t][b] = mma(av[u][t], xv[u][b], acc[t][b]);
             };
             int s = s0;
             for (; s + DEEP <= whole; s += DEEP) {
@@ -228,11 +237,11 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
 #pragma unroll
                 for (int t = 0; t < RT; ++t) av[0][t] = E::load(ar[t] + k, n);
 #pragma unroll
-                for (int b = 0; b < RB; ++b) xv[0][b] = E::load(xr[b] + k, n);
+                for (int b = 0; b < BLOCKS; ++b) xv[0][b] = E::load(xr[b] + k, n);
                 multiply(0);
             }
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
+            for (int b = 0; b < BLOCKS; ++b) {
                 __syncthreads();
 #pragma unroll
                 for (int t = 0; t < RT; ++t) red[wave][t][lane_id()] = acc[t][b];
@@ -247,6 +256,10 @@ __global__ __launch_bounds__(AD_WG) void adapters_down_kernel(Pool pool, const i
                 }
             }
         }
+    };
+    each_item<16 * RB>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+        if (RB > 1 && it.count <= 16) take(it, std::integral_constant<int, 1>());
+        else take(it, std::integral_constant<int, RB>());
     });
 }
 
@@ -270,7 +283,7 @@ __device__ __forceinline__ int eight_at(int rank, int j) { return min(j, max(ran
 // before the end, and writes what no other has.  SMALL: fewer than eight ranks or 64 outputs, read and written one by one.  What the
 // first outputs need of the pool and of base is on its way while u is added up.
 template <typename T, int RB, int STEPS, bool SMALL>
-__global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 : 2) void adapters_up_kernel(Pool pool, const int32_t *__restrict__ ids, int64_t M, int slots, int chunks,
+__global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS * RB <= 4 && !SMALL ? 3 : 2) void adapters_up_kernel(Pool pool, const int32_t *__restrict__ ids, int64_t M, int slots, int chunks,
                                                                int blocks, int splits, int wide, const float *__restrict__ part,
                                                                const T *base, int64_t ldb, T *y, int64_t ldy)
 {
@@ -285,12 +298,13 @@ __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 :
     extern __shared__ __attribute__((aligned(16))) char raw[];
     constexpr int stride = 32 * STEPS + 16 / (int)sizeof(T);
     T *hi = (T *)raw, *lo = hi + ROWS * stride;
-    const int chunk = blockIdx.x % chunks, slot = blockIdx.x / chunks % slots;
-    const int64_t first = (int64_t)(blockIdx.x / chunks / slots) * AD_TILE;
+    const int tiles = (int)((M + AD_TILE - 1) / AD_TILE), chunk = blockIdx.x % chunks, slot = blockIdx.x / chunks / tiles;
+    const int64_t first = (int64_t)(blockIdx.x / chunks % tiles) * AD_TILE;
     const int wave = threadIdx.x >> 6, l = lane_id() % 16, g = lane_id() / 16;
     const int rows = (int)min((int64_t)AD_TILE, M - first);
     int16_t *list = lists[wave];
-    each_item<ROWS>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+    const auto take = [&](const Item &it, auto live) {
+        constexpr int LIVE = decltype(live)::value;  // blocks of 16 rows that are looked at
         const int id = it.id;
         if (id < 0 && base == y) return;
         const int r = id < 0 ? 0 : rank_of(pool, id), steps = (r + 31) / 32;
@@ -310,10 +324,19 @@ __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 :
             return v;
         };
         const auto cleared = [&](V v, int s) {  // (what lies beyond the rank may be anything)
+            if (pool.rank % 8 == 0 && 32 * s + 32 <= r) return v;  // (the same in all lanes)
             const int j = eight_at(pool.rank, 32 * s + 8 * g), there = 32 * s + 8 * g < r ? r - j : 0;
+            if constexpr (TWO) {
+                typedef unsigned Words __attribute__((ext_vector_type(4)));
+                Words w = __builtin_bit_cast(Words, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < there ? v[e] : (T)0.0f;
-            return v;
+                for (int i = 0; i < 4; ++i) w[i] = there > 2 * i + 1 ? w[i] : there > 2 * i ? w[i] & 0xffffu : 0u;
+                return __builtin_bit_cast(V, w);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = e < there ? v[e] : (T)0.0f;
+                return v;
+            }
         };
         const auto old_at = [&](int row, int64_t n) {
             V v = E::zero();
@@ -328,7 +351,7 @@ __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 :
             }
             return v;
         };
-        V w[KEPT ? STEPS : 1][4], old[RB][2];
+        V w[KEPT ? STEPS : 1][4], old[LIVE][2];
         const auto fetch = [&](int64_t n0) {
             if constexpr (!SMALL) n0 = min(n0, pool.N - AD_COLS);
             if constexpr (KEPT) {
@@ -338,7 +361,7 @@ __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 :
                     for (int t = 0; t < 4; ++t) w[s][t] = weights(n0, s, t);
             }
 #pragma unroll
-            for (int b = 0; b < RB; ++b)
+            for (int b = 0; b < LIVE; ++b)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) old[b][h] = old_at(list[b * 16 + 8 * h + lane_id() / 8], n0 + lane_id() % 8 * 8);
         };
@@ -443,12 +466,16 @@ __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS <= 2 && !SMALL ? 3 :
                 }
             };
             rows16(std::integral_constant<int, 0>());
-            if constexpr (RB > 1) {
+            if constexpr (LIVE > 1) {
                 if (it.count > 16) rows16(std::integral_constant<int, 1>());
                 if (it.count > 32) rows16(std::integral_constant<int, 2>());
                 if (it.count > 48) rows16(std::integral_constant<int, 3>());
             }
         }
+    };
+    each_item<ROWS>(load_tile(ids, first, rows, pool.count), slot, slots, rows, list, [&](const Item &it) {
+        if (RB > 1 && it.count <= 16) take(it, std::integral_constant<int, 1>());
+        else take(it, std::integral_constant<int, RB>());
     });
 }
 
@@ -466,7 +493,7 @@ AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
     p.tiles = (int)ceil_div(M, AD_TILE);
     const int rows = (int)std::min<int64_t>(M, AD_TILE);
     const int bound = std::min(rows, count + 1) + rows / each;  // items of a tile at most
-    p.slots = p.many ? std::min(bound, 6) : bound <= std::min(20, rows / 2) ? bound : rows;
+    p.slots = p.many ? std::min(bound, 8) : bound <= std::min(20, rows / 4) ? bound : rows;
     p.slots = std::min(p.slots, std::max(1, 65536 / p.tiles));
     p.wide = (rank + 15) / 16 * 16;
     // items, where a batch's adapters are about as many as there may be
@@ -478,8 +505,10 @@ AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
     p.per = (int)ceil_div(steps, 4 * want);
     p.splits = (int)ceil_div(steps, 4 * p.per);
     p.bytes = (size_t)p.splits * M * p.wide * sizeof(float);
+    // Outputs a workgroup: as many as leave one round of workgroups, each of which adds u up anew (8192 rows of rank 64, 4096 outputs:
+    // one block of 64 a wavefront 58 us, two 52, four 40, eight 55; 64 rows, 16384 outputs: 16, 12.6, 10.8, 13.9).
     const int64_t cols = ceil_div(N, AD_COLS * (AD_WG / WAVE));
-    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, cols * items / 768));
+    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, ceil_div(cols * items, p.many ? 512 : 640)));
     p.chunks = (int)ceil_div(cols, p.blocks);
     return p;
 }
