@@ -232,6 +232,16 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _stream_of(t):
+    """The current stream, for a call on t's device, which has to be the current one."""
+    device = torch.cuda.current_device()
+    if t.device.index != device:
+        raise ValueError(f"tensor on cuda:{t.device.index}, the current device is cuda:{device}")
+    if _raw_stream is not None:
+        return _raw_stream(device)
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
 def _check(rc: int):
     if rc != QADC_OK:
         raise QadcError(rc, lib().qadc_last_error().decode())
@@ -782,7 +792,7 @@ def qadc_rms_norm(x, weight=None, residual=None, eps=1e-5, out_type=None, sum_ou
         raise ValueError(f"out_type must be {x.dtype} or torch.float8_e4m3fn")
     rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib().qadc_rms_norm(xp, ldx, rp, ldr, xtype, _vector(weight, d), _weight_type(weight, None, x), rows, d, eps, sp, ld_sum,
-                               y.data_ptr(), ytype, None if scale is None else scale.data_ptr(), rstd.data_ptr(), _stream()))
+                               y.data_ptr(), ytype, None if scale is None else scale.data_ptr(), rstd.data_ptr(), _stream_of(x)))
     return y, sum_out, scale, rstd
 
 
@@ -809,7 +819,7 @@ def qadc_rms_norm_backward(dy, h, weight, rstd, dsum=None, workspace=None, out=N
         workspace = None
     _check(lib().qadc_rms_norm_backward(dyp, lddy, sp, lds, hp, ldh, _type(h), _vector(weight, d), _weight_type(weight, None, h),
                                         _vector(rstd, rows, torch.float32), rows, d, _ptr(dx), _ptr(dw), _ptr(workspace), size,
-                                        _stream()))
+                                        _stream_of(h)))
     return dx, dw
 
 
@@ -924,7 +934,7 @@ def qadc_add_adapters(adapters, ids, x, base=None, out=None, workspace=None):
     if workspace is None:
         workspace = torch.empty((max(256, qadc_adapters_workspace_bytes(adapters, M)),), dtype=torch.uint8, device=x.device)
     _check(lib().qadc_add_adapters(ctypes.byref(adapters), _vector(ids, M, torch.int32), xp, ldx, M, bp, ldb, yp, ldy, _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream()))
+                                   workspace.numel() * workspace.element_size(), _stream_of(x)))
     return out
 
 
@@ -951,7 +961,7 @@ def qadc_distill(logits, top_idx, top_logp, scale=1.0, tail=True, workspace=None
     log_tail = torch.empty_like(loss)
     workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
     _check(lib().qadc_distill(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), loss.data_ptr(), lse.data_ptr(),
-                              log_tail.data_ptr(), _ptr(workspace), size, _stream()))
+                              log_tail.data_ptr(), _ptr(workspace), size, _stream_of(logits)))
     return loss, lse, log_tail
 
 
@@ -973,7 +983,7 @@ def qadc_distill_backward(logits, top_idx, top_logp, lse, log_tail, dloss, scale
     out, op, ldd = _gradient_like(out, logits)
     f32 = torch.float32
     _check(lib().qadc_distill_backward(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), _vector(lse, rows, f32),
-                                       _vector(log_tail, rows, f32), _vector(dloss, rows, f32), op, ldd, _stream()))
+                                       _vector(log_tail, rows, f32), _vector(dloss, rows, f32), op, ldd, _stream_of(logits)))
     return out
 
 
@@ -987,7 +997,7 @@ def qadc_distill_step(logits, top_idx, top_logp, weight, scale=1.0, tail=True, o
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
     _check(lib().qadc_distill_step(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)),
-                                   _vector(weight, rows, torch.float32), loss.data_ptr(), op, ldd, _ptr(workspace), size, _stream()))
+                                   _vector(weight, rows, torch.float32), loss.data_ptr(), op, ldd, _ptr(workspace), size, _stream_of(logits)))
     return loss, out
 
 
@@ -1023,7 +1033,7 @@ def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetiti
     _check(lib().qadc_adjust_logits(xp, ld, _type(logits), rows, V, hp, H, _vector(lengths, rows, i32), _vector(prompt, rows, i32),
                                     _vector(repetition, rows, f32), _vector(presence, rows, f32), _vector(frequency, rows, f32), bp,
                                     _vector(bias, rows * B, f32), B, mp, ldm, states, _vector(mask_of, rows, i32), op, ldo,
-                                    _stream()))
+                                    _stream_of(logits)))
     return out
 
 

@@ -493,6 +493,9 @@ AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
     p.tiles = (int)ceil_div(M, AD_TILE);
     const int rows = (int)std::min<int64_t>(M, AD_TILE);
     const int bound = std::min(rows, count + 1) + rows / each;  // items of a tile at most
+    // 64 rows to an item: a tile of a few requests has four or five items (with a slot for each of up to 24, 3198 rows of 21 adapters in any
+    // order 75 us for 59 in the second product).  16 rows: a workgroup for every row that may open one, unless these are four times
+    // as many as the items (237 rows of one adapter, 12945 outputs, counted up 23.6 us for 33; 36 rows of 15 adapters 20 for 12).
     p.slots = p.many ? std::min(bound, 8) : bound <= std::min(20, rows / 4) ? bound : rows;
     p.slots = std::min(p.slots, std::max(1, 65536 / p.tiles));
     p.wide = (rank + 15) / 16 * 16;
