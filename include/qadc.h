@@ -665,7 +665,7 @@ int qadc_distill_step(const void *logits, int64_t ld, int type, int64_t rows, in
  *   history [rows][H] i32, 0 <= H <= QADC_MAX_HISTORY, NULL when H = 0: entries outside [0, V) are passed over
  *   lengths [rows] i32 or NULL: how many entries of a row's history are used, 0 to H (H); prompt [rows] i32 or NULL: how many of
  *   the first ones are the prompt (0)
- *   repetition (> 0), presence, frequency [rows] f32, each or NULL (1, 0, 0)
+ *   repetition (1e-38 to 1e38), presence, frequency [rows] f32, each or NULL (1, 0, 0)
  *   bias_tokens [rows][B] i32, bias [rows][B] f32, 0 <= B <= QADC_MAX_R, NULL when B = 0: an entry outside [0, V) is an unused slot
  *   masks [states][mask_ld] u32 or NULL, mask_ld >= ceil(V / 32): token v is allowed where bit v % 32 of word v / 32 is set
  *   mask_of [rows] i32: which of the masks is a row's; a number outside [0, states): none.  NULL: row r has mask r, states >= rows

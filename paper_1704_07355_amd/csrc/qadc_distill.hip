@@ -111,14 +111,19 @@ struct Mass {
     double P, rest;
 };
 __device__ __forceinline__ Mass mass_of(double P, bool tail) { return {P, tail && P < 1.0 ? 1.0 - P : 0.0}; }
-// The teacher's whole probability as the gradient takes it, and the factor of what was not stored, where log Q is `log_tail`.
-__device__ __forceinline__ void shares(const Mass &a, bool tail, double log_tail, float &total, float &share)
+// The gradient's factors, where log Q is `log_tail`: T, the teacher's whole probability; and of a token that was not stored, with
+// T q - r q / Q = (T Q - r) q / Q, the factor of q / Q, which does not grow where Q is small, and log Q (1, and 0, without a tail).
+struct Factors {
+    float total, other, log_tail;
+};
+__device__ __forceinline__ Factors factors(const Mass &a, bool tail, double log_tail)
 {
     const double rest = log_tail == -INFINITY ? 0.0 : a.rest;  // (nothing is left to the student there)
     const double T = tail ? a.P + rest : a.P > 0.0 ? 1.0 : 0.0;
-    total = (float)T;
-    share = (float)(rest > 0.0 ? T - rest * exp(-log_tail) : T);
+    if (rest == 0.0) return {(float)T, (float)T, 0.0f};
+    return {(float)T, (float)(T * exp(log_tail) - rest), (float)log_tail};
 }
+constexpr float DS_NOTHING = 0x1p-100f;  // what the other tokens have, of the row's sum, that counts as nothing
 
 struct Loss {
     float *loss, *lse, *log_tail;  // lse and log_tail nullable
@@ -162,7 +167,8 @@ __device__ __forceinline__ void finish_row(Part2 others, const WaveStored &st, i
         own += first && !none ? exp2_fast(c * (st.at[i].logit - m)) : 0.0f;
     }
     own = wave_sum(own);
-    const float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
+    float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
+    if (rest < own * DS_NOTHING) rest = 0.0f;
     const double log_s = log((double)own + (double)rest);
     const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
     double l = 0.0;
@@ -350,14 +356,13 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
 #pragma unroll
         for (int w = 0; w < DS_WAVES; ++w) P += masses[w];
         const Mass mass = mass_of(P, t.tail);
-        float total, share;
-        shares(mass, t.tail, (double)log_tail[r], total, share);
+        const Factors by = factors(mass, t.tail, (double)log_tail[r]);
         if ((int)threadIdx.x < t.k) {
             grad.tokens[threadIdx.x] = st.token;
             grad.p[threadIdx.x] = (float)(t.tail ? p : mass.P > 0.0 ? p / mass.P : 0.0);
         }
-        const float f = w * share;
-        const auto value = [&](float logit) { return zero ? 0.0f : f * exp_of<T>(fmaf(scale, logit, -l)); };
+        const float f = w * by.other;
+        const auto value = [&](float logit) { return zero ? 0.0f : f * exp_of<T>(fmaf(scale, logit, -l) - by.log_tail); };
         for (int64_t j = j0; j < j1; ++j) {
             typename Pack<T>::V q[PACKS];
             if ((j > 0 || lead == 0) && (j + 1) * LP_CHUNK - lead <= v1) {
@@ -391,7 +396,7 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
             }
         }
         __syncthreads();
-        write_stored(out, st, t.k, grad, [&](float logit, float own) { return w * fmaf(total, exp_of<T>(fmaf(scale, logit, -l)), -own); });
+        write_stored(out, st, t.k, grad, [&](float logit, float own) { return w * fmaf(by.total, exp_of<T>(fmaf(scale, logit, -l)), -own); });
         __syncthreads();
     }
 }
@@ -496,15 +501,16 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     for (int w = 0; w < W; ++w) others += lds.others[w];
 #pragma unroll
     for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
+    if (others < own * DS_NOTHING) others = 0.0f;
     const float sum = own + others;
-    // r / Q, left out where the student has nothing left
-    const bool rest = mass.rest > 0.0 && others != 0.0f;
+    const bool rest = mass.rest > 0.0 && others != 0.0f;  // (left out where the student has nothing left)
     const double whole = t.tail ? mass.P + (rest ? mass.rest : 0.0) : mass.P > 0.0 ? 1.0 : 0.0;
     const float total = (float)whole;
-    const float share = rest ? (float)(whole - mass.rest * (1.0 + (double)own / (double)others)) : total;
+    // of q: T - r / Q, as (T others / sum - r) / others of e
+    const float share = rest ? (float)((whole * ((double)others / (double)sum) - mass.rest) / (double)others) : total / sum;
     const float w = scale * weight[r];
     const bool zero = w == 0.0f || none;
-    const float f = zero ? 0.0f : w * share / sum;
+    const float f = zero ? 0.0f : w * share;
     const auto value = [&](float logit) { return zero ? 0.0f : f * exp2_fast(c * (logit - m0)); };
     if (edge < V) out[edge] = (T)value(at_edge);
 #pragma unroll
@@ -548,7 +554,7 @@ int check_distill(const char *who, int type, int64_t ld, int64_t rows, int V, fl
 }
 
 // How the loss of a call is cut: a row per workgroup where the rows alone nearly fill the chip, parts of rows otherwise.
-constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024;
+constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024, DS_STEP = 128;
 struct Cut {
     int parts, per;
 };
@@ -664,7 +670,7 @@ int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, 
     float *lse = (float *)((char *)workspace + stats), *log_tail = (float *)((char *)workspace + stats + each);
     const size_t e = type_bytes(type);
     const size_t bytes = (size_t)V * e;
-    if (rows >= 128 && rows < 1 << 30 && bytes <= 262144) {
+    if (rows >= DS_STEP && rows <= 1 << 21 && bytes <= 262144) {  // (a grid's threads are counted in 32 bits)
         QADC_BY_TYPE(type, {
             if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
             else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
