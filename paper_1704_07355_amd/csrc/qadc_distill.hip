@@ -408,7 +408,7 @@ struct StepLds {
 };
 
 // Loss and gradient of a row whose logits stay in the registers of its workgroup: PACKS packs a thread, read and written once, and the
-// up to seven logits at either end that fill no pack of 16 bytes one a thread.  What the gradient needs (the largest logit, the two
+// logits before the first line of 128 bytes and behind the last pack of 16 one a thread.  What the gradient needs (the largest logit, the two
 // sums, the teacher's mass) comes first, the loss after the stores.  128 registers: half of them hold the row.
 template <typename T, int THREADS, int PACKS>
 __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logits, int64_t ld, int V, float scale, Teacher t,
@@ -417,17 +417,19 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
 {
     constexpr int N = Pack<T>::N, W = THREADS / WAVE;
     typedef typename Pack<T>::V P;
-    __shared__ uint32_t marks[THREADS * PACKS * N / 32 + 1];  // (and the pack before the first whole one)
+    constexpr int LINE = 128 / (int)sizeof(T), MARKS = (THREADS * PACKS * N + LINE) / 32 + 1;
+    __shared__ uint32_t marks[MARKS];  // from the beginning of the row's first line on
     __shared__ StepLds lds;
     const int64_t r = blockIdx.x;
     const T *row = logits + r * ld;
     T *out = dlogits + r * ldd;
-    const int lead = lead_of(row), wave = threadIdx.x >> 6, tid = threadIdx.x;
+    const int lead = (int)((uintptr_t)row % 128 / sizeof(T)), wave = threadIdx.x >> 6, tid = threadIdx.x;
     const float c = scale * LOG2E;
     const Stored st = stored_of(row, r, V, t, tid);
-    // whole packs begin .. end - 1 from the 16 bytes that hold the row's first logit on; this thread's at begin + u THREADS + tid
-    const int begin = lead ? 1 : 0, end = (V + lead) / N, here = end - begin - tid;  // (u THREADS < here: there is one)
-    const int head = lead ? min(N - lead, V) : 0, tail = max(end * N - lead, head);
+    // whole packs begin .. end - 1 from the line that holds the row's first logit on, the first of them where a line begins; this thread's
+    // at begin + u THREADS + tid
+    const int begin = lead ? LINE / N : 0, end = (V + lead) / N, here = end - begin - tid;  // (u THREADS < here: there is one)
+    const int head = lead ? min(LINE - lead, V) : 0, tail = max(end * N - lead, head);
     const int edge = tid < head ? tid : tail + tid - head;  // < V: this thread's logit at an end
     const T *from = row + (begin + tid) * N - lead;
     T *to = out + (begin + tid) * N - lead;
@@ -439,7 +441,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     }
     const float at_edge = edge < V ? (float)row[edge] : -INFINITY;
     // the teacher, while the row comes in
-    for (int i = threadIdx.x; i < THREADS * PACKS * N / 32 + 1; i += THREADS) marks[i] = 0;
+    for (int i = threadIdx.x; i < MARKS; i += THREADS) marks[i] = 0;
     double p = 0.0;
     if (wave < DS_WAVES) {
         p = st.token < 0 ? 0.0 : exp((double)st.logp);
@@ -554,7 +556,7 @@ int check_distill(const char *who, int type, int64_t ld, int64_t rows, int V, fl
 }
 
 // How the loss of a call is cut: a row per workgroup where the rows alone nearly fill the chip, parts of rows otherwise.
-constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024, DS_STEP = 128;
+constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024, DS_STEP = 64;
 struct Cut {
     int parts, per;
 };
@@ -670,7 +672,10 @@ int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, 
     float *lse = (float *)((char *)workspace + stats), *log_tail = (float *)((char *)workspace + stats + each);
     const size_t e = type_bytes(type);
     const size_t bytes = (size_t)V * e;
-    if (rows >= DS_STEP && rows <= 1 << 21 && bytes <= 262144) {  // (a grid's threads are counted in 32 bits)
+    // A row in a workgroup's registers: 16 x 16384 bfloat16 12 us, 17 in the two steps that other rows take, 256 x 65536 19 and 35, 1024 x
+    // 131072 115 and 133; of rows beyond 128 KB, one a compute unit, from 64 on (32: 25 and 19; 128: 26 and 35).  A grid's threads are
+    // counted in 32 bits.
+    if ((bytes <= 131072 || rows >= DS_STEP) && rows <= 1 << 21 && bytes <= 262144) {
         QADC_BY_TYPE(type, {
             if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
             else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
