@@ -432,8 +432,15 @@ __global__ __launch_bounds__(RMS_WG) void rms_dx_kernel(RmsBack b, const void *w
 }
 
 int rms_back_rows(int d) { return d > NORM_LONG ? 16 : std::max(1, 512 / norm_group(d)); }  // rows of a workgroup at a time
-int rms_back_most(int d) { return d <= NORM_LONG && norm_group(d) > 512 ? 256 : 512; }
-int rms_back_wgs(int64_t rows, int d) { return norm_wgs(rows, rms_back_rows(d), rms_back_most(d)); }
+// The most workgroups, each of which leaves a row of sums: two a compute unit for 16-bit rows of up to 4096 elements (16384 x 4096 91 us,
+// 97 with one), one for wider rows (8192 x 8192 92, 97 with two: a workgroup of 1024 threads fills the registers) and for float32
+// (16384 x 4096 171, 181 with two).
+constexpr int RMS_BACK_MOST = 512;
+int rms_back_most(int type, int d)
+{
+    return d <= NORM_LONG && (norm_group(d) > 512 || type == QADC_TYPE_F32) ? RMS_BACK_MOST / 2 : RMS_BACK_MOST;
+}
+int rms_back_wgs(int type, int64_t rows, int d) { return norm_wgs(rows, rms_back_rows(d), rms_back_most(type, d)); }
 
 int rms_check(const char *who, int type, int wtype, int64_t rows, int d)
 {
@@ -446,12 +453,12 @@ int rms_check(const char *who, int type, int wtype, int64_t rows, int d)
 
 }  // namespace
 
-// Enough for these rows and for any fewer.
+// Enough for these rows and for any fewer, of any type.
 size_t rms_norm_workspace(int64_t rows, int d)
 {
     if (rows < 0 || d < 1 || d > INT32_MAX - 16384) return 0;
-    const int64_t alone = std::min<int64_t>(rows, rms_back_rows(d) * (int64_t)rms_back_most(d));  // the most rows done in one turn
-    return (size_t)rms_back_wgs(alone, d) * (size_t)d * sizeof(float);
+    const int64_t alone = std::min<int64_t>(rows, rms_back_rows(d) * (int64_t)RMS_BACK_MOST);  // the most rows done in one turn
+    return (size_t)ceil_div(alone, rms_back_rows(d)) * (size_t)d * sizeof(float);
 }
 
 template <typename T, int G, int E>
@@ -459,7 +466,9 @@ static void rms_launch_rows(const T *x, int64_t ldx, const T *res, int64_t ldr, 
                             float eps, const RmsOut &o, hipStream_t st)
 {
     constexpr int THREADS = G > 256 ? G : 256;
-    constexpr int most = 256 * std::max(1, (E == 16 ? 1024 : sizeof(T) == 2 ? 2048 : 1536) / THREADS);
+    // As many threads as fit a compute unit with their registers: float32 16384 x 4096 190 us, 203 with 1536 threads, 193 with 1024; of sixteen
+    // elements 4096 x 16384 234, 240 with 2048.
+    constexpr int most = 256 * std::max(1, (E == 16 ? 1024 : 2048) / THREADS);
     const unsigned grid = (unsigned)norm_wgs(rows, THREADS / G, most);
     if (res)
         launch(QADC_PROF_RMS, rms_rows_kernel<T, G, E, THREADS, true>, dim3(grid), dim3(THREADS), 0, st, x, ldx, res, ldr, weight,
@@ -524,11 +533,10 @@ int rms_norm(const void *x, int64_t ldx, const void *res, int64_t ldr, int type,
 }
 
 template <typename T, int G, int E>
-static void rms_launch_back(const RmsBack &b, const void *weight, bool wide, int64_t rows, int d, hipStream_t st)
+static void rms_launch_back(const RmsBack &b, const void *weight, bool wide, int64_t rows, int d, unsigned grid, hipStream_t st)
 {
     constexpr int THREADS = G > 512 ? G : 512;
     constexpr bool AHEAD = E == 8;  // (sixteen elements a thread leave no registers for the next row's)
-    const unsigned grid = (unsigned)rms_back_wgs(rows, d);
     if (b.dsum)
         launch(QADC_PROF_RMS, rms_back_kernel<T, G, E, THREADS, AHEAD, true>, dim3(grid), dim3(THREADS), 0, st, b, weight, wide, rows, d);
     else
@@ -545,7 +553,7 @@ int rms_norm_backward(const void *dy, int64_t lddy, const void *dsum, int64_t ld
     if (rows > 0 && (!dy || !h || !rstd)) return fail(QADC_EINVAL, "%s: null pointer", who);
     if (dx && ((dx == dy && lddy != d) || (dx == h && ldh != d) || (dx == dsum && ldds != d)))
         return fail(QADC_EINVAL, "%s: in place needs dense rows", who);
-    const int count = rows > 0 ? rms_back_wgs(rows, d) : 0;  // without rows the sum of no parts is written
+    const int count = rows > 0 ? rms_back_wgs(type, rows, d) : 0;  // without rows the sum of no parts is written
     if (dweight) {
         const size_t need = (size_t)count * (size_t)d * sizeof(float);
         if (rows > 0 && (!workspace || workspace_bytes < need))
@@ -557,7 +565,7 @@ int rms_norm_backward(const void *dy, int64_t lddy, const void *dsum, int64_t ld
     if (rows > 0 && (dx || dweight)) {
         QADC_BY_TYPE(type, {
             if (d <= NORM_LONG) {
-                by_group(d, [&](auto g, auto e) { rms_launch_back<T, g.value, e.value>(b, weight, wide, rows, d, st); });
+                by_group(d, [&](auto g, auto e) { rms_launch_back<T, g.value, e.value>(b, weight, wide, rows, d, (unsigned)count, st); });
             } else {
                 if (dweight)
                     launch(QADC_PROF_RMS, rms_weights_kernel<T>, dim3((unsigned)ceil_div(d, NORM_WG), (unsigned)count), dim3(NORM_WG),
