@@ -316,8 +316,9 @@ __device__ __forceinline__ void write_stored(T *out, const Stored &st, int k, co
     if (first) out[st.token] = (T)value(st.logit, p);
 }
 
-// A workgroup per `per` chunks of a row: first every token's share as if it was not stored, then the stored tokens.
-template <typename T>
+// A workgroup per `per` chunks of a row: first every token's share as if it was not stored, then the stored tokens.  STREAM: stores past
+// the caches.
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, int64_t ld, int64_t rows, int V, float scale, Teacher t,
                                                              int parts, int per, const float *__restrict__ lse,
                                                              const float *__restrict__ log_tail, const float *__restrict__ dloss,
@@ -374,7 +375,9 @@ __global__ __launch_bounds__(LP_WG) void distill_grad_kernel(const T *logits, in
                 for (int u = 0; u < PACKS; ++u) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) q[u][e] = (T)value((float)q[u][e]);
-                    *reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead)) = q[u];
+                    auto *const to = reinterpret_cast<typename Pack<T>::V *>(out + pack_at<T>(j, u, lead));
+                    if constexpr (STREAM) __builtin_nontemporal_store(q[u], to);
+                    else *to = q[u];
                 }
             } else {
 #pragma unroll
@@ -410,6 +413,7 @@ struct StepLds {
 // Loss and gradient of a row whose logits stay in the registers of its workgroup: PACKS packs a thread, read and written once, and the
 // logits before the first line of 128 bytes and behind the last pack of 16 one a thread.  What the gradient needs (the largest logit, the two
 // sums, the teacher's mass) comes first, the loss after the stores.  128 registers: half of them hold the row.
+// Stores past the caches: 2048 x 128001 bfloat16 222 us and 240 through them, 512 x 32768 20.5 and 23.8 (2048 x 32768 alone 59 and 58).
 template <typename T, int THREADS, int PACKS>
 __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logits, int64_t ld, int V, float scale, Teacher t,
                                                                   const float *__restrict__ weight, float *__restrict__ loss, T *dlogits,
@@ -555,15 +559,17 @@ int check_distill(const char *who, int type, int64_t ld, int64_t rows, int V, fl
     return QADC_OK;
 }
 
-// How the loss of a call is cut: a row per workgroup where the rows alone nearly fill the chip, parts of rows otherwise.
-constexpr int64_t DS_WHOLE = 400, DS_PARTS = 1024, DS_STEP = 64;
+// How the loss of a call is cut: a row per workgroup where the rows alone nearly fill the chip or are short, parts of rows otherwise.  A
+// call of bfloat16 rows, whole and in parts: 400 x 131072 29.4 us and 26.9, 512 x 131072 30.3 and 31.7, 400 x 65536 18.4 and 18.6; 64 x 32000
+// 11.7 and 14.4, 64 x 50000 15.0 and 14.6, 64 x 131072 26.4 and 14.7, 1 x 50000 12.9 and 14.3.
+constexpr int64_t DS_WHOLE = 400, DS_SHORT = 5, DS_PARTS = 1024;  // rows; chunks of a row (some 40000 logits); workgroups
 struct Cut {
     int parts, per;
 };
 Cut cut_of(int64_t rows, int V)
 {
     const int64_t chunks = ceil_div((int64_t)V + 7, LP_CHUNK);  // (a row begins up to seven logits into its first pack)
-    const int64_t want = rows >= DS_WHOLE ? 1 : ceil_div(DS_PARTS, std::max<int64_t>(1, rows));
+    const int64_t want = rows >= DS_WHOLE || chunks <= DS_SHORT ? 1 : ceil_div(DS_PARTS, std::max<int64_t>(1, rows));
     const int per = (int)ceil_div(chunks, std::min(chunks, want));
     return {(int)ceil_div(chunks, per), per};
 }
@@ -605,10 +611,15 @@ static void launch_grad(const void *logits, int64_t ld, int64_t rows, int V, flo
     // (where rows begin off 16 bytes, up to seven logits into their first pack)
     const bool even = (uintptr_t)dlogits % 16 == 0 && (size_t)ldd * sizeof(T) % 16 == 0;
     const int64_t chunks = ceil_div((int64_t)V + (even ? 0 : 7), LP_CHUNK);
+    // Chunks a workgroup: more of them share the stored tokens and the factors, fewer fill the chip.  One and four: 32 x 128001 bfloat16 10.5 us
+    // and 12.7, 128 x 128001 19.6 and 20.9, 512 x 128001 57.7 and 50.9.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));
     const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
-    launch(QADC_PROF_DISTILL, distill_grad_kernel<T>, dim3((unsigned)std::min<int64_t>(rows * parts, 1 << 22)), dim3(LP_WG), 0, st,
-           (const T *)logits, ld, rows, V, scale, t, parts, per, lse, log_tail, dloss, (T *)dlogits, ldd);
+    // A gradient beyond the last cache's size goes past it: 2048 x 128001 bfloat16 203 us and 229, but 512 x 128001 60 and 51.
+    const bool stream = (size_t)rows * V * sizeof(T) > ((size_t)384 << 20);
+    const auto kernel = stream ? &distill_grad_kernel<T, true> : &distill_grad_kernel<T, false>;
+    launch(QADC_PROF_DISTILL, kernel, dim3((unsigned)std::min<int64_t>(rows * parts, 1 << 22)), dim3(LP_WG), 0, st, (const T *)logits, ld,
+           rows, V, scale, t, parts, per, lse, log_tail, dloss, (T *)dlogits, ldd);
 }
 
 int distill(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *idx, const float *logp, int k,
@@ -675,7 +686,7 @@ int distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, 
     // A row in a workgroup's registers: 16 x 16384 bfloat16 12 us, 17 in the two steps that other rows take, 256 x 65536 19 and 35, 1024 x
     // 131072 115 and 133; of rows beyond 128 KB, one a compute unit, from 64 on (32: 25 and 19; 128: 26 and 35).  A grid's threads are
     // counted in 32 bits.
-    if ((bytes <= 131072 || rows >= DS_STEP) && rows <= 1 << 21 && bytes <= 262144) {
+    if ((bytes <= 131072 || rows >= 64) && rows <= 1 << 21 && bytes <= 262144) {
         QADC_BY_TYPE(type, {
             if (bytes <= 16384) launch_step<T, 256, 4>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);
             else if (bytes <= 32768) launch_step<T, 256, 8>(logits, ld, rows, V, scale, t, weight, loss, dlogits, ldd, st);

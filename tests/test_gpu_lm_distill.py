@@ -107,7 +107,8 @@ def _check(x, idx, logp, w, scale, tail):
 @pytest.mark.parametrize("type", list(TYPES))
 @pytest.mark.parametrize("rows,V,k", [(1, 1, 1), (2, 2, 1), (3, 7, 9), (5, 100, 0), (4, 1000, 128), (2, 8192, 20), (3, 8193, 64), (7, 20011, 5),
                                       (1, 131072, 20), (2, 140001, 100), (130, 1000, 33), (131, 8190, 128), (129, 16500, 3), (140, 33000, 64),
-                                      (128, 65536, 64), (130, 65537, 20), (450, 3001, 17), (401, 12000, 1), (128, 131065, 10)])
+                                      (128, 65536, 64), (130, 65537, 20), (450, 3001, 17), (401, 12000, 1), (128, 131065, 10), (3, 40961, 64), (50, 50021, 20),
+                                      (12, 90003, 128)])
 def test_loss_and_gradients(rows, V, k, type):
     for tail in (True, False):
         scale = 1.0 if V % 2 else 0.6
@@ -115,7 +116,7 @@ def test_loss_and_gradients(rows, V, k, type):
 
 
 @pytest.mark.parametrize("type", list(TYPES))
-@pytest.mark.parametrize("rows,V,ld,shift", [(5, 1000, 1003, 1), (3, 9001, 9004, 3), (2, 7, 9, 5), (140, 4000, 4005, 7), (135, 70000, 70001, 1)])
+@pytest.mark.parametrize("rows,V,ld,shift", [(5, 1000, 1003, 1), (3, 9001, 9004, 3), (2, 7, 9, 5), (140, 4000, 4005, 7), (135, 70000, 70001, 1), (6, 41003, 41004, 3)])
 def test_rows_apart_and_unaligned(rows, V, ld, shift, type):
     import paper_1704_07355_amd as Q
     x, idx, logp, w = _inputs(rows, V, 20, type, ld)
@@ -238,10 +239,11 @@ def test_the_alternatives_of_a_teacher_are_what_is_stored():
         assert g.abs().max().item() <= 8 * E + 40 * EPS
 
 
-def test_equal_calls_give_equal_bits_and_a_workspace_serves_fewer_rows():
+@pytest.mark.parametrize("V", [20000, 50000])
+def test_equal_calls_give_equal_bits_and_a_workspace_serves_fewer_rows(V):
     import paper_1704_07355_amd as Q
-    x, idx, logp, w = _inputs(420, 20000, 20, "bf16", 3)
-    ws = torch.empty(Q.qadc_distill_workspace_bytes(420, 20000), dtype=torch.uint8, device=DEV)
+    x, idx, logp, w = _inputs(420, V, 20, "bf16", 3)
+    ws = torch.empty(Q.qadc_distill_workspace_bytes(420, V), dtype=torch.uint8, device=DEV)
     for rows in (1, 2, 7, 64, 127, 128, 399, 400, 420):
         a = Q.qadc_distill_step(x[:rows], idx[:rows], logp[:rows], w[:rows], workspace=ws)
         b = Q.qadc_distill(x[:rows], idx[:rows], logp[:rows], workspace=ws)
@@ -252,6 +254,22 @@ def test_equal_calls_give_equal_bits_and_a_workspace_serves_fewer_rows():
     for V in (1, 8192, 20000, 300000):
         most = Q.qadc_distill_workspace_bytes(1000, V)
         assert all(Q.qadc_distill_workspace_bytes(r, V) <= most for r in (1, 2, 100, 399, 400, 401, 999))
+
+
+def test_a_large_gradient_is_that_of_its_rows():
+    """Beyond the last cache's size the stores go past it; the bits stay."""
+    import paper_1704_07355_amd as Q
+    rows, V, k = 3300, 64001, 20
+    x = torch.randn((rows, V), generator=gen(7), device=DEV, dtype=torch.bfloat16)
+    _, idx, logp, w = _inputs(rows, 200, k, "bf16", 8)
+    lse, log_tail = Q.qadc_distill(x, idx, logp)[1:]
+    room = apart(torch.zeros_like(x), V + 5, 3)
+    Q.qadc_distill_backward(x, idx, logp, lse, log_tail, w, out=room)
+    for r in range(0, rows, 1100):
+        part = slice(r, r + 1100)
+        want = Q.qadc_distill_backward(x[part], idx[part], logp[part], lse[part], log_tail[part], w[part])
+        assert torch.equal(room[part], want)
+    assert torch.isnan(torch.as_strided(room, (rows - 1, 5), (V + 5, 1), room.storage_offset() + V).float()).all()
 
 
 def test_no_rows_and_wrong_tensors():
