@@ -646,7 +646,7 @@ int qadc_distill_backward(const void *logits, int64_t ld, int type, int64_t rows
 
 /*
  * Loss and gradient in one call, where every row's share of the loss is known beforehand: loss as qadc_distill writes it, dlogits
- * as qadc_distill_backward with dloss = weight.  Rows of up to 256 KB are read and written once.
+ * as qadc_distill_backward with dloss = weight.  Rows of up to 256 KB (128 KB in calls of fewer than 64) are read and written once.
  *   weight [rows] f32;  workspace as for qadc_distill (always needed)
  */
 int qadc_distill_step(const void *logits, int64_t ld, int type, int64_t rows, int V, float scale, const uint32_t *top_idx,

@@ -163,16 +163,16 @@ __device__ __forceinline__ void finish_row(Part2 others, const WaveStored &st, i
     }
     __builtin_amdgcn_wave_barrier();
     const Mass mass = mass_of(wave_sum64(P), t.tail);
-    const float m = fmaxf(others.m, wave_max(most));
-    const bool none = m == -INFINITY;
+    const float m = fmaxf(others.m, wave_max(most)), m0 = m == -INFINITY ? 0.0f : m;
     float own = 0.0f;
 #pragma unroll
     for (int i = 0; i < DS_WAVES; ++i) {  // a token that is stored twice counts once for the student
         const bool first = st.at[i].token >= 0 && first_of(tokens, st.at[i].token, t.k, i * WAVE + lane_id());
-        own += first && !none ? exp2_fast(c * (st.at[i].logit - m)) : 0.0f;
+        own += first ? exp2_fast(c * (st.at[i].logit - m0)) : 0.0f;
     }
     own = wave_sum(own);
-    float rest = none ? 0.0f : others.s * exp2_fast(shift_of(others.m, m, c));
+    float rest = others.s * exp2_fast(shift_of(others.m, m, c));
+    const bool none = m == -INFINITY && own + rest == 0.0f;  // (NaN where there is one among the masked)
     if (rest < own * DS_NOTHING) rest = 0.0f;
     const double log_s = log((double)own + (double)rest);
     const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
@@ -482,8 +482,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     m = lds.most[0];
 #pragma unroll
     for (int w = 1; w < W; ++w) m = fmaxf(m, lds.most[w]);
-    const bool none = m == -INFINITY;
-    const float m0 = none ? 0.0f : m;
+    const float m0 = m == -INFINITY ? 0.0f : m;
     float s = edge < V && !(marks[(edge + lead) / 32] >> ((edge + lead) % 32) & 1) ? exp2_fast(c * (at_edge - m0)) : 0.0f;
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
@@ -503,7 +502,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     s = wave_sum(s);
     if (lane_id() == 0) lds.others[wave] = s;
     if (wave < DS_WAVES) {
-        const float own = wave_sum(first && !none ? exp2_fast(c * (st.logit - m)) : 0.0f);
+        const float own = wave_sum(first ? exp2_fast(c * (st.logit - m0)) : 0.0f);
         if (lane_id() == 0) lds.own[wave] = own;
     }
     __syncthreads();
@@ -514,6 +513,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
     if (others < own * DS_NOTHING) others = 0.0f;
     const float sum = own + others;
+    const bool none = m == -INFINITY && sum == 0.0f;  // (NaN where there is one among the masked)
     const bool rest = mass.rest > 0.0 && others != 0.0f;  // (left out where the student has nothing left)
     const double whole = t.tail ? mass.P + (rest ? mass.rest : 0.0) : mass.P > 0.0 ? 1.0 : 0.0;
     const float total = (float)whole;

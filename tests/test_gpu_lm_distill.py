@@ -180,6 +180,28 @@ def test_rows_with_little_in_them(rows):
     assert (Q.qadc_distill_backward(x, idx, logp, loss, loss, none) == 0).all()
 
 
+@pytest.mark.parametrize("rows,V", [(5, 500), (200, 500), (5, 50021), (130, 70001), (410, 41000)])
+def test_rows_of_nothing_but_nan(rows, V):
+    """A NaN with nothing beside it, stored or not, is no row with nothing left."""
+    import paper_1704_07355_amd as Q
+    for type in TYPES:
+        x, idx, logp, w = _inputs(rows, V, 12, type, 5)
+        w = w.abs() + 0.1
+        x[:4] = -math.inf
+        x[0] = math.nan
+        x[1, 450] = math.nan
+        idx[1] = torch.arange(12, device=DEV)
+        x[2, idx[2, 0]] = math.nan
+        for tail in (True, False):
+            loss, lse, log_tail = Q.qadc_distill(x, idx, logp, 1.0, tail)
+            step_loss, step = Q.qadc_distill_step(x, idx, logp, w, 1.0, tail)
+            grad = Q.qadc_distill_backward(x, idx, logp, lse, log_tail, w, 1.0, tail)
+            for t in (loss, lse, step_loss, step.float(), grad.float()):
+                assert torch.isnan(t[:3]).all() and not torch.isnan(t[3:]).any()
+            assert loss[3] == step_loss[3] == math.inf and lse[3] == log_tail[3] == -math.inf
+            assert (step[3] == 0).all() and (grad[3] == 0).all()
+
+
 @pytest.mark.parametrize("rows", [4, 160])
 def test_a_student_that_gives_the_tail_next_to_nothing(rows):
     """Q down to 1e-25 keeps its gradient, whatever the row's share of the loss; below 2^-100 it counts as nothing."""
