@@ -504,7 +504,11 @@ AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
     const int steps = (K + 31) / 32;
     const int least = std::max(1, steps / 8);  // two steps a wavefront at least
     const int read = std::max(1, 65536 / (each * p.wide * 4));  // what every workgroup of the second product reads of the first
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(least, read), 768 / std::max<int64_t>(1, items)));
+    // More than that where a wavefront would have more than 16 steps, counted for every 64 ranks: 14336 inputs and rank 128, 2048 rows 191 us
+    // with two splits and 87 with eight, 16 rows 29 with eight and 23 with fourteen; but of 4096 and 64, 4096 rows, 43 with four and 50
+    // with eight.
+    const int longer = std::min(p.many ? 8 : 16, steps * ((rank + 63) / 64) / 64);
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(least, std::max(read, longer)), 768 / std::max<int64_t>(1, items)));
     p.per = (int)ceil_div(steps, 4 * want);
     p.splits = (int)ceil_div(steps, 4 * p.per);
     p.bytes = (size_t)p.splits * M * p.wide * sizeof(float);
