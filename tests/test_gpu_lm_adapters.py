@@ -85,7 +85,9 @@ def _check(w, ids, x, base, **how):
 @pytest.mark.parametrize("type", list(TYPES))
 @pytest.mark.parametrize("M,N,K,rank,count", [(1, 1, 1, 1, 1), (1, 64, 64, 16, 3), (2, 65, 33, 8, 2), (5, 257, 100, 3, 4), (16, 100, 1000, 17, 5),
                                               (17, 300, 4096, 64, 9), (64, 1000, 515, 16, 40), (255, 70, 96, 33, 300), (257, 130, 130, 128, 7),
-                                              (700, 513, 260, 100, 3), (64, 2000, 31, 5, 1), (3, 5000, 3000, 16, 2), (1000, 40, 2000, 20, 2)])
+                                              (700, 513, 260, 100, 3), (64, 2000, 31, 5, 1), (3, 5000, 3000, 16, 2), (1000, 40, 2000, 20, 2),
+                                              (1100, 333, 520, 64, 11), (1030, 130, 2100, 128, 16), (1500, 50, 200, 40, 23),
+                                              (1200, 300, 64, 5, 3), (1024, 200, 640, 128, 1)])
 def test_mixed_rows(M, N, K, rank, count, type):
     w = _pool(count, rank, N, K, type, M + N)
     x, base = _rows(M, N, K, type, K)
@@ -98,7 +100,7 @@ def test_mixed_rows(M, N, K, rank, count, type):
 
 
 @pytest.mark.parametrize("type", list(TYPES))
-@pytest.mark.parametrize("M,count", [(256, 1), (300, 4), (1000, 3), (513, 2), (640, 10)])
+@pytest.mark.parametrize("M,count", [(256, 1), (300, 4), (1000, 3), (513, 2), (640, 10), (1100, 3), (2000, 7)])
 def test_segments(M, count, type):
     """Requests one after the other, of lengths that end inside tiles, one of them without an adapter."""
     import paper_1704_07355_amd as Q
