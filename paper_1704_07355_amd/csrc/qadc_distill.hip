@@ -620,7 +620,8 @@ static void launch_grad(const void *logits, int64_t ld, int64_t rows, int V, flo
     // and 12.7, 128 x 128001 19.6 and 20.9, 512 x 128001 57.7 and 50.9.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));
     const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
-    // A gradient beyond the last cache's size goes past it: 2048 x 128001 bfloat16 203 us and 229, but 512 x 128001 60 and 51.
+    // A gradient beyond the last cache's size goes past it: 2048 x 128001 bfloat16 203 us and 229 (with six sets of inputs in turn 213 and 213),
+    // but 512 x 128001 59 and 51.
     const bool stream = (size_t)rows * V * sizeof(T) > ((size_t)384 << 20);
     const auto kernel = stream ? &distill_grad_kernel<T, true> : &distill_grad_kernel<T, false>;
     launch(QADC_PROF_DISTILL, kernel, dim3((unsigned)std::min<int64_t>(rows * parts, 1 << 22)), dim3(LP_WG), 0, st, (const T *)logits, ld,
