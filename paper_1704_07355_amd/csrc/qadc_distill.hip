@@ -128,7 +128,10 @@ __device__ __forceinline__ Factors factors(const Mass &a, bool tail, double log_
     if (rest == 0.0) return {(float)T, (float)T, 0.0f};
     return {(float)T, (float)(T * exp(log_tail) - rest), (float)log_tail};
 }
-constexpr float DS_NOTHING = 0x1p-100f;  // what the other tokens have, of the row's sum, that counts as nothing
+constexpr double DS_NOTHING = 1e-37;  // what the other tokens have, of what the stored ones have, that counts as nothing
+// Below this they are taken in 64 bits: as float32 they run out of the exponent.  (Above it, of a row of 2^17 exponentials each of which is there
+// down to 2^-126, no more than 2^-29 of the sum is missing.)
+constexpr float DS_DEEP = 0x1p-80f;
 
 struct Loss {
     float *loss, *lse, *log_tail;  // lse and log_tail nullable
@@ -171,11 +174,12 @@ __device__ __forceinline__ void finish_row(Part2 others, const WaveStored &st, i
         own += first ? exp2_fast(c * (st.at[i].logit - m0)) : 0.0f;
     }
     own = wave_sum(own);
-    float rest = others.s * exp2_fast(shift_of(others.m, m, c));
-    const bool none = m == -INFINITY && own + rest == 0.0f;  // (NaN where there is one among the masked)
-    if (rest < own * DS_NOTHING) rest = 0.0f;
-    const double log_s = log((double)own + (double)rest);
-    const double log_tail = rest == 0.0f ? -INFINITY : -log1p((double)own / (double)rest);
+    double rest = others.s * exp2_fast(shift_of(others.m, m, c));
+    if (rest < (double)own * DS_DEEP) rest = (double)others.s * exp((double)scale * ((double)others.m - (double)m));
+    const bool none = m == -INFINITY && (double)own + rest == 0.0;  // (NaN where there is one among the masked)
+    if (rest < (double)own * DS_NOTHING) rest = 0.0;
+    const double log_s = log((double)own + rest);
+    const double log_tail = rest == 0.0 ? -INFINITY : -log1p((double)own / rest);
     double l = 0.0;
 #pragma unroll
     for (int i = 0; i < DS_WAVES; ++i) l += loss_of(st.at[i], p[i], mass.P, t.tail, none, scale, m, log_s);
@@ -483,7 +487,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
 #pragma unroll
     for (int w = 1; w < W; ++w) m = fmaxf(m, lds.most[w]);
     const float m0 = m == -INFINITY ? 0.0f : m;
-    float s = edge < V && !(marks[(edge + lead) / 32] >> ((edge + lead) % 32) & 1) ? exp2_fast(c * (at_edge - m0)) : 0.0f;
+    const bool marked_edge = edge < V && (marks[(edge + lead) / 32] >> ((edge + lead) % 32) & 1);
+    float s = edge < V && !marked_edge ? exp2_fast(c * (at_edge - m0)) : 0.0f;
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
         asm volatile("" : "+v"(x[u]));  // (converted again rather than kept)
@@ -511,18 +516,61 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
     for (int w = 0; w < W; ++w) others += lds.others[w];
 #pragma unroll
     for (int w = 0; w < DS_WAVES; ++w) own += lds.own[w];
-    if (others < own * DS_NOTHING) others = 0.0f;
-    const float sum = own + others;
+    // What the other tokens have, relative to the row's largest logit as float32: far below it their exponentials run out of the exponent
+    // one by one, and are summed again, relative to the largest of their own.
+    float base = m0;  // what `others` and the gradient's exponentials are relative to
+    double left = others;  // `others` relative to m0
+    if (mass.rest > 0.0 && others < own * DS_DEEP) {  // (the same in all threads)
+        float v = edge < V && !marked_edge ? at_edge : -INFINITY;
+#pragma unroll
+        for (int u = 0; u < PACKS; ++u) {
+            asm volatile("" : "+v"(x[u]));
+            const unsigned b = u * THREADS < here ? marks_at<N>(marks, (begin + u * THREADS + tid) * N) : 0u;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v = fmaxf(v, b >> i & 1 ? -INFINITY : (float)x[u][i]);
+            asm volatile("" : "+v"(v));
+        }
+        v = wave_max(v);
+        if (lane_id() == 0) lds.most[wave] = v;
+        __syncthreads();
+        v = lds.most[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v = fmaxf(v, lds.most[w]);
+        base = v == -INFINITY ? m0 : v;
+        s = edge < V && !marked_edge ? exp2_fast(c * (at_edge - base)) : 0.0f;
+#pragma unroll
+        for (int u = 0; u < PACKS; ++u) {
+            asm volatile("" : "+v"(x[u]));
+            const unsigned b = u * THREADS < here ? marks_at<N>(marks, (begin + u * THREADS + tid) * N) : 0u;
+            float part = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) part += b >> i & 1 ? 0.0f : exp2_fast(c * ((float)x[u][i] - base));
+            s += part;
+            asm volatile("" : "+v"(s));
+        }
+        s = wave_sum(s);
+        if (lane_id() == 0) lds.others[wave] = s;
+        __syncthreads();
+        others = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) others += lds.others[w];
+        left = (double)others * exp((double)scale * ((double)base - (double)m0));
+        if (left < (double)own * DS_NOTHING) {
+            left = 0.0;
+            base = m0;
+        }
+    }
+    const float sum = own + (float)left;
     const bool none = m == -INFINITY && sum == 0.0f;  // (NaN where there is one among the masked)
-    const bool rest = mass.rest > 0.0 && others != 0.0f;  // (left out where the student has nothing left)
+    const bool rest = mass.rest > 0.0 && left != 0.0;  // (left out where the student has nothing left)
     const double whole = t.tail ? mass.P + (rest ? mass.rest : 0.0) : mass.P > 0.0 ? 1.0 : 0.0;
     const float total = (float)whole;
     // of q: T - r / Q, as (T others / sum - r) / others of e
-    const float share = rest ? (float)((whole * ((double)others / (double)sum) - mass.rest) / (double)others) : total / sum;
+    const float share = rest ? (float)((whole * (left / (double)sum) - mass.rest) / (double)others) : total / sum;
     const float w = scale * weight[r];
     const bool zero = w == 0.0f || none;
     const float f = zero ? 0.0f : w * share;
-    const auto value = [&](float logit) { return zero ? 0.0f : f * exp2_fast(c * (logit - m0)); };
+    const auto value = [&](float logit) { return zero ? 0.0f : f * exp2_fast(c * (logit - base)); };
     if (edge < V) out[edge] = (T)value(at_edge);
 #pragma unroll
     for (int u = 0; u < PACKS; ++u) {
@@ -538,8 +586,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
         if (!zero)
             write_stored(out, st, t.k, lds.grad,
                          [&](float logit, float p) { return w * fmaf(total, exp2_fast(c * (logit - m)) / sum, -p); });
-        double l = loss_of(st, p, mass.P, t.tail, none, scale, m, log((double)own + (double)others));
-        if (tid == 0 && rest) l += mass.rest * (log(mass.rest) + log1p((double)own / (double)others));
+        double l = loss_of(st, p, mass.P, t.tail, none, scale, m, log((double)own + left));
+        if (tid == 0 && rest) l += mass.rest * (log(mass.rest) + log1p((double)own / left));
         l = wave_sum64(l);
         if (lane_id() == 0) lds.loss[wave] = l;
     }

@@ -224,6 +224,26 @@ def test_a_student_that_gives_the_tail_next_to_nothing(rows):
     assert grad[others].abs().max() < 2.0 ** -99 and step[others].abs().max() < 2.0 ** -99
 
 
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("rows,V,k", [(4, 400, 12), (160, 400, 12), (3, 7001, 128), (70, 60001, 20), (90, 131072, 40), (2, 140001, 9)])
+def test_a_tail_of_any_depth_counts(rows, V, k, type):
+    """Q between 1e-24 and 1e-36 has its term in the loss and its gradient, in one call and in two, also where no single token's share
+    is a float32 any more; the log probabilities of the tokens beside it are those of the definition."""
+    g = gen(V)
+    idx = torch.stack([torch.randperm(V, generator=g, device=DEV)[:k] for _ in range(rows)]).to(torch.int32)
+    logp = torch.log_softmax(torch.randn((rows, k), generator=g, device=DEV), 1) - 0.5
+    w = 0.1 + torch.rand((rows,), generator=g, device=DEV)
+    for share in (1e-24, 1e-29, 1e-31, 1e-34, 1e-36):
+        # (the logits' mean exponential is exp(1/2) of that of their mean, among the stored tokens and the others)
+        depth = math.log(V / k / share)
+        x = torch.randn((rows, V), generator=g, device=DEV) - depth
+        x.scatter_(1, idx.long(), torch.randn((rows, k), generator=g, device=DEV))
+        loss, lse, log_tail, grad, step = _check(x.to(TYPES[type]), idx, logp, w, 1.0, True)
+        assert torch.isfinite(log_tail).all() and (loss > 8.0).all()  # r (log r - log Q), r = 0.39, of which is 21 to 33
+        # a scale between the logits and their exponentials moves nothing
+        _check((2.0 * x).to(TYPES[type]), idx, logp, w, 0.5, True)
+
+
 @pytest.mark.parametrize("rows", [3, 150])
 def test_gradient_against_differences(rows):
     """Central differences of sum(w loss) in 64 bits, along random directions."""
