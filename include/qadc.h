@@ -559,7 +559,7 @@ typedef struct qadc_adapters {
 
 /*
  *   ids [M] i32: a number outside [0, count) is a row without an adapter, y = base
- *   x [M][ldx], base [M][ldb] (or NULL: 0) of `type`, 0 <= M <= 2^24, (M / 256) * (N / 2048) at most about 2^20
+ *   x [M][ldx], base [M][ldb] (or NULL: 0) of `type`, 0 <= M <= 2^24, ceil(M / 256) * ceil(N / 2048) < 2^24
  *   y [M][ldy] of `type` (output; may be base when ldb == ldy: then rows without an adapter are not touched; must not overlap x)
  *   workspace >= qadc_adapters_workspace_bytes(adapters, M), 16-byte aligned; it need not be cleared and is not left cleared, and
  *   serves fewer rows too

@@ -29,6 +29,7 @@ constexpr int AD_WG = 256, AD_TILE = 256;  // threads; rows of a tile, one a thr
 // rank 16, 7754 x 742, 47 us for 118 with 16 rows; 400 rows of one of rank 94, 15312 x 1581 float32, 115 for 69 the other way round.
 constexpr int64_t AD_MANY = 1024;
 constexpr int AD_COLS = 64;                // outputs of a wavefront at a time
+constexpr int64_t AD_GROUPS = ((int64_t)1 << 32) / AD_WG;  // of a launch, less one: their threads are counted in 32 bits
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
@@ -521,6 +522,9 @@ AdPlan plan_adapters(int64_t M, int64_t N, int K, int rank, int count)
     const int64_t cols = ceil_div(N, AD_COLS * (AD_WG / WAVE));
     p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(8, ceil_div(cols * items, p.many ? 512 : 640)));
     p.chunks = (int)ceil_div(cols, p.blocks);
+    // A grid's threads are counted in 32 bits: with very many outputs a workgroup takes several of its tile's items one after the other.
+    const int64_t most = (AD_GROUPS - 1) / ((int64_t)p.tiles * std::max(p.splits, p.chunks));
+    p.slots = (int)std::min<int64_t>(p.slots, std::max<int64_t>(1, most));
     return p;
 }
 
@@ -579,7 +583,7 @@ int add_adapters(const qadc_adapters *w, const int32_t *ids, const void *x, int6
     if (!w->a || !w->b || !ids || !x || !y) return fail(QADC_EINVAL, "%s: null pointer", who);
     if (base == y && ldb != ldy) return fail(QADC_EINVAL, "%s: in place needs equal row distances", who);
     const AdPlan p = plan_adapters(M, w->N, w->K, w->rank, w->count);
-    if ((int64_t)p.tiles * p.slots * std::max(p.splits, p.chunks) > 1 << 24)
+    if ((int64_t)p.tiles * p.slots * std::max(p.splits, p.chunks) >= AD_GROUPS)
         return fail(QADC_EINVAL, "%s: M=%lld rows of N=%lld outputs are too many for one call", who, (long long)M, (long long)w->N);
     if (!workspace || workspace_bytes < p.bytes)
         return fail(QADC_ENOMEM, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, p.bytes);

@@ -99,6 +99,29 @@ def test_mixed_rows(M, N, K, rank, count, type):
     assert torch.equal(_check(w, ids, x, again, out=again), y)  # in place
 
 
+def test_more_outputs_than_a_launch_has_workgroups_for():
+    """256 rows, each of which may open an item, by 2^27 outputs and some: the pool repeats itself, and so has the result to."""
+    import paper_1704_07355_amd as Q
+    M, N, K, rank, count, period = 256, (1 << 27) + 4096, 40, 8, 4, 4096
+    small = _pool(count, rank, period, K, "bf16", 3)
+    a, b, scales, ranks = small.tensors
+    w = Q.qadc_adapters(a, b.repeat(1, N // period, 1), scales, ranks)
+    x, _ = _rows(M, period, K, "bf16", 3)
+    ids = torch.randint(-1, count + 1, (M,), generator=gen(1), device=DEV, dtype=torch.int32)
+    y = Q.qadc_add_adapters(w, ids, x)
+    want, tol = _want(small, ids, x, None, "bf16")
+    within(y[:, :period], want, tol, "y")
+    for r in range(M):
+        row = y[r].view(-1, period)
+        assert torch.equal(row, row[:1].expand(row.shape)), r
+
+
+def test_more_rows_than_tiles_with_a_workgroup_for_each_row():
+    w = _pool(1100, 8, 64, 24, "bf16", 5)
+    x, base = _rows(70001, 64, 24, "bf16", 5)
+    _check(w, torch.randint(-1, 1101, (70001,), generator=gen(6), device=DEV, dtype=torch.int32), x, base)
+
+
 @pytest.mark.parametrize("type", list(TYPES))
 @pytest.mark.parametrize("M,count", [(256, 1), (300, 4), (1000, 3), (513, 2), (640, 10), (1100, 3), (2000, 7)])
 def test_segments(M, count, type):

@@ -114,3 +114,24 @@ def test_add_adapters():
     assert b"qadc_add_adapters" in L.qadc_last_error()
     # more workgroups than a launch takes
     assert f(w=pool(N=1 << 30, count=300), M=1 << 24, ldb=1 << 30, ldy=1 << 30, size=1 << 40) == Q.QADC_EINVAL
+
+
+def test_add_adapters_takes_as_many_rows_and_outputs_as_it_says():
+    """ceil(M / 256) * ceil(N / 2048) < 2^24 on both sides, with adapters that leave rows single and with few; a call that is not refused for its
+    size goes on to its workspace, which is too small."""
+    import ctypes
+    L = Q.lib()
+
+    def f(M, N, count):
+        w = Q.qadc_adapters.__new__(Q.qadc_adapters)
+        for name, v in dict(a=PTR, b=PTR, N=N, K=64, rank=16, count=count, type=1).items():
+            setattr(w, name, v)
+        return L.qadc_add_adapters(ctypes.byref(w), PTR, PTR, 64, M, None, 0, 3 * PTR, N, PTR, 16, None)
+
+    for count in (1, 4, 300, 2000, 1 << 20):
+        for M, N in ((4096, 1 << 24), (65536, 1 << 20), (256, 1 << 27), (256, (1 << 27) + 2048), (255, 1 << 30), (1 << 24, 1), (1 << 24, 255 * 2048),
+                     (31 * 256, 1 << 30), ((1 << 24) - 300, 255 * 2048 - 1), (4097 * 256, 4094 * 2048), (1, 1 << 30), (3000 * 256, 5000 * 2048)):
+            assert f(M, N, count) == Q.QADC_ENOMEM, (M, N, count)
+        for M, N in ((1 << 24, 256 * 2048), (32 * 256, 1 << 30), (4096 * 256, 4096 * 2048), (31 * 256 + 1, 1 << 30), (1 << 24, 255 * 2048 + 1),
+                     (1 << 24, 1 << 30)):
+            assert f(M, N, count) == Q.QADC_EINVAL, (M, N, count)
