@@ -168,6 +168,19 @@ def test_zeros_tiny_large_and_broken_rows():
         assert (big == 0).all()
 
 
+def test_the_gradient_of_a_very_long_weight():
+    """More columns than the threads of a launch in one direction reach, sixteen a column, would be."""
+    import paper_1704_07355_amd as Q
+    rows, d = 2, (1 << 28) + 37
+    h, dy = (torch.randn((rows, d), generator=gen(s), device=DEV, dtype=torch.bfloat16) for s in (1, 2))
+    rstd = torch.tensor([0.7, 1.9], device=DEV)
+    none, dw = Q.qadc_rms_norm_backward(dy, h, None, rstd, need_dx=False)
+    for c in range(0, d, 1 << 26):
+        n = h[:, c:c + (1 << 26)].double() * rstd.double()[:, None]
+        g = dy[:, c:c + (1 << 26)].double()
+        within(dw[c:c + (1 << 26)], (g * n).sum(0), (_chain(rows, 300) + 4 * EPS) * (g * n).abs().sum(0), "dweight")
+
+
 def test_gradient_against_differences():
     """Central differences of sum(dy y) + sum(dsum h) in 64 bits, along random directions of x and of the weight."""
     import paper_1704_07355_amd as Q
