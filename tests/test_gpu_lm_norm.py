@@ -166,6 +166,22 @@ def test_gradient_by_differences(rows, d):
         assert abs(got - want) <= 20 * h * h * abs(got) + 2.0 ** -22 * size * 4 / h, (at, got, want)
 
 
+def test_the_gradients_of_very_long_weights():
+    """More columns than the threads of a launch in one direction reach, sixteen for each of both sums, would be."""
+    import paper_1704_07355_amd as Q
+    rows, d = 2, (1 << 27) + 37
+    x, dy = (torch.randn((rows, d), generator=gen(s), device=DEV, dtype=torch.bfloat16) for s in (1, 2))
+    mean, rstd = torch.tensor([0.1, -0.2], device=DEV), torch.tensor([0.7, 1.9], device=DEV)
+    none, dw, db = Q.qadc_layer_norm_backward(dy, x, None, mean, rstd, need_dx=False)
+    B = (math.ceil(rows / 256) + 300) * EPS
+    for c in range(0, d, 1 << 26):
+        at = slice(c, c + (1 << 26))
+        xs, g, mu, rs = x[:, at].double(), dy[:, at].double(), mean.double()[:, None], rstd.double()[:, None]
+        h = (xs - mu) * rs
+        within(dw[at], (g * h).sum(0), (B + 4 * EPS) * (g * h).abs().sum(0) + (g.abs() * 3 * EPS * (h.abs() + mu.abs() * rs)).sum(0), "dweight")
+        within(db[at], g.sum(0), B * g.abs().sum(0), "dbias")
+
+
 def test_no_rows_and_optional_outputs():
     import paper_1704_07355_amd as Q
     x, w, b, dy = _inputs(20, 333, "f16", 3, "own")
