@@ -63,6 +63,31 @@ __device__ __forceinline__ void group_sum_max(float &s, float &m, float *lds, in
     }
 }
 
+// Where eps leaves rows to themselves (TINY): float32 squares of elements below 2^-63 lose bits, and below 2^-75 are zeros.  A row whose sum is
+// this small is summed again in 64 bits, and normalised as 2^64 times itself.  Kernels of their own: the ordinary ones would have 10 to 20 more
+// registers.
+constexpr float RMS_TINY = 0x1p-90f, RMS_UP = 0x1p64f;
+constexpr float RMS_EPS_TINY = 0x1p-100f;  // from here on eps outweighs what such squares lose
+
+// The sum of s over a group of G threads, in every one of them.  Barriers before and behind.
+template <int G>
+__device__ __forceinline__ double group_sum64(double s, double *lds)
+{
+#pragma unroll
+    for (int o = (G < WAVE ? G : WAVE) / 2; o; o >>= 1) s += __shfl_xor(s, o);
+    if constexpr (G > WAVE) {
+        constexpr int W = G / WAVE;
+        const int wave = threadIdx.x >> 6, first = wave / W * W;
+        __syncthreads();
+        if (lane_id() == 0) lds[wave] = s;
+        __syncthreads();
+        s = 0.0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += lds[first + w];
+    }
+    return s;
+}
+
 // The factor that brings a row's values into 8 bits, and the scale that takes them back.  most: the largest |y|.  A row of zeros
 // has scale 0; below 448 / 2^126 the values use less of the range; a NaN stays one.
 __device__ __forceinline__ float to_8bit(float most, float &scale)
@@ -119,7 +144,7 @@ struct RmsOut {
 };
 
 // A group of G threads per row, THREADS / G rows of a workgroup at a time.  RES: there is a residual.
-template <typename T, int G, int E, int THREADS, bool RES>
+template <typename T, int G, int E, int THREADS, bool RES, bool TINY>
 __global__ __launch_bounds__(THREADS) void rms_rows_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr,
                                                            const void *__restrict__ weight, bool wide, int64_t rows, int d,
                                                            float eps, RmsOut o)
@@ -127,6 +152,7 @@ __global__ __launch_bounds__(THREADS) void rms_rows_kernel(const T *x, int64_t l
     typedef Part<T, G, E> P;
     constexpr int N = P::N;
     __shared__ float lds[4 * (1024 / WAVE)];
+    __shared__ double lds64[1024 / WAVE];
     constexpr int R = THREADS / G;
     const int t = threadIdx.x % G;
     int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / G;
@@ -161,7 +187,27 @@ __global__ __launch_bounds__(THREADS) void rms_rows_kernel(const T *x, int64_t l
             most = fmaxf(most, fabsf(now.x[i] * w[i]));
         }
         group_sum_max<G>(s, most, lds, turns);
-        const float rstd = 1.0f / sqrtf(s / (float)d + eps);
+        float rstd = 1.0f / sqrtf(s / (float)d + eps), of_row = rstd;
+        if (TINY && __syncthreads_or(s < RMS_TINY)) {  // (all groups of the workgroup)
+            double s64 = 0.0;
+            float up = 0.0f;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                s64 += (double)now.x[i] * (double)now.x[i];
+                up = fmaxf(up, fabsf(now.x[i] * RMS_UP * w[i]));
+            }
+            s64 = group_sum64<G>(s64, lds64);
+            float none = 0.0f;
+            group_sum_max<G>(none, up, lds, turns);
+            if (s < RMS_TINY) {
+                const double one = 1.0 / sqrt(s64 / (double)d + (double)eps);
+                of_row = (float)one;
+                rstd = (float)(one / RMS_UP);
+                most = up;
+#pragma unroll
+                for (int i = 0; i < E; ++i) now.x.set(i, now.x[i] * RMS_UP);
+            }
+        }
         if (r < rows) {
             if (o.bytes) {
                 float scale;
@@ -180,7 +226,7 @@ __global__ __launch_bounds__(THREADS) void rms_rows_kernel(const T *x, int64_t l
                 for (int i = 0; i < E; ++i) out.set(i, now.x[i] * rstd * w[i]);
                 out.store((T *)o.y + r * d, t, d);
             }
-            if (t == 0 && o.rstd) o.rstd[r] = rstd;
+            if (t == 0 && o.rstd) o.rstd[r] = of_row;
         }
         r += ahead;
         return more;
@@ -335,12 +381,13 @@ __device__ __forceinline__ void weight_pack(const void *w, bool wide, int64_t c,
         v[e] = !w || c + e >= d ? 1.0f : wide ? ((const float *)w)[c + e] : (float)((const T *)w)[c + e];
 }
 
-template <typename T>
+template <typename T, bool TINY>
 __global__ __launch_bounds__(RMS_WG) void rms_long_kernel(const T *x, int64_t ldx, const T *res, int64_t ldr, const void *weight,
                                                           bool wide, int64_t rows, int d, float eps, RmsOut o)
 {
     constexpr int N = Pack<T>::N;
     __shared__ float lds[4 * (1024 / WAVE)];
+    __shared__ double lds64[1024 / WAVE];
     int turns = 0;
     for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *xr = x + r * ldx;
@@ -363,16 +410,37 @@ __global__ __launch_bounds__(RMS_WG) void rms_long_kernel(const T *x, int64_t ld
             }
         }
         group_sum_max<RMS_WG>(s, most, lds, turns);
-        const float rstd = 1.0f / sqrtf(s / (float)d + eps);
+        float rstd = 1.0f / sqrtf(s / (float)d + eps), of_row = rstd, up = 1.0f;
+        const T *from = res ? sum : xr;  // (each thread reads what it wrote itself)
+        if (TINY && s < RMS_TINY) {  // (the same in all threads)
+            double s64 = 0.0;
+            most = 0.0f;
+            for (int64_t c = (int64_t)threadIdx.x * N; c < d; c += RMS_WG * N) {
+                const typename Pack<T>::V v = load_pack(from, c, d);
+                float w[N];
+                weight_pack<N, T>(weight, wide, c, d, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    s64 += (double)v[e] * (double)v[e];
+                    most = fmaxf(most, fabsf((float)v[e] * RMS_UP * w[e]));
+                }
+            }
+            s64 = group_sum64<RMS_WG>(s64, lds64);
+            float none = 0.0f;
+            group_sum_max<RMS_WG>(none, most, lds, turns);
+            const double one = 1.0 / sqrt(s64 / (double)d + (double)eps);
+            of_row = (float)one;
+            rstd = (float)(one / RMS_UP);
+            up = RMS_UP;
+        }
         float scale = 0.0f;
         const float f = o.bytes ? to_8bit(most * rstd, scale) : 1.0f;
-        const T *from = res ? sum : xr;  // (each thread reads what it wrote itself)
         for (int64_t c = (int64_t)threadIdx.x * N; c < d; c += RMS_WG * N) {
             typename Pack<T>::V v = load_pack(from, c, d);
             float w[N], y[N];
             weight_pack<N, T>(weight, wide, c, d, w);
 #pragma unroll
-            for (int e = 0; e < N; ++e) y[e] = (float)v[e] * rstd * w[e];
+            for (int e = 0; e < N; ++e) y[e] = (TINY ? (float)v[e] * up : (float)v[e]) * rstd * w[e];
             if (o.bytes) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) y[e] *= f;
@@ -385,7 +453,7 @@ __global__ __launch_bounds__(RMS_WG) void rms_long_kernel(const T *x, int64_t ld
         }
         if (threadIdx.x == 0) {
             if (o.bytes) o.scale[r] = scale;
-            if (o.rstd) o.rstd[r] = rstd;
+            if (o.rstd) o.rstd[r] = of_row;
         }
     }
 }
@@ -461,7 +529,7 @@ size_t rms_norm_workspace(int64_t rows, int d)
     return (size_t)rms_back_wgs(alone, d) * (size_t)d * sizeof(float);
 }
 
-template <typename T, int G, int E>
+template <typename T, int G, int E, bool TINY>
 static void rms_launch_rows(const T *x, int64_t ldx, const T *res, int64_t ldr, const void *weight, bool wide, int64_t rows, int d,
                             float eps, const RmsOut &o, hipStream_t st)
 {
@@ -471,10 +539,10 @@ static void rms_launch_rows(const T *x, int64_t ldx, const T *res, int64_t ldr, 
     constexpr int most = 256 * std::max(1, (E == 16 ? 1024 : 2048) / THREADS);
     const unsigned grid = (unsigned)norm_wgs(rows, THREADS / G, most);
     if (res)
-        launch(QADC_PROF_RMS, rms_rows_kernel<T, G, E, THREADS, true>, dim3(grid), dim3(THREADS), 0, st, x, ldx, res, ldr, weight,
+        launch(QADC_PROF_RMS, rms_rows_kernel<T, G, E, THREADS, true, TINY>, dim3(grid), dim3(THREADS), 0, st, x, ldx, res, ldr, weight,
                wide, rows, d, eps, o);
     else
-        launch(QADC_PROF_RMS, rms_rows_kernel<T, G, E, THREADS, false>, dim3(grid), dim3(THREADS), 0, st, x, ldx, res, ldr, weight,
+        launch(QADC_PROF_RMS, rms_rows_kernel<T, G, E, THREADS, false, TINY>, dim3(grid), dim3(THREADS), 0, st, x, ldx, res, ldr, weight,
                wide, rows, d, eps, o);
 }
 
@@ -519,13 +587,22 @@ int rms_norm(const void *x, int64_t ldx, const void *res, int64_t ldr, int type,
     const bool wide = wtype == QADC_TYPE_F32;
     QADC_BY_TYPE(type, {
         const T *xt = (const T *)x, *rt = (const T *)res;
-        if (d > NORM_LONG) {
-            launch(QADC_PROF_RMS, rms_long_kernel<T>, dim3(norm_grid(rows)), dim3(RMS_WG), 0, st, xt, ldx, rt, ldr, weight, wide, rows,
-                   d, eps, o);
+        const auto run = [&](auto tiny) {
+            constexpr bool TINY = decltype(tiny)::value;
+            if (d > NORM_LONG) {
+                launch(QADC_PROF_RMS, rms_long_kernel<T, TINY>, dim3(norm_grid(rows)), dim3(RMS_WG), 0, st, xt, ldx, rt, ldr, weight, wide,
+                       rows, d, eps, o);
+            } else {
+                by_group(d, [&](auto g, auto e) {
+                    rms_launch_rows<T, g.value, e.value, TINY>(xt, ldx, rt, ldr, weight, wide, rows, d, eps, o, st);
+                });
+            }
+        };
+        if constexpr (!std::is_same<T, _Float16>::value) {  // (which has no squares below 2^-48)
+            if (eps < RMS_EPS_TINY) run(std::true_type());
+            else run(std::false_type());
         } else {
-            by_group(d, [&](auto g, auto e) {
-                rms_launch_rows<T, g.value, e.value>(xt, ldx, rt, ldr, weight, wide, rows, d, eps, o, st);
-            });
+            run(std::false_type());
         }
     });
     QADC_HIP_TRY(hipGetLastError());

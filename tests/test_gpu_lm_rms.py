@@ -168,6 +168,70 @@ def test_zeros_tiny_large_and_broken_rows():
         assert (big == 0).all()
 
 
+def _equal(a, b):
+    return all(p is q is None or torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -146, 2.0 ** -116])
+def test_rows_so_small_that_their_squares_are_not_float32(eps, type):
+    """Rows without an eps that outweighs them, small ones beside ordinary ones in a workgroup: each as if it was alone."""
+    import paper_1704_07355_amd as Q
+    sizes = [1.0, 1e-4, 2.0 ** -12] if type == "f16" else [1.0, 1e-15, 1e-19, 1e-21, 1e-23, 1e-30, 1e-36]
+    for d in (1, 7, 100, 130, 300, 1000, 1500, 4096, 5003, 12000, 16385):
+        g = torch.Generator().manual_seed(d)
+        size = torch.tensor([sizes[i % len(sizes)] for i in range(23)], dtype=torch.float64)[:, None]
+        x, r = ((0.5 + torch.rand((23, d), generator=g, dtype=torch.float64)) * size for _ in range(2))
+        x, r = x.to(TYPES[type]).to(DEV), (0.3 * r).to(TYPES[type]).to(DEV)
+        w = (1.0 + 0.2 * torch.randn((d,), generator=g)).to(DEV)
+        dy, ds = (0.1 * torch.randn((23, d), generator=g).to(TYPES[type]).to(DEV) for _ in range(2))
+        for weight in (w, None):
+            for res in (None, r):
+                for out_type in (None, E4M3):
+                    got = Q.qadc_rms_norm(x, weight, res, eps, out_type)
+                    _check_forward(got, x, res, weight, eps, type)
+                h, rstd = x if res is None else got[1], got[3]
+                _check_backward(Q.qadc_rms_norm_backward(dy, h, weight, rstd, ds), dy, ds, h, weight, rstd, type)
+        one = Q.qadc_rms_norm(x[6:7], w, r[6:7], eps)
+        whole = Q.qadc_rms_norm(x, w, r, eps)
+        assert _equal(one, [None if t is None else t[6:7] for t in whole])
+        # in place, and rows apart
+        x2, r2 = apart(x, d + 3, 1), r.clone()
+        assert _equal(Q.qadc_rms_norm(x2, w, r2, eps, sum_out=x2, out=r2), whole)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+def test_rows_beyond_the_smallest_reciprocal(type):
+    """Without an eps, rows of a root mean square below 2^-128 have a y, but no float32 holds their rstd."""
+    import paper_1704_07355_amd as Q
+    least = 2.0 ** -149 if type == "f32" else 2.0 ** -133
+    for d in (3, 200, 4097, 20000):
+        steps = torch.randint(1, 9, (4, d), generator=torch.Generator().manual_seed(d))
+        x = (steps.double() * least).to(TYPES[type]).to(DEV)
+        want = steps.double().to(DEV)
+        want = want / torch.sqrt((want * want).mean(1, keepdim=True))
+        err = _chain(d) + 8 * EPS
+        y, _, _, rstd = Q.qadc_rms_norm(x, eps=0.0)
+        within(y, want, UNIT[type] * want + want * err * (1 + UNIT[type]), "y")
+        assert torch.isinf(rstd).all()
+        q, _, scale, _ = Q.qadc_rms_norm(x, eps=0.0, out_type=E4M3)
+        s = want.amax(1, keepdim=True) / 448
+        within(scale[:, None], s, (err + 4 * EPS) * s, "scale")
+        moved = 2 * err + 8 * EPS
+        within(q, want / s, want / s * (2.0 ** -4 * (1 + moved) + moved) + 2.0 ** -10, "q")
+        # an eps of their size
+        for eps in (2.0 ** -149, 2.0 ** -140):
+            y, _, _, rstd = Q.qadc_rms_norm(x, eps=eps)
+            rs = 1 / torch.sqrt((x.double() * x.double()).mean(1, keepdim=True) + eps)
+            within(rstd[:, None], rs, err * rs, "rstd")
+            within(y, x.double() * rs, UNIT[type] * x.double() * rs + LEAST[type] + x.double() * rs * err * (1 + UNIT[type]), "y")
+    zero = torch.zeros((2, 300), dtype=TYPES[type], device=DEV)
+    y, _, _, rstd = Q.qadc_rms_norm(zero, eps=2.0 ** -149)
+    assert (y == 0).all() and torch.equal(rstd, torch.full_like(rstd, 2.0 ** 74.5))
+    q, _, scale, _ = Q.qadc_rms_norm(zero, eps=0.0, out_type=E4M3)
+    assert torch.isnan(q.float()).all() and torch.isnan(scale).all()
+
+
 def test_the_gradient_of_a_very_long_weight():
     """More columns than the threads of a launch in one direction reach, sixteen a column, would be."""
     import paper_1704_07355_amd as Q
