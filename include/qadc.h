@@ -467,8 +467,8 @@ size_t qadc_layer_norm_workspace_bytes(int64_t rows, int d);
  * in float32.  h, the stream that goes on, is written to `sum`; it is the rounded h that is normalised, which is what the
  * backward pass reads.  y is rounded once to `type`, or, with `ytype` QADC_TYPE_E4M3, to 8 bits with a scale per row:
  *     scale = max |y| / 448,  q = y * (448 / max |y|) to the nearest 8-bit number (ties to even); y is about q * scale.
- * A row of zeros has scale 0; with eps = 0 it has no direction and becomes NaN.  A row that holds an infinity or a NaN becomes NaN, its
- * scale too.  Squares are summed in float32: |h| up to 1e19 / sqrt(d); rows beyond become zeros.  Rows that are small beside a small eps, or
+ * A row of zeros has scale 0; with eps = 0 it has no direction and becomes NaN.  A row that holds a NaN becomes NaN; in 8 bits one that holds an
+ * infinity too, and their scales, while a y of `type` is NaN where h is infinite and 0 elsewhere (rstd is 0).  Squares are summed in float32: |h| up to 1e19 / sqrt(d); rows beyond become zeros.  Rows that are small beside a small eps, or
  * without one, are summed in float64: below a mean of squares plus eps of 2^-256 only rstd does not fit (inf: such a row has no gradient).
  *   x [rows][ldx], residual [rows][ldr] (or NULL) of `type`, 1 <= d <= 2^31 - 16385
  *   weight [d] of `wtype`: QADC_TYPE_F32 or `type`, or NULL (1);  eps >= 0

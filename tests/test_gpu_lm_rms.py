@@ -168,6 +168,27 @@ def test_zeros_tiny_large_and_broken_rows():
         assert (big == 0).all()
 
 
+@pytest.mark.parametrize("type", list(TYPES))
+def test_rows_with_infinities(type):
+    """In 8 bits the row is NaN; of the rows' type its infinite elements are, and the others vanish beside them.  Its neighbours stay."""
+    import paper_1704_07355_amd as Q
+    for d in (64, 500, 20000):
+        x, r, w, dy, _ = _inputs(5, d, type, d, "f32")
+        x[1, 3], x[3, d - 1], r[3, 7] = math.inf, -math.inf, math.nan
+        for eps in (1e-5, 0.0):
+            y, total, _, rstd = Q.qadc_rms_norm(x, w, r, eps)
+            assert torch.isnan(y[1, 3]) and torch.isnan(y[1]).sum() == 1 and (y[1].nan_to_num() == 0).all() and rstd[1] == 0
+            assert torch.isnan(y[3]).all() and torch.isnan(rstd[3])
+            q, _, scale, _ = Q.qadc_rms_norm(x, w, r, eps, E4M3)
+            assert torch.isnan(q[1].float()).all() and torch.isnan(q[3].float()).all() and torch.isnan(scale[[1, 3]]).all()
+            dx, _ = Q.qadc_rms_norm_backward(dy, total, w, rstd)
+            assert torch.isnan(dx[[1, 3]]).all()
+            rest = [0, 2, 4]
+            alone = Q.qadc_rms_norm(x[rest], w, r[rest], eps)
+            assert torch.equal(y[rest], alone[0]) and torch.equal(rstd[rest], alone[3]) and torch.equal(
+                dx[rest], Q.qadc_rms_norm_backward(dy[rest], alone[1], w, alone[3])[0])
+
+
 def _equal(a, b):
     return all(p is q is None or torch.equal(p, q) for p, q in zip(a, b))
 
