@@ -77,10 +77,10 @@ class qadc_adapters(ctypes.Structure):
         if a.dim() != 3 or b.dim() != 3 or (b.shape[0], b.shape[2]) != (a.shape[0], a.shape[1]):
             raise ValueError("expected a [count][rank][K] and b [count][N][rank]")
         count, rank, K = a.shape
-        _ptr(a), _ptr(b, a.dtype)
-        super().__init__(a.data_ptr(), b.data_ptr(), _vector(scales, count, torch.float32), _vector(ranks, count, torch.int32),
-                         b.shape[1], K, rank, count, _type(a))
-        self.dtype, self.tensors = a.dtype, (a, b, scales, ranks)
+        device = a.get_device()
+        super().__init__(_ptr(a), _ptr(b, a.dtype, device), _vector(scales, count, torch.float32, device),
+                         _vector(ranks, count, torch.int32, device), b.shape[1], K, rank, count, _type(a))
+        self.dtype, self.device, self.tensors = a.dtype, device, (a, b, scales, ranks)
 
 
 class QadcError(RuntimeError):
@@ -212,11 +212,19 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-def _ptr(t, dtype=None):
+# `device`, of the helpers that look at a tensor: the GPU that it has to be on, in calls that say so (its number costs what is_cuda
+# does).
+def _refusal(t, device, what):
+    if device is not None and t.is_cuda and t.get_device() != device:
+        what = f"tensors of one call on cuda:{device} and cuda:{t.get_device()}"
+    return ValueError(what)
+
+
+def _ptr(t, dtype=None, device=None):
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("tensor must be a contiguous GPU tensor")
+    if not (t.is_cuda if device is None else t.get_device() == device) or not t.is_contiguous():
+        raise _refusal(t, device, "tensor must be a contiguous GPU tensor")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"expected {dtype}, got {t.dtype}")
     return ctypes.c_void_p(t.data_ptr())
@@ -232,11 +240,11 @@ def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _stream_of(t):
-    """The current stream, for a call on t's device, which has to be the current one."""
-    device = torch.cuda.current_device()
-    if t.device.index != device:
-        raise ValueError(f"tensor on cuda:{t.device.index}, the current device is cuda:{device}")
+def _stream_on(device):
+    """The current stream, for a call on tensors of GPU number `device`, which has to be the current one."""
+    current = torch.cuda.current_device()
+    if device != current:
+        raise ValueError(f"tensors on cuda:{device}, the current device is cuda:{current}")
     if _raw_stream is not None:
         return _raw_stream(device)
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
@@ -664,7 +672,7 @@ def _type(t) -> int:
     return _TYPES[t.dtype]
 
 
-def _matrix(t, dtype=None):
+def _matrix(t, dtype=None, device=None):
     """Pointer and row distance of a matrix whose rows are dense but may lie apart."""
     if t.dim() != 2:
         raise ValueError("expected a matrix")
@@ -672,19 +680,19 @@ def _matrix(t, dtype=None):
         raise ValueError(f"expected {dtype}, got {t.dtype}")
     rows, cols = t.shape
     ld = t.stride(0) if rows > 1 else cols
-    if not t.is_cuda or (cols > 1 and rows > 0 and t.stride(1) != 1) or ld < cols:
-        raise ValueError("tensor must be a GPU matrix with dense rows that do not overlap")
+    if not (t.is_cuda if device is None else t.get_device() == device) or (cols > 1 and rows > 0 and t.stride(1) != 1) or ld < cols:
+        raise _refusal(t, device, "tensor must be a GPU matrix with dense rows that do not overlap")
     return t.data_ptr(), ld
 
 
-def _vector(t, n, dtype=None):
+def _vector(t, n, dtype=None, device=None):
     """Pointer of a dense vector of n elements, or None."""
     if t is None:
         return None
     if t.numel() != n:
         raise ValueError(f"expected {n} elements, got {t.numel()}")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("tensor must be a contiguous GPU tensor")
+    if not (t.is_cuda if device is None else t.get_device() == device) or not t.is_contiguous():
+        raise _refusal(t, device, "tensor must be a contiguous GPU tensor")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"expected {dtype}, got {t.dtype}")
     return t.data_ptr()
@@ -700,12 +708,13 @@ def _weight_type(weight, bias, x) -> int:
     return _TYPES[weight.dtype]
 
 
-def _like(t, x):
+def _like(t, x, device=None):
     """The caller's dense output tensor, checked to be one like the matrix x, or a new one."""
     if t is None:
         return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if t.shape != x.shape or t.dtype != x.dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"output must be a contiguous {x.dtype} GPU tensor of {tuple(x.shape)}")
+    if (t.shape != x.shape or t.dtype != x.dtype or not (t.is_cuda if device is None else t.get_device() == device) or
+            not t.is_contiguous()):
+        raise _refusal(t, device, f"output must be a contiguous {x.dtype} GPU tensor of {tuple(x.shape)}")
     return t
 
 
@@ -766,33 +775,35 @@ def qadc_rms_norm(x, weight=None, residual=None, eps=1e-5, out_type=None, sum_ou
     -> (y [rows][d], x + residual [rows][d] of x's type | None, scale f32 [rows] | None, rstd f32 [rows])."""
     rows, d = x.shape
     xp, ldx = _matrix(x)
+    device = x.get_device()
     xtype = ytype = _type(x)
     rp = sp = scale = None
     ldr = ld_sum = d
     if residual is not None:
         if residual.shape != x.shape:
             raise ValueError("residual must have x's shape")
-        rp, ldr = _matrix(residual, x.dtype)
+        rp, ldr = _matrix(residual, x.dtype, device)
         if sum_out is None:
             sum_out = _like(None, x)
         elif sum_out.shape != x.shape:
             raise ValueError(f"sum_out must be {tuple(x.shape)}")
-        sp, ld_sum = _matrix(sum_out, x.dtype)
+        sp, ld_sum = _matrix(sum_out, x.dtype, device)
     elif sum_out is not None:
         raise ValueError("sum_out needs a residual")
     if out_type is None or out_type == x.dtype:
-        y = _like(out, x)
+        y = _like(out, x, device)
     elif out_type == torch.float8_e4m3fn:
         ytype = QADC_TYPE_E4M3
         y = out if out is not None else torch.empty(rows, d, dtype=out_type, device=x.device)
-        if y.shape != x.shape or y.dtype != out_type or not y.is_cuda or not y.is_contiguous():
-            raise ValueError(f"output must be a contiguous {out_type} GPU tensor of {tuple(x.shape)}")
+        if y.shape != x.shape or y.dtype != out_type or y.get_device() != device or not y.is_contiguous():
+            raise _refusal(y, device, f"output must be a contiguous {out_type} GPU tensor of {tuple(x.shape)}")
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     else:
         raise ValueError(f"out_type must be {x.dtype} or torch.float8_e4m3fn")
     rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-    _check(lib().qadc_rms_norm(xp, ldx, rp, ldr, xtype, _vector(weight, d), _weight_type(weight, None, x), rows, d, eps, sp, ld_sum,
-                               y.data_ptr(), ytype, None if scale is None else scale.data_ptr(), rstd.data_ptr(), _stream_of(x)))
+    _check(lib().qadc_rms_norm(xp, ldx, rp, ldr, xtype, _vector(weight, d, None, device), _weight_type(weight, None, x), rows, d, eps, sp,
+                               ld_sum, y.data_ptr(), ytype, None if scale is None else scale.data_ptr(), rstd.data_ptr(),
+                               _stream_on(device)))
     return y, sum_out, scale, rstd
 
 
@@ -806,10 +817,11 @@ def qadc_rms_norm_backward(dy, h, weight, rstd, dsum=None, workspace=None, out=N
     rows, d = h.shape
     if tuple(dy.shape) != (rows, d) or (dsum is not None and tuple(dsum.shape) != (rows, d)):
         raise ValueError("dy and dsum must have h's shape")
-    dyp, lddy = _matrix(dy, h.dtype)
     hp, ldh = _matrix(h)
-    sp, lds = (None, d) if dsum is None else _matrix(dsum, h.dtype)
-    dx = _like(out, h) if need_dx else None
+    device = h.get_device()
+    dyp, lddy = _matrix(dy, h.dtype, device)
+    sp, lds = (None, d) if dsum is None else _matrix(dsum, h.dtype, device)
+    dx = _like(out, h, device) if need_dx else None
     dw = None
     size = 0
     if need_weight:
@@ -817,9 +829,9 @@ def qadc_rms_norm_backward(dy, h, weight, rstd, dsum=None, workspace=None, out=N
         workspace, size = _scratch(workspace, qadc_rms_norm_workspace_bytes, (rows, d), h.device)
     else:
         workspace = None
-    _check(lib().qadc_rms_norm_backward(dyp, lddy, sp, lds, hp, ldh, _type(h), _vector(weight, d), _weight_type(weight, None, h),
-                                        _vector(rstd, rows, torch.float32), rows, d, _ptr(dx), _ptr(dw), _ptr(workspace), size,
-                                        _stream_of(h)))
+    _check(lib().qadc_rms_norm_backward(dyp, lddy, sp, lds, hp, ldh, _type(h), _vector(weight, d, None, device),
+                                        _weight_type(weight, None, h), _vector(rstd, rows, torch.float32, device), rows, d, _ptr(dx), _ptr(dw),
+                                        _ptr(workspace, None, device), size, _stream_on(device)))
     return dx, dw
 
 
@@ -864,13 +876,13 @@ def qadc_token_logprobs_workspace_bytes(rows: int, V: int, k: int) -> int:
     return int(lib().qadc_token_logprobs_workspace_bytes(rows, V, k))
 
 
-def _tokens(tokens, rows):
+def _tokens(tokens, rows, device=None):
     """Pointer and number per row of the given tokens, i32 [rows][T] or None."""
     if tokens is None:
         return None, 0
     if tokens.dim() != 2 or tokens.shape[0] != rows:
         raise ValueError(f"expected tokens [{rows}][T]")
-    return _ptr(tokens, torch.int32), tokens.shape[1]
+    return _ptr(tokens, torch.int32, device), tokens.shape[1]
 
 
 def qadc_token_logprobs(logits, tokens=None, k=0, scale=1.0, workspace=None):
@@ -920,31 +932,32 @@ def qadc_add_adapters(adapters, ids, x, base=None, out=None, workspace=None):
     M, K = x.shape
     if K != adapters.K:
         raise ValueError(f"adapters of {adapters.K} inputs, x of {K}")
-    xp, ldx = _matrix(x, adapters.dtype)
+    device = adapters.device
+    xp, ldx = _matrix(x, adapters.dtype, device)
     bp, ldb = None, adapters.N
     if base is not None:
         if tuple(base.shape) != (M, adapters.N):
             raise ValueError(f"base must be {(M, adapters.N)}")
-        bp, ldb = _matrix(base, adapters.dtype)
+        bp, ldb = _matrix(base, adapters.dtype, device)
     if out is None:
         out = torch.empty(M, adapters.N, dtype=adapters.dtype, device=x.device)
     elif tuple(out.shape) != (M, adapters.N):
         raise ValueError(f"output must be {(M, adapters.N)}")
-    yp, ldy = _matrix(out, adapters.dtype)
+    yp, ldy = _matrix(out, adapters.dtype, device)
     if workspace is None:
         workspace = torch.empty((max(256, qadc_adapters_workspace_bytes(adapters, M)),), dtype=torch.uint8, device=x.device)
-    _check(lib().qadc_add_adapters(ctypes.byref(adapters), _vector(ids, M, torch.int32), xp, ldx, M, bp, ldb, yp, ldy, _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream_of(x)))
+    _check(lib().qadc_add_adapters(ctypes.byref(adapters), _vector(ids, M, torch.int32, device), xp, ldx, M, bp, ldb, yp, ldy,
+                                   _ptr(workspace, None, device), workspace.numel() * workspace.element_size(), _stream_on(device)))
     return out
 
 
-def _teacher(top_idx, top_logp, rows):
+def _teacher(top_idx, top_logp, rows, device):
     """Pointers and number per row of a teacher's stored tokens and log probabilities."""
     if top_idx.dim() != 2 or top_idx.shape[0] != rows or top_logp.shape != top_idx.shape:
         raise ValueError(f"expected top_idx and top_logp [{rows}][k]")
     if top_idx.dtype not in (torch.int32, torch.uint32):
         raise ValueError(f"expected 32-bit indexes, got {top_idx.dtype}")
-    return _ptr(top_idx), _ptr(top_logp, torch.float32), top_idx.shape[1]
+    return _ptr(top_idx, None, device), _ptr(top_logp, torch.float32, device), top_idx.shape[1]
 
 
 def qadc_distill_workspace_bytes(rows: int, V: int) -> int:
@@ -956,12 +969,13 @@ def qadc_distill(logits, top_idx, top_logp, scale=1.0, tail=True, workspace=None
     (qadc_token_logprobs) -> (loss f32 [rows], lse f32 [rows], log_tail f32 [rows])."""
     rows, V = logits.shape
     xp, ld = _matrix(logits)
-    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    device = logits.get_device()
+    ip, lp, k = _teacher(top_idx, top_logp, rows, device)
     loss, lse = _pair(logits.device, rows)
     log_tail = torch.empty_like(loss)
     workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
     _check(lib().qadc_distill(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), loss.data_ptr(), lse.data_ptr(),
-                              log_tail.data_ptr(), _ptr(workspace), size, _stream_of(logits)))
+                              log_tail.data_ptr(), _ptr(workspace, None, device), size, _stream_on(device)))
     return loss, lse, log_tail
 
 
@@ -971,7 +985,7 @@ def _gradient_like(out, logits):
         out = _like(None, logits)
     elif out.shape != logits.shape:
         raise ValueError(f"output must be {tuple(logits.shape)}")
-    return (out, *_matrix(out, logits.dtype))
+    return (out, *_matrix(out, logits.dtype, logits.get_device()))
 
 
 def qadc_distill_backward(logits, top_idx, top_logp, lse, log_tail, dloss, scale=1.0, tail=True, out=None):
@@ -979,11 +993,12 @@ def qadc_distill_backward(logits, top_idx, top_logp, lse, log_tail, dloss, scale
     type."""
     rows, V = logits.shape
     xp, ld = _matrix(logits)
-    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    device = logits.get_device()
+    ip, lp, k = _teacher(top_idx, top_logp, rows, device)
     out, op, ldd = _gradient_like(out, logits)
     f32 = torch.float32
-    _check(lib().qadc_distill_backward(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), _vector(lse, rows, f32),
-                                       _vector(log_tail, rows, f32), _vector(dloss, rows, f32), op, ldd, _stream_of(logits)))
+    _check(lib().qadc_distill_backward(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)), _vector(lse, rows, f32, device),
+                                       _vector(log_tail, rows, f32, device), _vector(dloss, rows, f32, device), op, ldd, _stream_on(device)))
     return out
 
 
@@ -992,12 +1007,14 @@ def qadc_distill_step(logits, top_idx, top_logp, weight, scale=1.0, tail=True, o
     -> (loss f32 [rows], gradient [rows][V] of the logits' type)."""
     rows, V = logits.shape
     xp, ld = _matrix(logits)
-    ip, lp, k = _teacher(top_idx, top_logp, rows)
+    device = logits.get_device()
+    ip, lp, k = _teacher(top_idx, top_logp, rows, device)
     out, op, ldd = _gradient_like(out, logits)
     loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
     workspace, size = _scratch(workspace, qadc_distill_workspace_bytes, (rows, V), logits.device)
     _check(lib().qadc_distill_step(xp, ld, _type(logits), rows, V, scale, ip, lp, k, int(bool(tail)),
-                                   _vector(weight, rows, torch.float32), loss.data_ptr(), op, ldd, _ptr(workspace), size, _stream_of(logits)))
+                                   _vector(weight, rows, torch.float32, device), loss.data_ptr(), op, ldd, _ptr(workspace, None, device), size,
+                                   _stream_on(device)))
     return loss, out
 
 
@@ -1008,8 +1025,9 @@ def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetiti
     i32 [rows], each | None -> adjusted logits [rows][V] of their type."""
     rows, V = logits.shape
     xp, ld = _matrix(logits)
-    hp, H = _tokens(history, rows)
-    bp, B = _tokens(bias_tokens, rows)
+    device = logits.get_device()
+    hp, H = _tokens(history, rows, device)
+    bp, B = _tokens(bias_tokens, rows, device)
     if (bias is None) != (bias_tokens is None):
         raise ValueError("bias and bias_tokens belong together")
     if history is None and not (lengths is prompt is repetition is presence is frequency is None):
@@ -1018,7 +1036,7 @@ def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetiti
     if masks is not None:
         if masks.dtype not in (torch.int32, torch.uint32):
             raise ValueError(f"expected masks of 32-bit words, got {masks.dtype}")
-        mp, ldm = _matrix(masks)
+        mp, ldm = _matrix(masks, None, device)
         states = masks.shape[0]
         if masks.shape[1] < -(-V // 32):
             raise ValueError(f"expected masks of {-(-V // 32)} words")
@@ -1028,12 +1046,13 @@ def qadc_adjust_logits(logits, history=None, lengths=None, prompt=None, repetiti
         out = _like(None, logits)
     elif tuple(out.shape) != (rows, V):
         raise ValueError(f"output must be {(rows, V)}")
-    op, ldo = _matrix(out, logits.dtype)
+    op, ldo = _matrix(out, logits.dtype, device)
     f32, i32 = torch.float32, torch.int32
-    _check(lib().qadc_adjust_logits(xp, ld, _type(logits), rows, V, hp, H, _vector(lengths, rows, i32), _vector(prompt, rows, i32),
-                                    _vector(repetition, rows, f32), _vector(presence, rows, f32), _vector(frequency, rows, f32), bp,
-                                    _vector(bias, rows * B, f32), B, mp, ldm, states, _vector(mask_of, rows, i32), op, ldo,
-                                    _stream_of(logits)))
+    _check(lib().qadc_adjust_logits(xp, ld, _type(logits), rows, V, hp, H, _vector(lengths, rows, i32, device),
+                                    _vector(prompt, rows, i32, device), _vector(repetition, rows, f32, device),
+                                    _vector(presence, rows, f32, device), _vector(frequency, rows, f32, device), bp,
+                                    _vector(bias, rows * B, f32, device), B, mp, ldm, states, _vector(mask_of, rows, i32, device), op,
+                                    ldo, _stream_on(device)))
     return out
 
 
