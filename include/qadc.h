@@ -620,7 +620,7 @@ int qadc_token_logprobs_backward(const void *logits, int64_t ld, int type, int64
  * Terms with p = 0 or r = 0 are 0; a row whose teacher is empty (P = 0, tail == 0) has loss 0.  Where Q is 0 (every token is
  * stored, a mask of -inf leaves no other, or it is below 1e-37) the tail's term is left out.  A stored token that the student's mask
  * excludes makes the loss +inf.  A token that is stored twice has both its terms, and counts once for the student.  A row that
- * holds a NaN or +inf has loss NaN; a row with nothing left lse = log Q = -inf.
+ * holds a NaN or +inf has loss NaN, whatever its teacher; a row with nothing left lse = log Q = -inf.
  * Sums over the vocabulary are in float32, the teacher's probabilities and the loss in float64, rounded to float32.
  *   logits [rows][ld] of `type`, V <= ld of them per row, 1 <= V <= 2^31 - 65537;  0 < scale <= 2e38
  *   top_idx [rows][k] u32, top_logp [rows][k] f32, 0 <= k <= QADC_MAX_ALTERNATIVES: an index >= V (0xFFFFFFFF) is an unused slot

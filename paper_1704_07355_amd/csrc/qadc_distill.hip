@@ -186,7 +186,7 @@ __device__ __forceinline__ void finish_row(Part2 others, const WaveStored &st, i
     l = wave_sum64(l);
     if (lane_id() == 0) {
         if (mass.rest > 0.0 && log_tail != -INFINITY) l += mass.rest * (log(mass.rest) - log_tail);
-        o.loss[r] = (float)l;
+        o.loss[r] = log_s == log_s ? (float)l : NAN;  // (a broken row is one to an empty teacher too)
         if (o.lse) {
             const float lse = (float)((double)scale * (double)m + log_s);  // (no float holds it: NaN)
             o.lse[r] = none ? -INFINITY : fabsf(lse) < INFINITY ? lse : NAN;
@@ -596,7 +596,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_step_kernel(const T *logit
         double l = 0.0;
 #pragma unroll
         for (int v = 0; v < DS_WAVES; ++v) l += lds.loss[v];
-        loss[r] = (float)l;
+        loss[r] = sum == sum ? (float)l : NAN;  // (a broken row is one to an empty teacher too)
     }
 }
 

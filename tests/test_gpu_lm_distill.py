@@ -224,6 +224,28 @@ def test_a_student_that_gives_the_tail_next_to_nothing(rows):
     assert grad[others].abs().max() < 2.0 ** -99 and step[others].abs().max() < 2.0 ** -99
 
 
+@pytest.mark.parametrize("rows,V", [(6, 500), (200, 500), (6, 50021), (130, 70001)])
+def test_broken_rows_of_an_empty_teacher(rows, V):
+    """A NaN or an infinity shows in the loss as it does in the gradient, whatever the teacher says; without one an empty teacher has none."""
+    import paper_1704_07355_amd as Q
+    for type in TYPES:
+        x, idx, logp, w = _inputs(rows, V, 12, type, 5)
+        w = w.abs() + 0.1
+        idx[:4] = -1
+        x[0, V - 1], x[1, V // 2], x[2] = math.nan, math.inf, -math.inf
+        x[4, 7] = math.nan
+        for tail in (True, False):
+            for teacher in ((idx, logp), (idx[:, :0].contiguous(), logp[:, :0].contiguous())):
+                loss, lse, log_tail = Q.qadc_distill(x, *teacher, 1.0, tail)
+                step_loss, step = Q.qadc_distill_step(x, *teacher, w, 1.0, tail)
+                grad = Q.qadc_distill_backward(x, *teacher, lse, log_tail, w, 1.0, tail)
+                for t in (loss, step_loss, step.float(), grad.float()):
+                    assert torch.isnan(t[[0, 1, 4]]).all() and not torch.isnan(t[[2, 3, 5]]).any()
+                assert loss[2] == step_loss[2] == 0 and (step[2] == 0).all() and (grad[2] == 0).all()
+                if not tail:
+                    assert loss[3] == step_loss[3] == 0 and (step[3] == 0).all() and (grad[3] == 0).all()
+
+
 @pytest.mark.parametrize("type", list(TYPES))
 @pytest.mark.parametrize("rows,V,k", [(4, 400, 12), (160, 400, 12), (3, 7001, 128), (70, 60001, 20), (90, 131072, 40), (2, 140001, 9)])
 def test_a_tail_of_any_depth_counts(rows, V, k, type):
