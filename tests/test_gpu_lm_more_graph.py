@@ -179,3 +179,21 @@ def test_a_padded_batch_gives_what_its_rows_give():
     room = torch.full((ROWS, V), 7.0, dtype=torch.bfloat16, device=DEV)
     Q.qadc_add_adapters(work.adapters, work.ids[:n], state, torch.zeros((n, V), dtype=torch.bfloat16, device=DEV), out=room[:n])
     assert (room[n:] == 7.0).all()
+
+
+def test_the_rows_of_a_shorter_batch_have_the_bits_of_the_longer_one():
+    """The first rows alone, beside rows that hold something else: outputs in 8 bits, adapters on the shared product, log probabilities."""
+    import paper_1704_07355_amd as Q
+    work = Decode()
+    work.fill(6)
+    state, total, rstd, small, scale, adapted, ruled, lse, entropy, top, top_logp = work.step()
+    logits = Q.qadc_linear4(work.head, state)
+    for n in (1, 4, 5):
+        q, _, s, r = Q.qadc_rms_norm(work.x[:n], work.weight, work.residual[:n], out_type=torch.float8_e4m3fn)
+        assert torch.equal(q.view(torch.uint8), small[:n]) and torch.equal(s, scale[:n]) and torch.equal(r, rstd[:n])
+        room = torch.full((ROWS, V), 7.0, dtype=torch.bfloat16, device=DEV)
+        Q.qadc_add_adapters(work.adapters, work.ids[:n], state[:n], logits[:n], out=room[:n], workspace=work.ws)
+        # (256 inputs are not cut, for however many rows)
+        assert torch.equal(room[:n], adapted[:n]) and (room[n:] == 7.0).all()
+        got = Q.qadc_token_logprobs(ruled[:n], k=10, workspace=work.ws)
+        assert _same(got[1:], (lse[:n], entropy[:n], top[:n], top_logp[:n]))
