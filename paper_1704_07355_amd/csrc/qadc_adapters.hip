@@ -27,6 +27,8 @@ namespace {
 constexpr int AD_WG = 256, AD_TILE = 256;  // threads; rows of a tile, one a thread
 // Rows from which on an item has 64 of them, if each adapter has as many: the pool is read a quarter as often.  4990 rows of 42 adapters of
 // rank 16, 7754 x 742, 47 us for 118 with 16 rows; 400 rows of one of rank 94, 15312 x 1581 float32, 115 for 69 the other way round.
+// In any order a tile of many adapters has few rows of each, and the pool is read again for every tile: 8192 rows of rank 64, 4096 x 4096, bfloat16,
+// in segments and in any order: 16 adapters 81 us and 151, 32 86 and 237, 64 95 and 478, 128 120 and 860.
 constexpr int64_t AD_MANY = 1024;
 constexpr int AD_COLS = 64;                // outputs of a wavefront at a time
 constexpr int64_t AD_GROUPS = ((int64_t)1 << 32) / AD_WG;  // of a launch, less one: their threads are counted in 32 bits
@@ -283,7 +285,8 @@ constexpr int AD_TURN = 68;  // floats from row to row
 __device__ __forceinline__ int eight_at(int rank, int j) { return min(j, max(rank - 8, 0)); }
 
 // y of the rows of an item, `blocks` times 64 outputs a wavefront; STEPS times 32 ranks at most.  The last block of outputs begins 64
-// before the end, and writes what no other has.  SMALL: fewer than eight ranks or 64 outputs, read and written one by one.  What the
+// before the end, and writes what no other has.  SMALL: fewer than eight ranks or 64 outputs, read and written one by one (8192 rows of 4096 x
+// 4096 bfloat16 in segments, four ranks 127 us where eight take 51; 64 rows of 16384 outputs 23.5 and 13.1; one row 10 and 10).  What the
 // first outputs need of the pool and of base is on its way while u is added up.
 template <typename T, int RB, int STEPS, bool SMALL>
 __global__ __launch_bounds__(AD_WG, sizeof(T) == 2 && STEPS * RB <= 4 && !SMALL ? 3 : 2) void adapters_up_kernel(Pool pool, const int32_t *__restrict__ ids, int64_t M, int slots, int chunks,

@@ -11,8 +11,9 @@
 //
 // Bound by memory in large calls: 4096 x 65536 bfloat16, loss and gradient in one call, 228 us, 4.7 TB/s read and written (the row lies
 // in registers between them, so that a compute unit loads or stores at a time, not both); 512 x 128001 74 us, two
-// rounds of one workgroup a compute unit; the gradient alone, 1111 x 32003 float32, 56 us, 5.1 TB/s.  Small calls are bound by the host and
-// the launches: 48 x 50021 binary16, loss alone, 14 us, parts 5.2 and join 6.4.
+// rounds of one workgroup a compute unit; the gradient alone, 1111 x 32003 float32, 57 us, 5.0 TB/s, in calls one after the other that share their
+// output, 70 us, 4.1 TB/s, with a new one in every call.  Small calls are bound by the host and the launches: 48 x 50021 binary16, loss alone,
+// 14 us, parts 5.2 and join 6.4.  Tails below 2^-80 of every row are summed twice: 4096 x 65536 261 us in one call, and in two as others.
 #include <algorithm>
 
 #include "qadc_logits.h"
@@ -668,8 +669,10 @@ static void launch_grad(const void *logits, int64_t ld, int64_t rows, int V, flo
     // and 12.7, 128 x 128001 19.6 and 20.9, 512 x 128001 57.7 and 50.9.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(4, chunks * rows / 2048));
     const int parts = (int)ceil_div(chunks, most), per = (int)ceil_div(chunks, parts);
-    // A gradient beyond the last cache's size goes past it: 2048 x 128001 bfloat16 203 us and 229 (with six sets of inputs in turn 213 and 213),
-    // but 512 x 128001 59 and 51.
+    // A gradient beyond the last cache's size goes past it: with inputs that change 2048 x 128001 bfloat16 211 us and 226, 4096 x 65536 190 and 211,
+    // 4096 x 50257 float32 351 and 363, 8192 x 128001 878 and 868; but 512 x 128001 59 and 51.  Between the products of a training step the
+    // gradient itself is slower past the caches (2048 x 128001 236 and 207) and the product behind it faster: both 1220 and 1224 there, 4096 x
+    // 65536 1001 and 1012, 8192 x 65536 1194 and 1261.
     const bool stream = (size_t)rows * V * sizeof(T) > ((size_t)384 << 20);
     const auto kernel = stream ? &distill_grad_kernel<T, true> : &distill_grad_kernel<T, false>;
     launch(QADC_PROF_DISTILL, kernel, dim3((unsigned)std::min<int64_t>(rows * parts, 1 << 22)), dim3(LP_WG), 0, st, (const T *)logits, ld,

@@ -10,7 +10,8 @@
 // comes in while this one is reduced.  Longer rows are read again for the output.
 //
 // Bound by memory: forward with a residual 16384 x 4096 bfloat16 82 us, 6.5 TB/s read and written (float32 190); backward with the residual's
-// gradient 91 us for the rows, 5.9 TB/s, and 5 for joining the workgroups' sums.  Small calls are bound by the host: 5 x 4096 with a
+// gradient 91 us for the rows, 5.9 TB/s, and 5 for joining the workgroups' sums.  In 8 bits a call takes 84 us where y takes 87 (float32 159 and
+// 187).  Without an eps ordinary rows take as long, rows with squares below float32 130 (float32 195).  Small calls are bound by the host: 5 x 4096 with a
 // residual to 8 bits 14 us a call, kernel 3.4.  3001 x 1537 float32 backward: rows 14 us in three turns a workgroup, each of which exposes a
 // load and a barrier, join 6.
 #include <type_traits>
