@@ -12,6 +12,14 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
 
 
+@pytest.fixture
+def memory_back():
+    """For tests of many gigabytes: what torch keeps of them goes back, before others allocate and are timed."""
+    yield
+    import torch
+    torch.cuda.empty_cache()
+
+
 @pytest.fixture(scope="session")
 def tiny_pq():
     """Config-1-shaped PQ at reduced size: d=128, m=16 x 16 centroids, trained by the oracle."""

@@ -99,7 +99,7 @@ def test_mixed_rows(M, N, K, rank, count, type):
     assert torch.equal(_check(w, ids, x, again, out=again), y)  # in place
 
 
-def test_more_outputs_than_a_launch_has_workgroups_for():
+def test_more_outputs_than_a_launch_has_workgroups_for(memory_back):
     """256 rows, each of which may open an item, by 2^27 outputs and some: the pool repeats itself, and so has the result to."""
     import paper_1704_07355_amd as Q
     M, N, K, rank, count, period = 256, (1 << 27) + 4096, 40, 8, 4, 4096

@@ -166,7 +166,7 @@ def test_gradient_by_differences(rows, d):
         assert abs(got - want) <= 20 * h * h * abs(got) + 2.0 ** -22 * size * 4 / h, (at, got, want)
 
 
-def test_the_gradients_of_very_long_weights():
+def test_the_gradients_of_very_long_weights(memory_back):
     """More columns than the threads of a launch in one direction reach, sixteen for each of both sums, would be."""
     import paper_1704_07355_amd as Q
     rows, d = 2, (1 << 27) + 37

@@ -253,7 +253,7 @@ def test_rows_beyond_the_smallest_reciprocal(type):
     assert torch.isnan(q.float()).all() and torch.isnan(scale).all()
 
 
-def test_the_gradient_of_a_very_long_weight():
+def test_the_gradient_of_a_very_long_weight(memory_back):
     """More columns than the threads of a launch in one direction reach, sixteen a column, would be."""
     import paper_1704_07355_amd as Q
     rows, d = 2, (1 << 28) + 37
