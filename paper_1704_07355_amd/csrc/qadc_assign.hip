@@ -1131,6 +1131,9 @@ static void launch_filter(const float *coarse, int K, int d, const float *x, int
 static int assign_pass(const float *coarse, int K, int d, const float *x, int64_t ldx, int64_t n, int32_t *cells,
                        int scale, int accumulate, hipStream_t st)
 {
+    constexpr int64_t SLAB = 1ll << 30;  // (two threads a vector, and a launch's are counted in 32 bits)
+    for (; n > SLAB; x += SLAB * ldx, cells += SLAB, n -= SLAB)
+        if (const int rc = assign_pass(coarse, K, d, x, ldx, SLAB, cells, scale, accumulate, st)) return rc;
     const bool filter = d <= AF_MAX_D && K <= ASG_MARK_MAX_K;
     const int range = (int)std::min<int64_t>(ASG_RANGE, std::max<int64_t>(256, ceil_div(ceil_div(n, 1024), ASG_TM) * ASG_TM));
     if (!filter)

@@ -86,4 +86,13 @@ __device__ __forceinline__ unsigned wave_append_slot(bool pred, unsigned *counte
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t align_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
 
+// A launch's threads in one direction are counted in 32 bits, and those beyond are dropped without an error: very many workgroups lie in two
+// directions.  The last few may be beyond `wgs`.
+static inline dim3 grid_of(int64_t wgs, int threads)
+{
+    const int64_t down = ceil_div(wgs, ((1ll << 32) - 1) / threads);
+    return dim3((unsigned)ceil_div(wgs, down), (unsigned)down);
+}
+__device__ __forceinline__ int64_t workgroup() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 }  // namespace qadc

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void pq_encode_kernel(
     const int dsub = DS ? DS : d / m;
     const int row = KSUB == 16 ? m / 2 : KSUB == 64 ? 3 * (m / 4) : m;
     const int groups = (m + COMPS - 1) / COMPS;
-    const int64_t unit = (int64_t)blockIdx.x * (256 / WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int64_t unit = workgroup() * (256 / WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int64_t block = unit / groups;
     const int gr = (int)(unit - block * groups);
     const int64_t r = block * WAVE + (threadIdx.x & (WAVE - 1));
@@ -125,13 +125,12 @@ static int encode_launch(const char *name, const float *codebooks, int d, int m,
     if (!codebooks || !x || !codes) return fail(QADC_EINVAL, "%s: null pointer", name);
     const int groups = (int)ceil_div(m, ksub == 16 ? 8 : 4);
     const int64_t blocks = ceil_div(ceil_div(n, WAVE) * groups, 256 / WAVE);
-    if (ceil_div(n * (ksub == 16 ? m / 2 : ksub == 64 ? m / 4 : m), 256) > 0x7fffffffll || blocks > 0x7fffffffll)
-        return fail(QADC_EINVAL, "%s: n too large for one call", name);
+    if (blocks > 0x7fffffffll) return fail(QADC_EINVAL, "%s: n too large for one call", name);
     // Sub-vectors of the usual dimensions stay in registers; with 16 centroids, whose walk is short, all up to 20 do (500 k
     // vectors of 16 x 5 components 46 us; the general form, which waits for its scalar loads, took 221).
 #define QADC_ENC(K_, D_)                                                                                    \
     case D_:                                                                                                \
-        hipLaunchKernelGGL((pq_encode_kernel<K_, D_>), dim3((unsigned)blocks), dim3(256), 0, st, codebooks, d, m, x, \
+        hipLaunchKernelGGL((pq_encode_kernel<K_, D_>), grid_of(blocks, 256), dim3(256), 0, st, codebooks, d, m, x, \
                            n, codes, cc, cells, ids, n_x);                                                  \
         break;
 #define QADC_ENC_DS(K_, ...)                                                                                \
@@ -139,7 +138,7 @@ static int encode_launch(const char *name, const float *codebooks, int d, int m,
     QADC_ENC(K_, 1) QADC_ENC(K_, 2) QADC_ENC(K_, 3) QADC_ENC(K_, 4) QADC_ENC(K_, 6) QADC_ENC(K_, 8) QADC_ENC(K_, 12) QADC_ENC(K_, 16) \
     __VA_ARGS__                                                                                             \
     default:                                                                                                \
-        hipLaunchKernelGGL((pq_encode_kernel<K_, 0>), dim3((unsigned)blocks), dim3(256), 0, st, codebooks, d, m, x, \
+        hipLaunchKernelGGL((pq_encode_kernel<K_, 0>), grid_of(blocks, 256), dim3(256), 0, st, codebooks, d, m, x, \
                            n, codes, cc, cells, ids, n_x);                                                  \
     }
     if (ksub == 16) {

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(LAYOUT_NT) void relayout_kernel(const uint8_t *__re
 {
     __shared__ __attribute__((aligned(16))) uint8_t tile[LAYOUT_NT * 16];
     const int tid = threadIdx.x;
-    const int64_t piece = (int64_t)blockIdx.x * LAYOUT_NT + tid;   // global 16-byte piece
+    const int64_t piece = workgroup() * LAYOUT_NT + tid;   // global 16-byte piece
     const int64_t std_bytes = n * B;                                // bytes of the standard list
     const int64_t nblk = (n + 15) / 16;
     const int64_t pieces = nblk * B;
@@ -103,9 +103,9 @@ int relayout(bool pack, const uint8_t *src, int64_t n, int m, int layout, uint8_
     const int64_t grid = ceil_div(pieces, LAYOUT_NT);
     if (grid > 0x7fffffffll) return fail(QADC_EINVAL, "%s: n too large for one call", name);
     if (pack)
-        hipLaunchKernelGGL(relayout_kernel<true>, dim3((unsigned)grid), dim3(LAYOUT_NT), 0, st, src, n, B, dst);
+        hipLaunchKernelGGL(relayout_kernel<true>, grid_of(grid, LAYOUT_NT), dim3(LAYOUT_NT), 0, st, src, n, B, dst);
     else
-        hipLaunchKernelGGL(relayout_kernel<false>, dim3((unsigned)grid), dim3(LAYOUT_NT), 0, st, src, n, B, dst);
+        hipLaunchKernelGGL(relayout_kernel<false>, grid_of(grid, LAYOUT_NT), dim3(LAYOUT_NT), 0, st, src, n, B, dst);
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }

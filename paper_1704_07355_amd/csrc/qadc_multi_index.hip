@@ -34,7 +34,7 @@ constexpr int MI_MAX_PAIRS = 2048;   // sum over a of floor(256 / a) = 1546
 __global__ __launch_bounds__(256) void mi_cells_kernel(const float *__restrict__ halves, int K, int dh,
                                                        float *__restrict__ coarse, int64_t total)
 {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t e = workgroup() * 256 + threadIdx.x;
     if (e >= total) return;
     const int d = 2 * dh;
     const int64_t cell = e / d;
@@ -127,7 +127,7 @@ int multi_index_cells(const float *halves, int K, int d, float *coarse, hipStrea
     const int64_t total = (int64_t)K * K * d;
     const int64_t grid = ceil_div(total, 256);
     if (grid > 0x7fffffffll) return fail(QADC_EINVAL, "qadc_multi_index_cells: K*K*d too large");
-    hipLaunchKernelGGL(mi_cells_kernel, dim3((unsigned)grid), dim3(256), 0, st, halves, K, d / 2, coarse, total);
+    hipLaunchKernelGGL(mi_cells_kernel, grid_of(grid, 256), dim3(256), 0, st, halves, K, d / 2, coarse, total);
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(256) void mi_slots_kernel(const uint32_t *__restric
                                                        const int32_t *__restrict__ cells, int64_t count,
                                                        int32_t *__restrict__ slots)
 {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t e = workgroup() * 256 + threadIdx.x;
     if (e >= count) return;
     const int32_t c = cells[e];
     int32_t out = -1;
@@ -221,7 +221,7 @@ int multi_index_slots(const uint32_t *cell_ids, int64_t n_lists, const int32_t *
     if (!cells || !slots || (n_lists > 0 && !cell_ids)) return fail(QADC_EINVAL, "qadc_multi_index_slots: null pointer");
     const int64_t grid = ceil_div(count, 256);
     if (grid > 0x7fffffffll) return fail(QADC_EINVAL, "qadc_multi_index_slots: count too large for one call");
-    launch(QADC_PROF_IVF_INDEX, mi_slots_kernel, dim3((unsigned)grid), dim3(256), 0, st, cell_ids, n_lists, cells,
+    launch(QADC_PROF_IVF_INDEX, mi_slots_kernel, grid_of(grid, 256), dim3(256), 0, st, cell_ids, n_lists, cells,
            count, slots);
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;

@@ -182,7 +182,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const float *__restrict
 {
     __shared__ float lds[16][WAVE];
     const int wave = threadIdx.x >> 6, lane = lane_id();
-    const int64_t c = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * WAVE + lane;
+    const int64_t c = workgroup() * WAVE + lane;
     float s = 0.0f;
     if (c < 2 * (int64_t)d) {
 #pragma unroll 16
@@ -416,12 +416,9 @@ static void norm_backward_launch(const void *dy, int64_t lddy, const void *x, in
         launch(QADC_PROF_NORM, norm_weights_kernel<T>, dim3((unsigned)ceil_div(d, NORM_WG), (unsigned)count), dim3(NORM_WG), 0,
                st, (const T *)dy, lddy, (const T *)x, ldx, mean, rstd, rows, d, ceil_div(rows, count), parts);
     }
-    if (sums) {
-        // (a grid's threads in one direction are counted in 32 bits)
-        const int64_t wgs = ceil_div(2 * (int64_t)d, WAVE), across = std::min<int64_t>(wgs, 1 << 20);
-        launch(QADC_PROF_NORM, norm_join_kernel, dim3((unsigned)across, (unsigned)ceil_div(wgs, across)), dim3(1024), 0, st, parts, count,
-               d, dweight, dbias);
-    }
+    if (sums)
+        launch(QADC_PROF_NORM, norm_join_kernel, grid_of(ceil_div(2 * (int64_t)d, WAVE), 1024), dim3(1024), 0, st, parts, count, d,
+               dweight, dbias);
     if (dx && rows > 0 && d > NORM_LONG)
         launch(QADC_PROF_NORM, norm_dx_kernel<T, W>, dim3(norm_grid(rows)), dim3(NORM_WG), 0, st, (const T *)dy, lddy,
                (const T *)x, ldx, (const W *)weight, mean, rstd, rows, d, (T *)dx);

@@ -333,7 +333,7 @@ __global__ __launch_bounds__(1024) void rms_join_kernel(const float *__restrict_
 {
     __shared__ float lds[16][WAVE];
     const int wave = threadIdx.x >> 6, lane = lane_id();
-    const int64_t c = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * WAVE + lane;
+    const int64_t c = workgroup() * WAVE + lane;
     float s = 0.0f;
     if (c < d) {
 #pragma unroll 16
@@ -653,12 +653,9 @@ int rms_norm_backward(const void *dy, int64_t lddy, const void *dsum, int64_t ld
             }
         });
     }
-    if (dweight) {
-        // (a grid's threads in one direction are counted in 32 bits)
-        const int64_t wgs = ceil_div(d, WAVE), across = std::min<int64_t>(wgs, 1 << 20);
-        launch(QADC_PROF_RMS, rms_join_kernel, dim3((unsigned)across, (unsigned)ceil_div(wgs, across)), dim3(1024), 0, st,
-               (const float *)b.parts, count, d, dweight);
-    }
+    if (dweight)
+        launch(QADC_PROF_RMS, rms_join_kernel, grid_of(ceil_div(d, WAVE), 1024), dim3(1024), 0, st, (const float *)b.parts, count, d,
+               dweight);
     QADC_HIP_TRY(hipGetLastError());
     return QADC_OK;
 }

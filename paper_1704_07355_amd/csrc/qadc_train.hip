@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void train_assign_kernel(const float *__restri
                                                            const float *__restrict__ cb, uint8_t *__restrict__ labels)
 {
     const int dsub = DS ? DS : d / m;
-    const int64_t unit = (int64_t)blockIdx.x * (256 / WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int64_t unit = workgroup() * (256 / WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int64_t block = unit / m;
     const int j = (int)(unit - block * m);
     if (block * WAVE >= n) return;  // uniform
@@ -52,7 +52,7 @@ template <int KSUB>
 static void launch_train_assign(const float *train, int64_t n, int d, int m, const float *cb, uint8_t *labels,
                                 hipStream_t st)
 {
-    const dim3 grid((unsigned)ceil_div(ceil_div(n, WAVE) * m, 256 / WAVE));
+    const dim3 grid = grid_of(ceil_div(ceil_div(n, WAVE) * m, 256 / WAVE), 256);
 #define QADC_ASG(D_)                                                                                          \
     case D_:                                                                                                  \
         hipLaunchKernelGGL((train_assign_kernel<KSUB, D_>), grid, dim3(256), 0, st, train, n, d, m, cb, labels); \

@@ -113,7 +113,8 @@ def test_more_outputs_than_a_launch_has_workgroups_for(memory_back):
     within(y[:, :period], want, tol, "y")
     for r in range(M):
         row = y[r].view(-1, period)
-        assert torch.equal(row, row[:1].expand(row.shape)), r
+        same = torch.equal(row, row[:1].expand(row.shape))
+        assert same, r
 
 
 def test_more_rows_than_tiles_with_a_workgroup_for_each_row():
